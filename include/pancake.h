@@ -70,7 +70,13 @@ extern "C" {
 typedef struct pk_index pk_index; /* opaque per-agent handle (host object) */
 
 typedef enum { PK_METRIC_IP = 0, PK_METRIC_L2 = 1 } pk_metric;
-typedef enum { PK_F32 = 0, PK_F16 = 1 } pk_dtype; /* storage type of list vectors */
+typedef enum {
+    PK_F32 = 0,
+    PK_F16 = 1,  /* these two: storage types of list vectors                           */
+    PK_BF16 = 2, /* rows of a key/value cache's callers, and its storage types: the     */
+    PK_I8 = 3,   /* 16-bit ones, and codes of 8 bits with a scale for each row          */
+    PK_F8 = 4    /* (e4m3)                                                              */
+} pk_dtype;
 
 typedef enum {
     PK_OK = 0,
@@ -412,6 +418,123 @@ int pk_profile_end(pk_index *index, pk_profile *out, void *stream);
 /* Frees the host object and the library-owned workspace (not the arenas).  The caller
  * must have synchronised every stream that still uses the index. */
 int pk_index_free(pk_index *index);
+
+/*
+ * ---------------------------------------------------------------- key/value cache
+ *
+ * What a search finds is put before a model, which keeps the context that it has read as keys and values, a row of each
+ * for every token, layer and head.  These calls hold them for one layer of many agents' sequences in pages (as the lists' delta pages are held: a
+ * table for each sequence, tokens appended at its end), in 16 or 8 bits, and attend over them: over everything, or, as a search does
+ * with its lists, over the blocks that a cheap score of bounds promises the most of.
+ *
+ * A token's key (or value) of one head is a row of head_dim elements.  Storage of a row x:
+ *   PK_F16, PK_BF16  rounded once to nearest even
+ *   PK_I8            scale = max|x| * (1/127), codes rint(x * (127 / max|x|)); a row of zeros has scale 0
+ *   PK_F8            scale = max|x| * (1/448), codes x * (448 / max|x|) rounded to nearest even e4m3
+ * all in 32 bits, so that a row's stored value depends on the row alone.  The bounds of a page (and head) are for every channel the
+ * largest and the smallest stored value of the keys in it, as int8 codes hi = ceil(max * 127 / a - 2^-10),
+ * lo = floor(min * 127 / a + 2^-10) with a = the largest magnitude among them, and the scale a * (1/127).
+ *
+ * The arena belongs to the caller.  The handle owns a workspace of fixed size that pk_kv_create allocates (kept until
+ * pk_kv_free); no other call allocates, waits for the device or keeps counters on the host, so all of
+ * them may be captured into a graph and replayed with other contents of the batch's DEVICE arrays.  Calls on one handle come from one
+ * stream at a time; work on different handles may overlap.  Outputs are valid once the stream is synchronised.
+ *
+ * Inputs must be finite.  What lies in pages beyond a sequence's length may be anything.
+ */
+typedef struct pk_kv pk_kv;
+
+#define PK_KV_MAX_DIM 256    /* head_dim: a multiple of 8                              */
+#define PK_KV_MAX_SEQS 65535 /* sequences of one batch                                 */
+
+typedef struct {
+    int64_t n_pages;
+    int32_t n_heads;     /* key/value heads, 1 .. 1024                                 */
+    int32_t head_dim;    /* multiple of 8 in [8, PK_KV_MAX_DIM]                        */
+    int32_t page_tokens; /* 16, 32, 64 or 128: also the block of pk_kv_select          */
+    int32_t storage;     /* PK_F16, PK_BF16, PK_I8 or PK_F8                            */
+} pk_kv_config;
+
+/*
+ * One step of a batch of sequences.  Sequence s holds lens[s] tokens once the step is over; the last
+ * m = offsets[s + 1] - offsets[s] of them are its new ones, at positions lens[s] - m .. lens[s] - 1, and have the rows
+ * offsets[s] .. offsets[s + 1] - 1 of the call's arrays.  Position p lies in page tables[s][p / page_tokens]; an entry outside
+ * [0, n_pages) is a page that the sequence has not (or no longer): nothing is written to it, read from it (zeros) or
+ * attended to.  Sequences may share pages that neither appends to in this call.
+ * The HOST numbers bound what the DEVICE arrays hold: whatever is beyond them is left out.
+ */
+typedef struct {
+    const int32_t *tables;  /* DEVICE [n_seqs] rows of n_cols entries                  */
+    const int32_t *offsets; /* DEVICE [n_seqs + 1], offsets[0] = 0, non-decreasing     */
+    const int32_t *lens;    /* DEVICE [n_seqs]                                         */
+    int64_t table_stride;   /* entries from one row of the tables to the next          */
+    int32_t n_seqs, n_cols;
+    int32_t n_tokens;       /* new tokens of all sequences                             */
+    int32_t max_new;        /* most new tokens of a sequence                           */
+    int32_t max_len;        /* most tokens of a sequence                               */
+} pk_kv_batch;
+
+/* Rows [n_tokens][heads][head_dim] of the caller's: DEVICE, elements of a row side by side, aligned to an element. */
+typedef struct {
+    const void *data;
+    int64_t token_stride, head_stride; /* in elements                                  */
+    int32_t dtype;                     /* PK_F32, PK_F16 or PK_BF16                    */
+} pk_rows;
+
+/* Bytes of arena that a cache needs; 0 for an invalid config. */
+size_t pk_kv_arena_bytes(const pk_kv_config *cfg);
+
+/* arena: DEVICE, 256-byte aligned, caller-owned, must stay allocated until pk_kv_free; its contents do not matter. */
+int pk_kv_create(const pk_kv_config *cfg, void *arena, size_t arena_bytes, pk_kv **out);
+
+/* The caller must have synchronised every stream that still uses the cache. */
+int pk_kv_free(pk_kv *kv);
+
+/* Writes the new tokens' keys and values into their pages and renews those pages' bounds.  k and v have one type, each of the three
+ * whatever the storage.  Asynchronous. */
+int pk_kv_append(pk_kv *kv, const pk_kv_batch *batch, const pk_rows *k, const pk_rows *v, void *stream);
+
+/* The stored values of the batch's new tokens (any tokens at the ends of its sequences), as dtype: code times scale, rounded once.
+ *   k_out, v_out  DEVICE [n_tokens][n_heads][head_dim], 16-byte aligned.  Asynchronous. */
+int pk_kv_read(pk_kv *kv, const pk_kv_batch *batch, void *k_out, void *v_out, int32_t dtype, void *stream);
+
+/* The bounds of pages: hi, lo DEVICE [n][n_heads][head_dim] float32 (codes times scale); zeros for a page number outside the cache.
+ *   pages  DEVICE [n] int32.  Asynchronous. */
+int pk_kv_bounds(pk_kv *kv, const int32_t *pages, int64_t n, float *hi, float *lo, void *stream);
+
+/*
+ * Attention of the new tokens over their sequences, their own keys (appended before) included: the query of position p sees the
+ * keys of positions j <= p (window > 0: and j > p - window), and
+ *   out = sum_j w_j v_j / sum_j w_j,  w_j = exp(scale q.k_j),  lse = log sum_j w_j
+ * A query that sees no key has zeros, and -inf.  Query head i reads key/value head i / (n_q_heads / n_heads).
+ * Sums, maxima and lse are held in 32 bits; the weights are rounded to 16 for the product with the values.
+ *   q    PK_F16 or PK_BF16; the storage's own type where that is one of the two (else PK_ERR_UNSUPPORTED)
+ *   out  DEVICE [n_tokens][n_q_heads][head_dim] of q's type, 16-byte aligned;  lse  DEVICE [n_tokens][n_q_heads] or NULL
+ * Equal calls give equal bits.  Asynchronous.
+ */
+int pk_kv_attend(pk_kv *kv, const pk_kv_batch *batch, const pk_rows *q, int32_t n_q_heads, float scale, int32_t window, void *out,
+                 float *lse, void *stream);
+
+/*
+ * The blocks (pages) that each new token attends to, one choice for each key/value head: the first `sink` blocks, the last
+ * `local` ones up to its own, and of those between the ones with the best scores, n_blocks in all (all that there are, if fewer).
+ *   q in int8 by head (code and scale as PK_I8 storage);  U = sum_c max(q_c hi_c, q_c lo_c) over the codes, a whole number
+ *   score of a block = (largest U * scale_q among the head's queries) * scale of the bounds
+ * Ties go to the lower block.  No sum in it is rounded: the choice depends on nothing but the inputs.
+ *   sink >= 0, local >= 1, sink + local <= n_blocks
+ *   out_blocks  DEVICE [n_tokens][n_heads][n_blocks] int32: block numbers (position / page_tokens), ascending, then -1
+ * PK_ERR_UNSUPPORTED where a sequence may have more than 32768 blocks.  Asynchronous.
+ */
+int pk_kv_select(pk_kv *kv, const pk_kv_batch *batch, const pk_rows *q, int32_t n_q_heads, int32_t n_blocks, int32_t sink, int32_t local,
+                 int32_t *out_blocks, void *stream);
+
+/*
+ * As pk_kv_attend without a window, over the keys of listed blocks alone.
+ *   blocks  DEVICE [n_tokens][n_heads][n_blocks] int32, in any order, no block twice in a row; numbers that the sequence
+ *           has no block for (-1 among them) are left out
+ */
+int pk_kv_attend_blocks(pk_kv *kv, const pk_kv_batch *batch, const pk_rows *q, int32_t n_q_heads, float scale, const int32_t *blocks,
+                        int32_t n_blocks, void *out, float *lse, void *stream);
 
 const char *pk_strerror(int status);
 

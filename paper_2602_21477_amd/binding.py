@@ -16,7 +16,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libpancake.so")
 
 PK_METRIC_IP, PK_METRIC_L2 = 0, 1
-PK_F32, PK_F16 = 0, 1
+PK_F32, PK_F16, PK_BF16, PK_I8, PK_F8 = 0, 1, 2, 3, 4
 PK_OK = 0
 PK_ERR_INVALID_ARG, PK_ERR_BAD_HANDLE, PK_ERR_DIM_MISMATCH, PK_ERR_NOMEM, PK_ERR_HIP, PK_ERR_UNSUPPORTED = (
     -1, -2, -3, -4, -5, -6)
@@ -25,7 +25,8 @@ PK_NOALLOC_WORKSPACE_BYTES = 64 << 20
 
 EXPORTS = ["pk_workspace_reserve", "pk_index_set_emit_cap", "pk_index_set_tile_cap", "pk_index_set_values_cap", "pk_search_noalloc", "pk_search_noalloc_bytes", "pk_search_levels", "pk_search_union", "pk_insert_multi", "pk_delete", "pk_index_split", "pk_index_centroids", "pk_list_ids", "pk_arena_bytes", "pk_index_build", "pk_index_add_arena", "pk_index_compact", "pk_kmeans", "pk_insert", "pk_insert_assigned", "pk_search",
            "pk_search_multi", "pk_coarse", "pk_scan_probes", "pk_index_stats", "pk_list_lengths", "pk_profile_begin",
-           "pk_profile_end", "pk_index_free", "pk_strerror"]
+           "pk_profile_end", "pk_index_free", "pk_kv_arena_bytes", "pk_kv_create", "pk_kv_free", "pk_kv_append", "pk_kv_read",
+           "pk_kv_bounds", "pk_kv_attend", "pk_kv_select", "pk_kv_attend_blocks", "pk_strerror"]
 
 
 class pk_config(C.Structure):
@@ -45,6 +46,19 @@ class pk_profile(C.Structure):
                 ("scan_ms", C.c_float), ("select_ms", C.c_float), ("scanned_rows", C.c_int64),
                 ("candidates", C.c_int64), ("tiles", C.c_int64), ("emitted", C.c_int64),
                 ("overflowed", C.c_int64), ("max_emitted", C.c_int64), ("scan_hot_ms", C.c_float)]
+
+
+class pk_kv_config(C.Structure):
+    _fields_ = [("n_pages", C.c_int64), ("n_heads", C.c_int32), ("head_dim", C.c_int32), ("page_tokens", C.c_int32), ("storage", C.c_int32)]
+
+
+class pk_kv_batch(C.Structure):
+    _fields_ = [("tables", C.c_void_p), ("offsets", C.c_void_p), ("lens", C.c_void_p), ("table_stride", C.c_int64), ("n_seqs", C.c_int32), ("n_cols", C.c_int32),
+                ("n_tokens", C.c_int32), ("max_new", C.c_int32), ("max_len", C.c_int32)]
+
+
+class pk_rows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64), ("dtype", C.c_int32)]
 
 
 class PancakeError(RuntimeError):
@@ -95,10 +109,20 @@ def lib():
         L.pk_profile_begin.argtypes = [vp, vp]
         L.pk_profile_end.argtypes = [vp, C.POINTER(pk_profile), vp]
         L.pk_index_free.argtypes = [vp]
+        L.pk_kv_arena_bytes.restype = C.c_size_t
+        L.pk_kv_arena_bytes.argtypes = [C.POINTER(pk_kv_config)]
+        L.pk_kv_create.argtypes = [C.POINTER(pk_kv_config), vp, C.c_size_t, C.POINTER(vp)]
+        L.pk_kv_free.argtypes = [vp]
+        L.pk_kv_append.argtypes = [vp, C.POINTER(pk_kv_batch), C.POINTER(pk_rows), C.POINTER(pk_rows), vp]
+        L.pk_kv_read.argtypes = [vp, C.POINTER(pk_kv_batch), vp, vp, i32, vp]
+        L.pk_kv_bounds.argtypes = [vp, vp, i64, vp, vp, vp]
+        L.pk_kv_attend.argtypes = [vp, C.POINTER(pk_kv_batch), C.POINTER(pk_rows), i32, C.c_float, i32, vp, vp, vp]
+        L.pk_kv_select.argtypes = [vp, C.POINTER(pk_kv_batch), C.POINTER(pk_rows), i32, i32, i32, i32, vp, vp]
+        L.pk_kv_attend_blocks.argtypes = [vp, C.POINTER(pk_kv_batch), C.POINTER(pk_rows), i32, C.c_float, vp, i32, vp, vp, vp]
         L.pk_strerror.restype = C.c_char_p
         L.pk_strerror.argtypes = [C.c_int]
         for name in EXPORTS:
-            if name not in ("pk_arena_bytes", "pk_strerror", "pk_search_noalloc_bytes"):
+            if name not in ("pk_arena_bytes", "pk_strerror", "pk_search_noalloc_bytes", "pk_kv_arena_bytes"):
                 getattr(L, name).restype = C.c_int
         _lib = L
     return _lib
@@ -423,3 +447,150 @@ def search_multi(indexes, q_offsets, queries, k, nprobe):
     dist = torch.empty((queries.shape[0], k), dtype=torch.float32, device=dev)
     pk_search_multi([ix.handle for ix in indexes], q_offsets, queries, k, nprobe, ids, dist)
     return ids, dist
+
+
+# ------------------------------------------------------------------------------- key/value cache
+
+ROW_TYPES = {torch.float32: PK_F32, torch.float16: PK_F16, torch.bfloat16: PK_BF16}
+
+
+def pk_kv_arena_bytes(cfg: pk_kv_config) -> int:
+    return int(lib().pk_kv_arena_bytes(C.byref(cfg)))
+
+
+def pk_kv_create(cfg: pk_kv_config, arena) -> int:
+    """Returns the handle (an integer).  `arena` is a uint8 CUDA tensor the caller keeps alive."""
+    h = C.c_void_p()
+    _check(lib().pk_kv_create(C.byref(cfg), _dev(arena, torch.uint8, "arena"), arena.numel(), C.byref(h)), "pk_kv_create")
+    return h.value
+
+
+def pk_kv_free(handle: int):
+    _check(lib().pk_kv_free(handle), "pk_kv_free")
+
+
+def _rows(t, what) -> pk_rows:
+    """Rows [token, head, channel] of any strides, the channels side by side."""
+    kind = ROW_TYPES.get(t.dtype)
+    if kind is None or not t.is_cuda or t.dim() != 3 or (t.stride(2) != 1 and t.shape[2] > 1):
+        raise ValueError(f"{what}: need a CUDA tensor [token, head, channel] of float32, float16 or bfloat16 with its channels side by side")
+    return pk_rows(t.data_ptr(), t.stride(0), t.stride(1), kind)
+
+
+def pk_kv_append(handle: int, batch: pk_kv_batch, k, v):
+    _check(lib().pk_kv_append(handle, batch, _rows(k, "k"), _rows(v, "v"), _stream()), "pk_kv_append")
+
+
+def pk_kv_read(handle: int, batch: pk_kv_batch, k_out, v_out):
+    kind = ROW_TYPES.get(k_out.dtype)
+    if kind is None:
+        raise ValueError("k_out: need float32, float16 or bfloat16")
+    _check(lib().pk_kv_read(handle, batch, _dev(k_out, k_out.dtype, "k_out"), _dev(v_out, k_out.dtype, "v_out"), kind, _stream()), "pk_kv_read")
+
+
+def pk_kv_bounds(handle: int, pages, hi, lo):
+    _check(lib().pk_kv_bounds(handle, _dev(pages, torch.int32, "pages"), pages.numel(), _dev(hi, torch.float32, "hi"), _dev(lo, torch.float32, "lo"),
+                              _stream()), "pk_kv_bounds")
+
+
+def pk_kv_attend(handle: int, batch: pk_kv_batch, q, scale: float, window: int, out, lse=None):
+    _check(lib().pk_kv_attend(handle, batch, _rows(q, "q"), q.shape[1], scale, window, _dev(out, q.dtype, "out"), _dev(lse, torch.float32, "lse"),
+                              _stream()), "pk_kv_attend")
+
+
+def pk_kv_select(handle: int, batch: pk_kv_batch, q, n_blocks: int, sink: int, local: int, out_blocks):
+    _check(lib().pk_kv_select(handle, batch, _rows(q, "q"), q.shape[1], n_blocks, sink, local, _dev(out_blocks, torch.int32, "out_blocks"), _stream()),
+           "pk_kv_select")
+
+
+def pk_kv_attend_blocks(handle: int, batch: pk_kv_batch, q, scale: float, blocks, out, lse=None):
+    _check(lib().pk_kv_attend_blocks(handle, batch, _rows(q, "q"), q.shape[1], scale, _dev(blocks, torch.int32, "blocks"), blocks.shape[2],
+                                     _dev(out, q.dtype, "out"), _dev(lse, torch.float32, "lse"), _stream()), "pk_kv_attend_blocks")
+
+
+class KVBatch:
+    """One step of a batch of sequences: page tables, row offsets and lengths on the GPU (int32; tensors that are kept and may
+    change from step to step), and their bounds on the host."""
+
+    def __init__(self, tables, offsets, lens, n_tokens, max_new, max_len):
+        n = lens.shape[0]
+        if tables.dim() != 2 or tables.shape[0] != n or offsets.shape != (n + 1,) or lens.dim() != 1:
+            raise ValueError("a batch has tables [sequence, page], offsets [sequence + 1] and lens [sequence]")
+        if not tables.is_cuda or tables.dtype != torch.int32 or (tables.shape[1] > 1 and tables.stride(1) != 1):
+            raise ValueError("tables: need an int32 CUDA tensor with its rows' entries side by side")
+        self.tables, self.offsets, self.lens, self.n_tokens = tables, offsets, lens, n_tokens
+        self.c = pk_kv_batch(tables.data_ptr(), _dev(offsets, torch.int32, "offsets"), _dev(lens, torch.int32, "lens"),
+                             tables.stride(0) if n > 1 else max(tables.stride(0), tables.shape[1]), n, tables.shape[1], n_tokens, max_new, max_len)
+
+
+class KVCache:
+    """Convenience owner of one cache's handle and its arena tensor (no arithmetic here)."""
+
+    def __init__(self, n_pages, n_heads, head_dim, storage=PK_BF16, page_tokens=64, device="cuda"):
+        self.cfg = pk_kv_config(n_pages, n_heads, head_dim, page_tokens, storage)
+        self.handle = None
+        need = pk_kv_arena_bytes(self.cfg)
+        if need == 0:
+            raise PancakeError(PK_ERR_INVALID_ARG, "pk_kv_arena_bytes")
+        self.arena = torch.empty(need, dtype=torch.uint8, device=device)
+        self.n_heads, self.head_dim = n_heads, head_dim
+        with torch.cuda.device(self.arena.device):
+            self.handle = pk_kv_create(self.cfg, self.arena)
+
+    def _shape(self, t, batch, heads, what):
+        if t.dim() != 3 or t.shape[0] != batch.n_tokens or t.shape[2] != self.head_dim or (heads and t.shape[1] != heads):
+            raise ValueError(f"{what}: need [{batch.n_tokens}, {heads or 'heads'}, {self.head_dim}], got {list(t.shape)}")
+        if t.device != self.arena.device:
+            raise ValueError(f"{what}: is on {t.device}, the cache on {self.arena.device}")
+
+    def append(self, k, v, batch):
+        self._shape(k, batch, self.n_heads, "k")
+        self._shape(v, batch, self.n_heads, "v")
+        pk_kv_append(self.handle, batch.c, k, v)
+
+    def read(self, batch, dtype):
+        k, v = (torch.empty((batch.n_tokens, self.n_heads, self.head_dim), dtype=dtype, device=self.arena.device) for _ in range(2))
+        pk_kv_read(self.handle, batch.c, k, v)
+        return k, v
+
+    def bounds(self, pages):
+        hi, lo = (torch.empty((pages.numel(), self.n_heads, self.head_dim), dtype=torch.float32, device=self.arena.device) for _ in range(2))
+        pk_kv_bounds(self.handle, pages, hi, lo)
+        return hi, lo
+
+    def _outputs(self, q, want_lse):
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        return out, torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if want_lse else None
+
+    def attend(self, q, batch, scale, window=0, want_lse=False):
+        self._shape(q, batch, 0, "q")
+        out, lse = self._outputs(q, want_lse)
+        pk_kv_attend(self.handle, batch.c, q, scale, window, out, lse)
+        return (out, lse) if want_lse else out
+
+    def select(self, q, batch, n_blocks, sink=1, local=2):
+        self._shape(q, batch, 0, "q")
+        blocks = torch.empty((batch.n_tokens, self.n_heads, n_blocks), dtype=torch.int32, device=q.device)
+        pk_kv_select(self.handle, batch.c, q, n_blocks, sink, local, blocks)
+        return blocks
+
+    def attend_blocks(self, q, blocks, batch, scale, want_lse=False):
+        self._shape(q, batch, 0, "q")
+        if blocks.dim() != 3 or blocks.shape[0] != batch.n_tokens or blocks.shape[1] != self.n_heads:
+            raise ValueError(f"blocks: need [{batch.n_tokens}, {self.n_heads}, blocks], got {list(blocks.shape)}")
+        out, lse = self._outputs(q, want_lse)
+        pk_kv_attend_blocks(self.handle, batch.c, q, scale, blocks, out, lse)
+        return (out, lse) if want_lse else out
+
+    def close(self):
+        if self.handle:
+            torch.cuda.synchronize(self.arena.device)
+            pk_kv_free(self.handle)
+            self.handle = None
+            self.arena = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass

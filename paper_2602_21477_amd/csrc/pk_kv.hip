@@ -1,0 +1,590 @@
+// Paged key/value cache: writing tokens into their pages, reading them back, and the host side of all its calls.
+// See include/pancake.h for the contract and pk_kv.h for the layout.
+#include <algorithm>
+#include <cmath>
+#include <new>
+
+#include "pk_kv.h"
+
+namespace pk {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kRowLanes = 16; // lanes that share a row: a quarter of a wave
+constexpr int kRowsAtOnce = kThreads / kRowLanes;
+
+// largest of 16 neighbouring lanes, in all of them
+__device__ __forceinline__ float quarter_max(float x)
+{
+#pragma unroll
+    for (int d = 1; d < kRowLanes; d *= 2) x = fmaxf(x, __shfl_xor(x, d));
+    return x;
+}
+
+// E consecutive elements of a caller's row, zeros past its D.
+template <int T, int E>
+__device__ __forceinline__ void load_row(float (&x)[E], const char *row, int at, int D)
+{
+    if constexpr (E >= 8) {
+#pragma unroll
+        for (int j = 0; j < E; j += 8) {
+            float y[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] = 0.f;
+            if (at + j < D) load_eight<T>(y, row, at + j);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[j + i] = y[i];
+        }
+    } else {
+        static_assert(E == 4, "");
+        float y[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = 0.f;
+        const int half = at & 4;
+        if (at < D) load_eight<T>(y, row, at - half);
+#pragma unroll
+        for (int i = 0; i < E; ++i) x[i] = half ? y[i + 4] : y[i];
+    }
+}
+
+// One workgroup: one page that the batch touches, one head.  A row is read by 16 lanes, its largest magnitude found by four
+// exchanges, its codes written as they come; values go through LDS, as their page is held by channels.  The bounds of the page's
+// keys are made of the rows that the cache holds once the call is over: those of this call from registers, older ones
+// read back.  They depend on the rows alone, not on the calls that brought them.
+template <int S, int T, int DP>
+__global__ __launch_bounds__(kThreads) void kv_append_kernel(KvDev c, KvBatch b, KvRows kin, KvRows vin)
+{
+    constexpr int ES = KvBytes<S>::v;
+    constexpr int E = DP / kRowLanes; // elements of a lane
+    __shared__ __align__(16) char vt[DP * kKvMaxPage * ES];
+    __shared__ float red[4][2][DP];
+    const int s = blockIdx.z, h = blockIdx.y, tid = threadIdx.x;
+    const KvSeq q = kv_seq(b, s, c.P);
+    const int begin = max(q.len - q.m, 0);
+    const int lp = (begin >> c.logP) + (int)blockIdx.x;
+    if (q.m == 0 || ((long long)lp << c.logP) >= q.len) return;
+    const uint32_t page = (uint32_t)b.tables[(size_t)s * b.table_stride + lp];
+    if (page >= c.n_pages) return;
+    const int base = lp << c.logP;
+    const int p0 = max(begin - base, 0), p1 = min(q.len - base, c.P); // rows of this call in the page
+    const size_t ph = (size_t)page * c.H + h;
+    char *kp = c.k + ph * c.P * DP * ES;
+    char *vp = c.v + ph * DP * c.P * ES;
+    const int sub = tid & (kRowLanes - 1), at = sub * E;
+    const int pitch = c.P * ES;
+
+    float hi[E], lo[E];
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+        hi[i] = -INFINITY;
+        lo[i] = INFINITY;
+    }
+    for (int r0 = 0; r0 < p1; r0 += kRowsAtOnce) {
+        const int r = r0 + tid / kRowLanes;
+        const bool in = r < p1, fresh = in && r >= p0;
+        float x[E];
+        float scale = 1.f;
+        char codes[E * ES];
+        if (fresh) {
+            const int t = q.first + (base + r - (q.len - q.m));
+            load_row<T, E>(x, kin.data + ((size_t)t * kin.token_stride + (size_t)h * kin.head_stride) * (T == PK_F32 ? 4 : 2), at, c.D);
+            if constexpr (kv_coded<S>) {
+                float most = 0.f;
+#pragma unroll
+                for (int i = 0; i < E; ++i) most = fmaxf(most, fabsf(x[i]));
+                most = quarter_max(most);
+                const float up = code_factor(most, kv_largest<S>);
+                scale = most * (1.f / kv_largest<S>);
+#pragma unroll
+                for (int i = 0; i < E; ++i) codes[i] = (char)to_code<S>(x[i], up);
+                if (sub == 0) c.ks[ph * c.P + r] = scale;
+            } else {
+#pragma unroll
+                for (int i = 0; i < E; i += 2) {
+                    const uint32_t w = pack16<S>(x[i], x[i + 1]);
+                    __builtin_memcpy(codes + 2 * i, &w, 4);
+                }
+            }
+            __builtin_memcpy(kp + ((size_t)r * DP + at) * ES, codes, E * ES);
+            float y[E];
+            load_row<T, E>(y, vin.data + ((size_t)t * vin.token_stride + (size_t)h * vin.head_stride) * (T == PK_F32 ? 4 : 2), at, c.D);
+            if constexpr (kv_coded<S>) {
+                float most = 0.f;
+#pragma unroll
+                for (int i = 0; i < E; ++i) most = fmaxf(most, fabsf(y[i]));
+                most = quarter_max(most);
+                const float up = code_factor(most, kv_largest<S>);
+                if (sub == 0) c.vs[ph * c.P + r] = most * (1.f / kv_largest<S>);
+#pragma unroll
+                for (int i = 0; i < E; ++i) vt[(at + i) * pitch + r] = (char)to_code<S>(y[i], up);
+            } else {
+#pragma unroll
+                for (int i = 0; i < E; i += 2) {
+                    const uint32_t w = pack16<S>(y[i], y[i + 1]);
+                    reinterpret_cast<uint16_t *>(vt + (at + i) * pitch)[r] = (uint16_t)w;
+                    reinterpret_cast<uint16_t *>(vt + (at + i + 1) * pitch)[r] = (uint16_t)(w >> 16);
+                }
+            }
+        } else if (in) {
+            __builtin_memcpy(codes, kp + ((size_t)r * DP + at) * ES, E * ES);
+            if constexpr (kv_coded<S>) scale = c.ks[ph * c.P + r];
+        }
+        if (in) {
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                float z;
+                if constexpr (kv_coded<S>) z = code_value<S>((uint8_t)codes[i]) * scale;
+                else {
+                    uint16_t w;
+                    __builtin_memcpy(&w, codes + 2 * i, 2);
+                    if constexpr (S == PK_BF16) z = __uint_as_float((uint32_t)w << 16);
+                    else z = (float)__builtin_bit_cast(_Float16, w);
+                }
+                hi[i] = fmaxf(hi[i], z);
+                lo[i] = fminf(lo[i], z);
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+        hi[i] = fmaxf(hi[i], __shfl_xor(hi[i], 16));
+        lo[i] = fminf(lo[i], __shfl_xor(lo[i], 16));
+        hi[i] = fmaxf(hi[i], __shfl_xor(hi[i], 32));
+        lo[i] = fminf(lo[i], __shfl_xor(lo[i], 32));
+        if ((tid & 63) < kRowLanes) {
+            red[tid >> 6][0][at + i] = hi[i];
+            red[tid >> 6][1][at + i] = lo[i];
+        }
+    }
+    __syncthreads();
+    if (tid < kRowLanes) {
+        float most = 0.f;
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+#pragma unroll
+            for (int w = 1; w < 4; ++w) {
+                hi[i] = fmaxf(hi[i], red[w][0][at + i]);
+                lo[i] = fminf(lo[i], red[w][1][at + i]);
+            }
+            most = fmaxf(most, fmaxf(fabsf(hi[i]), fabsf(lo[i])));
+        }
+        most = quarter_max(most);
+        const float up = code_factor(most, 127.f);
+        constexpr float kSlack = 1.f / 1024.f; // of a step: a bound this little beyond a whole number is that number
+        int8_t *bc = c.bc + ph * 2 * DP;
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+            bc[at + i] = (int8_t)fminf(fmaxf(ceilf(__fsub_rn(__fmul_rn(hi[i], up), kSlack)), -127.f), 127.f);
+            bc[DP + at + i] = (int8_t)fminf(fmaxf(floorf(__fadd_rn(__fmul_rn(lo[i], up), kSlack)), -127.f), 127.f);
+        }
+        if (tid == 0) c.bs[ph] = most * (1.f / 127.f);
+    }
+    // the values' page by channels: 16 bytes a thread where all of them are new, else one by one
+    constexpr int N = 16 / ES;
+    const int pieces = c.P / N;
+    for (int i = tid; i < DP * pieces; i += kThreads) {
+        const int d = i / pieces, r = (i - d * pieces) * N;
+        if (d >= c.D || r + N <= p0 || r >= p1) continue;
+        if (r >= p0 && r + N <= p1) {
+            *reinterpret_cast<u32x4 *>(vp + (size_t)d * pitch + r * ES) = *reinterpret_cast<const u32x4 *>(vt + d * pitch + r * ES);
+        } else {
+            for (int j = max(r, p0); j < min(r + N, p1); ++j) {
+                if constexpr (ES == 1) vp[(size_t)d * pitch + j] = vt[d * pitch + j];
+                else reinterpret_cast<uint16_t *>(vp + (size_t)d * pitch)[j] = reinterpret_cast<const uint16_t *>(vt + d * pitch)[j];
+            }
+        }
+    }
+}
+
+// One workgroup: one page of the batch's tokens, one head.  Keys are rows already; values are turned in LDS.
+template <int S, int T, int DP>
+__global__ __launch_bounds__(kThreads) void kv_read_kernel(KvDev c, KvBatch b, char *kout, char *vout)
+{
+    constexpr int ES = KvBytes<S>::v, TS = T == PK_F32 ? 4 : 2;
+    __shared__ __align__(16) char vt[DP * (kKvMaxPage * ES + 4)];
+    const int s = blockIdx.z, h = blockIdx.y, tid = threadIdx.x;
+    const KvSeq q = kv_seq(b, s, c.P);
+    const int begin = max(q.len - q.m, 0);
+    const int lp = (begin >> c.logP) + (int)blockIdx.x;
+    if (q.m == 0 || ((long long)lp << c.logP) >= q.len) return;
+    const uint32_t page = (uint32_t)b.tables[(size_t)s * b.table_stride + lp];
+    const int base = lp << c.logP;
+    const int p0 = max(begin - base, 0), p1 = min(q.len - base, c.P);
+    const bool there = page < c.n_pages;
+    const size_t ph = (size_t)(there ? page : 0) * c.H + h;
+    const char *kp = c.k + ph * c.P * DP * ES;
+    const char *vp = c.v + ph * DP * c.P * ES;
+    const int vpitch = c.P * ES + 4;
+    for (int i = tid; i < c.D * (c.P * ES / 4); i += kThreads) {
+        const int d = i / (c.P * ES / 4), w = i - d * (c.P * ES / 4);
+        reinterpret_cast<uint32_t *>(vt + d * vpitch)[w] = reinterpret_cast<const uint32_t *>(vp + (size_t)d * c.P * ES)[w];
+    }
+    __syncthreads();
+    auto element = [&](const char *at) {
+        if constexpr (kv_coded<S>) return code_value<S>((uint8_t)*at);
+        else if constexpr (S == PK_BF16) return __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t *>(at) << 16);
+        else return (float)*reinterpret_cast<const _Float16 *>(at);
+    };
+    const int pairs = c.D / 2;
+    for (int i = tid; i < (p1 - p0) * pairs; i += kThreads) {
+        const int r = p0 + i / pairs, d = (i % pairs) * 2;
+        float ks = 1.f, vs = 1.f;
+        if constexpr (kv_coded<S>) {
+            ks = c.ks[ph * c.P + r];
+            vs = c.vs[ph * c.P + r];
+        }
+        const size_t t = (size_t)(q.first + (base + r - (q.len - q.m)));
+        const size_t o = ((t * c.H + h) * c.D + d) * TS;
+        float k0 = element(kp + ((size_t)r * DP + d) * ES) * ks, k1 = element(kp + ((size_t)r * DP + d + 1) * ES) * ks;
+        float v0 = element(vt + d * vpitch + r * ES) * vs, v1 = element(vt + (d + 1) * vpitch + r * ES) * vs;
+        if (!there) k0 = k1 = v0 = v1 = 0.f;
+        if constexpr (T == PK_F32) {
+            *reinterpret_cast<f32x2 *>(kout + o) = f32x2{k0, k1};
+            *reinterpret_cast<f32x2 *>(vout + o) = f32x2{v0, v1};
+        } else {
+            *reinterpret_cast<uint32_t *>(kout + o) = pack16<T>(k0, k1);
+            *reinterpret_cast<uint32_t *>(vout + o) = pack16<T>(v0, v1);
+        }
+    }
+}
+
+__global__ __launch_bounds__(kThreads) void kv_bounds_kernel(KvDev c, int dp, const int32_t *pages, float *hi, float *lo)
+{
+    const size_t n = blockIdx.x;
+    const uint32_t page = (uint32_t)pages[n];
+    const bool there = page < c.n_pages;
+    for (int i = threadIdx.x; i < c.H * c.D; i += kThreads) {
+        const int h = i / c.D, d = i - h * c.D;
+        const size_t ph = (size_t)(there ? page : 0) * c.H + h;
+        const float s = there ? c.bs[ph] : 0.f;
+        hi[n * c.H * c.D + i] = there ? (float)c.bc[ph * 2 * dp + d] * s : 0.f;
+        lo[n * c.H * c.D + i] = there ? (float)c.bc[(ph * 2 + 1) * dp + d] * s : 0.f;
+    }
+}
+
+// pages that one sequence's new tokens can touch
+int touched(const KvDev &c, const KvBatch &b)
+{
+    return std::min((b.max_new + c.P - 2) / c.P + 1, b.cols);
+}
+
+template <int S, int T>
+hipError_t append_dp(const KvDev &c, int dp, const KvBatch &b, const KvRows &k, const KvRows &v, hipStream_t s)
+{
+    const dim3 grid(touched(c, b), c.H, b.n_seqs);
+    if (dp == 64) kv_append_kernel<S, T, 64><<<grid, kThreads, 0, s>>>(c, b, k, v);
+    else if (dp == 128) kv_append_kernel<S, T, 128><<<grid, kThreads, 0, s>>>(c, b, k, v);
+    else kv_append_kernel<S, T, 256><<<grid, kThreads, 0, s>>>(c, b, k, v);
+    return hipGetLastError();
+}
+
+template <int S>
+hipError_t append_s(const KvDev &c, int dp, const KvBatch &b, const KvRows &k, const KvRows &v, int dtype, hipStream_t s)
+{
+    if (dtype == PK_F32) return append_dp<S, PK_F32>(c, dp, b, k, v, s);
+    if (dtype == PK_F16) return append_dp<S, PK_F16>(c, dp, b, k, v, s);
+    return append_dp<S, PK_BF16>(c, dp, b, k, v, s);
+}
+
+template <int S, int T>
+hipError_t read_dp(const KvDev &c, int dp, const KvBatch &b, char *k, char *v, hipStream_t s)
+{
+    const dim3 grid(touched(c, b), c.H, b.n_seqs);
+    if (dp == 64) kv_read_kernel<S, T, 64><<<grid, kThreads, 0, s>>>(c, b, k, v);
+    else if (dp == 128) kv_read_kernel<S, T, 128><<<grid, kThreads, 0, s>>>(c, b, k, v);
+    else kv_read_kernel<S, T, 256><<<grid, kThreads, 0, s>>>(c, b, k, v);
+    return hipGetLastError();
+}
+
+template <int S>
+hipError_t read_s(const KvDev &c, int dp, const KvBatch &b, char *k, char *v, int dtype, hipStream_t s)
+{
+    if (dtype == PK_F32) return read_dp<S, PK_F32>(c, dp, b, k, v, s);
+    if (dtype == PK_F16) return read_dp<S, PK_F16>(c, dp, b, k, v, s);
+    return read_dp<S, PK_BF16>(c, dp, b, k, v, s);
+}
+
+} // namespace
+
+hipError_t launch_kv_append(const KvDev &c, int storage, int dp, const KvBatch &b, const KvRows &k, const KvRows &v, int dtype, hipStream_t s)
+{
+    switch (storage) {
+    case PK_I8: return append_s<PK_I8>(c, dp, b, k, v, dtype, s);
+    case PK_F8: return append_s<PK_F8>(c, dp, b, k, v, dtype, s);
+    case PK_F16: return append_s<PK_F16>(c, dp, b, k, v, dtype, s);
+    default: return append_s<PK_BF16>(c, dp, b, k, v, dtype, s);
+    }
+}
+
+hipError_t launch_kv_read(const KvDev &c, int storage, int dp, const KvBatch &b, void *k, void *v, int dtype, hipStream_t s)
+{
+    char *ko = static_cast<char *>(k), *vo = static_cast<char *>(v);
+    switch (storage) {
+    case PK_I8: return read_s<PK_I8>(c, dp, b, ko, vo, dtype, s);
+    case PK_F8: return read_s<PK_F8>(c, dp, b, ko, vo, dtype, s);
+    case PK_F16: return read_s<PK_F16>(c, dp, b, ko, vo, dtype, s);
+    default: return read_s<PK_BF16>(c, dp, b, ko, vo, dtype, s);
+    }
+}
+
+hipError_t launch_kv_bounds(const KvDev &c, int dp, const int32_t *pages, int64_t n, float *hi, float *lo, hipStream_t s)
+{
+    kv_bounds_kernel<<<dim3((unsigned)n), kThreads, 0, s>>>(c, dp, pages, hi, lo);
+    return hipGetLastError();
+}
+
+} // namespace pk
+
+// ------------------------------------------------------------------ host side
+
+using namespace pk;
+
+struct pk_kv {
+    uint64_t magic;
+    pk_kv_config cfg;
+    int dp;
+    KvDev dev;
+    int num_cu;
+    char *ws; // partial results of split attention
+};
+
+namespace {
+
+constexpr uint64_t kKvMagic = 0x70616e63616b7631ull;
+constexpr int64_t kMaxUnits = 1 << 22; // row tiles of a launch, all of a head: its grid has 32 bits for their threads
+constexpr int kMaxHeads = 1024; // key/value heads of a cache, and query heads of one of them
+
+size_t up256(size_t v) { return (v + 255) / 256 * 256; }
+
+int padded(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
+
+bool valid(const pk_kv_config *g)
+{
+    return g && g->n_pages >= 1 && g->n_pages <= 0x7fffffff && g->n_heads >= 1 && g->n_heads <= kMaxHeads && g->head_dim >= 8 &&
+           g->head_dim <= PK_KV_MAX_DIM && g->head_dim % 8 == 0 && g->page_tokens >= 16 && g->page_tokens <= kKvMaxPage &&
+           (g->page_tokens & (g->page_tokens - 1)) == 0 && g->storage >= PK_F16 && g->storage <= PK_F8;
+}
+
+// Regions of the arena; base may be null (sizes only).
+size_t lay_out(const pk_kv_config &g, char *base, KvDev *c)
+{
+    const int dp = padded(g.head_dim);
+    const size_t es = g.storage == PK_I8 || g.storage == PK_F8 ? 1 : 2, ph = (size_t)g.n_pages * g.n_heads;
+    size_t off = 0;
+    auto take = [&](size_t n) {
+        char *p = base ? base + off : nullptr;
+        off = up256(off + n);
+        return p;
+    };
+    c->k = take(ph * g.page_tokens * dp * es);
+    c->v = take(ph * g.page_tokens * dp * es);
+    const size_t scales = es == 1 ? ph * g.page_tokens * sizeof(float) : 0;
+    c->ks = reinterpret_cast<float *>(take(scales));
+    c->vs = reinterpret_cast<float *>(take(scales));
+    c->bc = reinterpret_cast<int8_t *>(take(ph * 2 * dp));
+    c->bs = reinterpret_cast<float *>(take(ph * sizeof(float)));
+    c->n_pages = (uint32_t)g.n_pages;
+    c->H = g.n_heads;
+    c->D = g.head_dim;
+    c->P = g.page_tokens;
+    c->logP = __builtin_ctz((unsigned)g.page_tokens);
+    return off;
+}
+
+bool live(const pk_kv *kv) { return kv && kv->magic == kKvMagic; }
+
+bool row_type(int32_t t) { return t == PK_F32 || t == PK_F16 || t == PK_BF16; }
+
+// The batch as the kernels get it.  *none: there is nothing to do.
+int take_batch(const pk_kv_batch *b, KvBatch *o, bool *none)
+{
+    if (!b || b->n_seqs < 0 || b->n_tokens < 0 || b->max_new < 0 || b->max_len < 0 || b->n_cols < 0) return PK_ERR_INVALID_ARG;
+    if (b->max_new > b->n_tokens) return PK_ERR_INVALID_ARG;
+    if (b->n_seqs > PK_KV_MAX_SEQS) return PK_ERR_UNSUPPORTED;
+    *none = b->n_seqs == 0 || b->n_tokens == 0 || b->max_new == 0;
+    if (*none) return b->n_tokens > 0 ? PK_ERR_INVALID_ARG : PK_OK; // tokens of no sequence
+    if (!b->tables || !b->offsets || !b->lens || b->n_cols < 1 || b->table_stride < b->n_cols || b->max_len < 1) return PK_ERR_INVALID_ARG;
+    *o = KvBatch{b->tables, b->offsets, b->lens, b->n_seqs, b->n_tokens, b->max_new, b->max_len, b->n_cols, b->table_stride};
+    return PK_OK;
+}
+
+int take_rows(const pk_rows *r, KvRows *o, int dim)
+{
+    if (!r || !r->data || !row_type(r->dtype) || r->token_stride < 0 || r->head_stride < 0) return PK_ERR_INVALID_ARG;
+    if (reinterpret_cast<uintptr_t>(r->data) % (r->dtype == PK_F32 ? 4 : 2)) return PK_ERR_INVALID_ARG;
+    *o = KvRows{static_cast<const char *>(r->data), r->token_stride, r->head_stride};
+    return PK_OK;
+}
+
+// Queries of a 16-bit type; a cache of a 16-bit storage takes its own type only.
+int take_queries(const pk_kv *kv, const pk_rows *q, int32_t n_q_heads, KvRows *o, int *group)
+{
+    const int rc = take_rows(q, o, kv->cfg.head_dim);
+    if (rc != PK_OK) return rc;
+    if (n_q_heads < 1 || n_q_heads % kv->cfg.n_heads) return PK_ERR_INVALID_ARG;
+    *group = n_q_heads / kv->cfg.n_heads;
+    if (*group > kMaxHeads || q->dtype == PK_F32) return PK_ERR_UNSUPPORTED;
+    if ((kv->cfg.storage == PK_F16 || kv->cfg.storage == PK_BF16) && q->dtype != kv->cfg.storage) return PK_ERR_UNSUPPORTED;
+    return PK_OK;
+}
+
+int attend(pk_kv *kv, const pk_kv_batch *batch, const pk_rows *q, int32_t n_q_heads, float scale, int32_t window, const int32_t *blocks,
+           int32_t n_blocks, void *out, float *lse, hipStream_t s)
+{
+    if (!live(kv)) return PK_ERR_BAD_HANDLE;
+    KvAttend a{};
+    bool none;
+    int rc = take_batch(batch, &a.b, &none);
+    if (rc != PK_OK) return rc;
+    if (window < 0 || !std::isfinite(scale)) return PK_ERR_INVALID_ARG;
+    if (none) return PK_OK;
+    rc = take_queries(kv, q, n_q_heads, &a.q, &a.G);
+    if (rc != PK_OK) return rc;
+    if (!out || reinterpret_cast<uintptr_t>(out) % 16) return PK_ERR_INVALID_ARG;
+    a.c = kv->dev;
+    a.scale = scale;
+    a.window = window;
+    a.blocks = blocks;
+    a.n_blocks = n_blocks;
+    a.out = static_cast<char *>(out);
+    a.lse = lse;
+    const int H = kv->cfg.n_heads;
+    // Row tiles of 16 queries that share their keys, and how many parts each one's keys are cut into: enough workgroups for the
+    // whole device, each of them with at least a tile for each of its four waves.
+    const int64_t rows = blocks ? a.G : (int64_t)a.b.max_new * a.G;
+    a.row_tiles = (int32_t)((rows + 15) / 16);
+    const int64_t items = (blocks ? (int64_t)a.b.n_tokens : (int64_t)a.b.n_seqs) * a.row_tiles * H;
+    if (items / H > kMaxUnits) return PK_ERR_UNSUPPORTED;
+    const int64_t keys = blocks ? (int64_t)n_blocks * kv->cfg.page_tokens : std::min<int64_t>(a.b.max_len, (int64_t)a.b.cols * kv->cfg.page_tokens);
+    const int64_t tiles = std::max<int64_t>((keys + kKvTile - 1) / kKvTile, 1);
+    const int64_t most = std::min<int64_t>(kKvMaxPartials / std::max<int64_t>(items, 1), (6 * kv->num_cu + items - 1) / items);
+    const int64_t want = std::max<int64_t>(std::min(most, tiles / 4), 1);
+    a.split_tiles = (int32_t)((tiles + want - 1) / want);
+    a.n_split = (int32_t)((tiles + a.split_tiles - 1) / a.split_tiles);
+    a.part_ml = reinterpret_cast<float *>(kv->ws);
+    a.part = a.part_ml + (size_t)kKvMaxPartials * 32;
+    return launch_kv_attend(a, kv->cfg.storage, kv->dp, q->dtype, s) == hipSuccess ? PK_OK : PK_ERR_HIP;
+}
+
+} // namespace
+
+extern "C" {
+
+size_t pk_kv_arena_bytes(const pk_kv_config *cfg)
+{
+    KvDev c;
+    return valid(cfg) ? lay_out(*cfg, nullptr, &c) : 0;
+}
+
+int pk_kv_create(const pk_kv_config *cfg, void *arena, size_t arena_bytes, pk_kv **out)
+{
+    if (!out) return PK_ERR_INVALID_ARG;
+    *out = nullptr;
+    if (!valid(cfg) || !arena || (reinterpret_cast<uintptr_t>(arena) & 255)) return PK_ERR_INVALID_ARG;
+    if (arena_bytes < pk_kv_arena_bytes(cfg)) return PK_ERR_NOMEM;
+    pk_kv *kv = new (std::nothrow) pk_kv();
+    if (!kv) return PK_ERR_NOMEM;
+    kv->cfg = *cfg;
+    kv->dp = padded(cfg->head_dim);
+    lay_out(*cfg, static_cast<char *>(arena), &kv->dev);
+    int device = 0;
+    if (hipGetDevice(&device) != hipSuccess || hipDeviceGetAttribute(&kv->num_cu, hipDeviceAttributeMultiprocessorCount, device) != hipSuccess) {
+        (void)hipGetLastError();
+        delete kv;
+        return PK_ERR_HIP;
+    }
+    void *p = nullptr;
+    if (hipMalloc(&p, (size_t)kKvMaxPartials * (32 + 16 * kv->dp) * sizeof(float)) != hipSuccess) {
+        (void)hipGetLastError();
+        delete kv;
+        return PK_ERR_NOMEM;
+    }
+    kv->ws = static_cast<char *>(p);
+    kv->magic = kKvMagic;
+    *out = kv;
+    return PK_OK;
+}
+
+int pk_kv_free(pk_kv *kv)
+{
+    if (!live(kv)) return PK_ERR_BAD_HANDLE;
+    kv->magic = 0;
+    const bool ok = hipFree(kv->ws) == hipSuccess;
+    delete kv;
+    return ok ? PK_OK : PK_ERR_HIP;
+}
+
+int pk_kv_append(pk_kv *kv, const pk_kv_batch *batch, const pk_rows *k, const pk_rows *v, void *stream)
+{
+    if (!live(kv)) return PK_ERR_BAD_HANDLE;
+    KvBatch b;
+    bool none;
+    int rc = take_batch(batch, &b, &none);
+    if (rc != PK_OK || none) return rc;
+    KvRows kr, vr;
+    rc = take_rows(k, &kr, kv->cfg.head_dim);
+    if (rc == PK_OK) rc = take_rows(v, &vr, kv->cfg.head_dim);
+    if (rc != PK_OK) return rc;
+    if (k->dtype != v->dtype) return PK_ERR_INVALID_ARG;
+    return launch_kv_append(kv->dev, kv->cfg.storage, kv->dp, b, kr, vr, k->dtype, static_cast<hipStream_t>(stream)) == hipSuccess ? PK_OK : PK_ERR_HIP;
+}
+
+int pk_kv_read(pk_kv *kv, const pk_kv_batch *batch, void *k_out, void *v_out, int32_t dtype, void *stream)
+{
+    if (!live(kv)) return PK_ERR_BAD_HANDLE;
+    KvBatch b;
+    bool none;
+    const int rc = take_batch(batch, &b, &none);
+    if (rc != PK_OK || none) return rc;
+    if (!k_out || !v_out || !row_type(dtype) || ((reinterpret_cast<uintptr_t>(k_out) | reinterpret_cast<uintptr_t>(v_out)) & 15)) return PK_ERR_INVALID_ARG;
+    return launch_kv_read(kv->dev, kv->cfg.storage, kv->dp, b, k_out, v_out, dtype, static_cast<hipStream_t>(stream)) == hipSuccess ? PK_OK : PK_ERR_HIP;
+}
+
+int pk_kv_bounds(pk_kv *kv, const int32_t *pages, int64_t n, float *hi, float *lo, void *stream)
+{
+    if (!live(kv)) return PK_ERR_BAD_HANDLE;
+    if (n < 0 || n > 0x7fffffff) return PK_ERR_INVALID_ARG;
+    if (n == 0) return PK_OK;
+    if (!pages || !hi || !lo) return PK_ERR_INVALID_ARG;
+    return launch_kv_bounds(kv->dev, kv->dp, pages, n, hi, lo, static_cast<hipStream_t>(stream)) == hipSuccess ? PK_OK : PK_ERR_HIP;
+}
+
+int pk_kv_attend(pk_kv *kv, const pk_kv_batch *batch, const pk_rows *q, int32_t n_q_heads, float scale, int32_t window, void *out, float *lse,
+                 void *stream)
+{
+    return attend(kv, batch, q, n_q_heads, scale, window, nullptr, 0, out, lse, static_cast<hipStream_t>(stream));
+}
+
+int pk_kv_attend_blocks(pk_kv *kv, const pk_kv_batch *batch, const pk_rows *q, int32_t n_q_heads, float scale, const int32_t *blocks,
+                        int32_t n_blocks, void *out, float *lse, void *stream)
+{
+    if (!live(kv)) return PK_ERR_BAD_HANDLE;
+    if (n_blocks < 1 || n_blocks > kKvMaxSelect) return PK_ERR_INVALID_ARG;
+    if (!blocks && batch && batch->n_tokens > 0) return PK_ERR_INVALID_ARG;
+    static const int32_t nothing = 0;
+    return attend(kv, batch, q, n_q_heads, scale, 0, blocks ? blocks : &nothing, n_blocks, out, lse, static_cast<hipStream_t>(stream));
+}
+
+int pk_kv_select(pk_kv *kv, const pk_kv_batch *batch, const pk_rows *q, int32_t n_q_heads, int32_t n_blocks, int32_t sink, int32_t local,
+                 int32_t *out_blocks, void *stream)
+{
+    if (!live(kv)) return PK_ERR_BAD_HANDLE;
+    KvBatch b;
+    bool none;
+    int rc = take_batch(batch, &b, &none);
+    if (rc != PK_OK) return rc;
+    if (n_blocks < 1 || sink < 0 || local < 1 || (int64_t)sink + local > n_blocks) return PK_ERR_INVALID_ARG;
+    if (n_blocks > kKvMaxSelect || (!none && (std::min<int64_t>(b.max_len, (int64_t)b.cols * kv->cfg.page_tokens) + kv->cfg.page_tokens - 1) / kv->cfg.page_tokens > kKvMaxSelect))
+        return PK_ERR_UNSUPPORTED;
+    if (none) return PK_OK;
+    KvRows qr;
+    int G;
+    rc = take_queries(kv, q, n_q_heads, &qr, &G);
+    if (rc != PK_OK) return rc;
+    if (!out_blocks) return PK_ERR_INVALID_ARG;
+    return launch_kv_select(kv->dev, kv->dp, b, qr, q->dtype, G, n_blocks, sink, local, out_blocks, static_cast<hipStream_t>(stream)) == hipSuccess
+               ? PK_OK
+               : PK_ERR_HIP;
+}
+
+} // extern "C"
