@@ -196,9 +196,12 @@ struct KvAttend {
     int32_t n_blocks;
     char *out;            // [n_tokens][H * G][D]
     float *lse;           // [n_tokens][H * G] or null
-    // split over the keys: partial results [row tile][H][n_split] of 16 rows
-    int32_t n_split, split_tiles, row_tiles; // row_tiles: of one sequence (sparse: of one token)
-    float *part, *part_ml;
+    float *part, *part_ml; // room for partial results of kKvMaxPartials times 16 rows
+    int32_t num_cu;
+    // set by the launch
+    int32_t few_rows;      // sequences with more rows of queries than this are taken by the kernel for many
+    int32_t row_tiles;     // of one sequence (sparse: of one token)
+    int32_t n_split, split_tiles; // parts that the keys are cut into, and tiles of 64 keys of each
 };
 
 hipError_t launch_kv_append(const KvDev &c, int storage, int dp, const KvBatch &b, const KvRows &k, const KvRows &v, int dtype, hipStream_t s);

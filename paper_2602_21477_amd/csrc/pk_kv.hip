@@ -351,7 +351,7 @@ struct pk_kv {
 namespace {
 
 constexpr uint64_t kKvMagic = 0x70616e63616b7631ull;
-constexpr int64_t kMaxUnits = 1 << 22; // row tiles of a launch, all of a head: its grid has 32 bits for their threads
+constexpr int64_t kMaxUnits = 1 << 22; // row tiles of a launch: its grid has 32 bits for their threads
 constexpr int kMaxHeads = 1024; // key/value heads of a cache, and query heads of one of them
 
 size_t up256(size_t v) { return (v + 255) / 256 * 256; }
@@ -448,19 +448,10 @@ int attend(pk_kv *kv, const pk_kv_batch *batch, const pk_rows *q, int32_t n_q_he
     a.n_blocks = n_blocks;
     a.out = static_cast<char *>(out);
     a.lse = lse;
-    const int H = kv->cfg.n_heads;
-    // Row tiles of 16 queries that share their keys, and how many parts each one's keys are cut into: enough workgroups for the
-    // whole device, each of them with at least a tile for each of its four waves.
-    const int64_t rows = blocks ? a.G : (int64_t)a.b.max_new * a.G;
-    a.row_tiles = (int32_t)((rows + 15) / 16);
-    const int64_t items = (blocks ? (int64_t)a.b.n_tokens : (int64_t)a.b.n_seqs) * a.row_tiles * H;
-    if (items / H > kMaxUnits) return PK_ERR_UNSUPPORTED;
-    const int64_t keys = blocks ? (int64_t)n_blocks * kv->cfg.page_tokens : std::min<int64_t>(a.b.max_len, (int64_t)a.b.cols * kv->cfg.page_tokens);
-    const int64_t tiles = std::max<int64_t>((keys + kKvTile - 1) / kKvTile, 1);
-    const int64_t most = std::min<int64_t>(kKvMaxPartials / std::max<int64_t>(items, 1), (6 * kv->num_cu + items - 1) / items);
-    const int64_t want = std::max<int64_t>(std::min(most, tiles / 4), 1);
-    a.split_tiles = (int32_t)((tiles + want - 1) / want);
-    a.n_split = (int32_t)((tiles + a.split_tiles - 1) / a.split_tiles);
+    a.num_cu = kv->num_cu;
+    // (more workgroups than a grid has threads for)
+    if ((blocks ? (int64_t)a.b.n_tokens : (int64_t)a.b.n_seqs) * (((blocks ? a.G : (int64_t)a.b.max_new * a.G) + 15) / 16) * kv->cfg.n_heads > kMaxUnits)
+        return PK_ERR_UNSUPPORTED;
     a.part_ml = reinterpret_cast<float *>(kv->ws);
     a.part = a.part_ml + (size_t)kKvMaxPartials * 32;
     return launch_kv_attend(a, kv->cfg.storage, kv->dp, q->dtype, s) == hipSuccess ? PK_OK : PK_ERR_HIP;
