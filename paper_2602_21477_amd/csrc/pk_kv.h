@@ -196,11 +196,15 @@ struct KvAttend {
     int32_t n_blocks;
     char *out;            // [n_tokens][H * G][D]
     float *lse;           // [n_tokens][H * G] or null
-    float *part, *part_ml; // room for partial results of kKvMaxPartials times 16 rows
+    float *part, *part_ml; // room for partial results: part_floats of O, and two floats for each row
+    int64_t part_floats;
+    uint32_t *arrivals;    // parts of a row tile that have ended, zeros between calls: kKvArrivals of them
     int32_t num_cu;
     // set by the launch
     int32_t few_rows;      // sequences with more rows of queries than this are taken by the kernel for many
     int32_t row_tiles;     // of one sequence (sparse: of one token)
+    int32_t part_row;      // floats of a row of partial results
+    int32_t join_here;     // the kernel for few rows joins its parts itself
     int32_t n_split, split_tiles; // parts that the keys are cut into, and tiles of 64 keys of each
 };
 
@@ -212,7 +216,8 @@ hipError_t launch_kv_select(const KvDev &c, int dp, const KvBatch &b, const KvRo
 hipError_t launch_kv_attend(const KvAttend &a, int storage, int dp, int dtype, hipStream_t s);
 
 constexpr int kKvTile = 64;          // keys of one step of the attention kernels
-constexpr int kKvMaxPartials = 4096; // partial results of 16 rows that a cache's workspace has room for
+constexpr int64_t kKvPartFloats = 16 << 20; // partial results that a cache's workspace has room for: 512 workgroups' of 256 rows of 128 channels
+constexpr int kKvArrivals = 4096;
 constexpr int kKvMaxPage = 128;
 constexpr int kKvMaxSelect = 32768;  // blocks that one query chooses from: their keys lie in LDS
 

@@ -452,8 +452,10 @@ int attend(pk_kv *kv, const pk_kv_batch *batch, const pk_rows *q, int32_t n_q_he
     // (more workgroups than a grid has threads for)
     if ((blocks ? (int64_t)a.b.n_tokens : (int64_t)a.b.n_seqs) * (((blocks ? a.G : (int64_t)a.b.max_new * a.G) + 15) / 16) * kv->cfg.n_heads > kMaxUnits)
         return PK_ERR_UNSUPPORTED;
-    a.part_ml = reinterpret_cast<float *>(kv->ws);
-    a.part = a.part_ml + (size_t)kKvMaxPartials * 32;
+    a.part = reinterpret_cast<float *>(kv->ws);
+    a.part_floats = kKvPartFloats;
+    a.part_ml = a.part + kKvPartFloats;
+    a.arrivals = reinterpret_cast<uint32_t *>(a.part_ml + kKvPartFloats / kv->dp * 2);
     return launch_kv_attend(a, kv->cfg.storage, kv->dp, q->dtype, s) == hipSuccess ? PK_OK : PK_ERR_HIP;
 }
 
@@ -485,12 +487,20 @@ int pk_kv_create(const pk_kv_config *cfg, void *arena, size_t arena_bytes, pk_kv
         return PK_ERR_HIP;
     }
     void *p = nullptr;
-    if (hipMalloc(&p, (size_t)kKvMaxPartials * (32 + 16 * kv->dp) * sizeof(float)) != hipSuccess) {
+    const size_t parts = (size_t)(kKvPartFloats + kKvPartFloats / kv->dp * 2) * sizeof(float);
+    if (hipMalloc(&p, parts + kKvArrivals * sizeof(uint32_t)) != hipSuccess) {
         (void)hipGetLastError();
         delete kv;
         return PK_ERR_NOMEM;
     }
     kv->ws = static_cast<char *>(p);
+    // (a blocking clear, done before any stream's work can reach it)
+    if (hipMemset(kv->ws + parts, 0, kKvArrivals * sizeof(uint32_t)) != hipSuccess || hipDeviceSynchronize() != hipSuccess) {
+        (void)hipGetLastError();
+        (void)hipFree(p);
+        delete kv;
+        return PK_ERR_HIP;
+    }
     kv->magic = kKvMagic;
     *out = kv;
     return PK_OK;

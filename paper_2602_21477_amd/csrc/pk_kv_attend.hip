@@ -49,6 +49,39 @@ __device__ __forceinline__ float over_quarters_sum(float x)
     return x + __shfl_xor(x, 32);
 }
 
+// The largest of three (without the rounds that fmaxf makes for signalling NaNs).
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+
+// A number that all lanes of a wave have.
+__device__ __forceinline__ int same(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// Where a wave's lane finds its part of a tile of 64 keys: a run of 16 tokens that lie in one page.
+struct KvRun {
+    int base;      // position of its first token; -1: there are none
+    uint32_t page; // a number of n_pages and more: the table has none there
+};
+
+// What a workgroup (or the last one of a split row tile) does with a row of its results: 16 threads a row, four channels each at a time.
+template <int T, int DP, typename F>
+__device__ __forceinline__ void kv_write_row(const KvAttend &a, int h, int tok, int member, int sub, float m, float l, F value)
+{
+    const size_t oh = (size_t)tok * a.c.H * a.G + h * a.G + member;
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+#pragma unroll
+    for (int d = 0; d < DP; d += 64) {
+        const int dd = d + sub * 4;
+        if (dd >= a.c.D) continue;
+        const f32x4 y = value(dd) * inv;
+        *reinterpret_cast<u32x2 *>(a.out + (oh * a.c.D + dd) * 2) = u32x2{pack16<T>(y[0], y[1]), pack16<T>(y[2], y[3])};
+    }
+    if (sub == 0 && a.lse) a.lse[oh] = l > 0.f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+}
+
 // Rows of 16 queries that share a key/value head (query heads of its group, several tokens' where the group is small) against
 // keys that four waves of a workgroup take in turns, 64 at a time, with no LDS until they join their results:
 //   S^T = K Q^T   rows are keys, columns queries; the products' operands come from memory as they lie there
@@ -58,7 +91,12 @@ __device__ __forceinline__ float over_quarters_sum(float x)
 // One pass with a running maximum and sum per query, in 32 bits.  Products are taken in the queries' type, which holds 8-bit codes
 // exactly; weights are rounded to it for the second one.  With codes a weight carries the value's scale.  In half precision that
 // is in units of the largest scale seen, and the largest weight is 2^kHalfTop, as that type has the more of its range below it; in bfloat16,
-// whose 8 bits are fewer than the codes are worth, a weight is the sum of two numbers, and its product two.  blockIdx: row tile of a sequence (sparse: of a token) and part of its keys, head.
+// whose 8 bits are fewer than the codes are worth, a weight is the sum of two numbers, and its product two.
+// Bound by memory: K of a wave's next tile is asked for when the products with this one's are done, V of a tile when its K is about to be
+// used, and the pages of both a round (their blocks, where they are listed, two rounds) earlier, so that a wave always has 8 or 16 KB on
+// its way.  Where the keys are cut into few parts, the workgroup that ends last joins them, in their order: no launch of its own.
+// blockIdx: row tile of a sequence (sparse: of a token), part of its keys, head; the heads fastest, so that each of the chip's eight
+// parts reads few of them.
 template <int S, int T, int DP, bool SPARSE>
 __global__ __launch_bounds__(256) void kv_rows_kernel(KvAttend a)
 {
@@ -69,16 +107,19 @@ __global__ __launch_bounds__(256) void kv_rows_kernel(KvAttend a)
     constexpr int KS = DP / 32;               // products over the channels
     constexpr int DT = DP / 16;               // tiles of 16 channels of the output
     constexpr int VC = CODED ? 1 : 2;         // loads of a lane for 16 tokens of a channel
-    __shared__ float join_o[4][16][DP + 4];
+    __shared__ __align__(16) float join_o[4][16][DP + 4];
     __shared__ float join_m[4][16], join_l[4][16];
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 15, g = lane >> 4;
-    const int unit = blockIdx.x / a.n_split, split = blockIdx.x - unit * a.n_split, h = blockIdx.y;
-    const KvDev &c = a.c;
+    __shared__ uint32_t arrived;
+    const int tid = threadIdx.x, wave = same(tid >> 6), lane = tid & 63, col = lane & 15, g = lane >> 4;
+    const KvDev c = a.c;
     const int P = c.P, G = a.G;
+    int at = blockIdx.x;
+    const int h = at % c.H;
+    at /= c.H;
+    const int split = at % a.n_split, unit = at / a.n_split;
 
     // the tile's queries
-    int seq, tile;
-    int token0 = 0;
+    int seq, tile, token0 = 0;
     if constexpr (SPARSE) {
         token0 = unit / a.row_tiles;
         tile = unit - token0 * a.row_tiles;
@@ -115,6 +156,43 @@ __global__ __launch_bounds__(256) void kv_rows_kernel(KvAttend a)
         t1 = min(last_pos < 0 ? 0 : last_pos / kKvTile + 1, (split + 1) * a.split_tiles);
     }
 
+    // ---- blocks, pages and K on their way
+    const int ksub = col >> 2; // the lane's run of K's rows; of V's tokens: g
+    auto block_of = [&](int t, int sub) __attribute__((always_inline)) -> int {
+        if constexpr (SPARSE) {
+            const int bi = min((t * kKvTile + sub * 16) >> c.logP, a.n_blocks - 1);
+            return list[bi];
+        } else return 0;
+    };
+    auto base_of = [&](int t, int sub, int block) __attribute__((always_inline)) -> int {
+        const int at = t * kKvTile + sub * 16;
+        if constexpr (SPARSE) {
+            const bool in = t < t1 && (at >> c.logP) < a.n_blocks && block >= 0 && block <= (sq.len - 1) >> c.logP;
+            return in ? (block << c.logP) + (at & (P - 1)) : -1;
+        } else return t < t1 && at < sq.len ? at : -1;
+    };
+    auto page_of = [&](int base) __attribute__((always_inline)) -> uint32_t { return base >= 0 ? (uint32_t)table[base >> c.logP] : c.n_pages; };
+    u32x4 kw[4][KC];
+    auto ask_k = [&](const KvRun &r) __attribute__((always_inline)) {
+        const size_t ph = (size_t)(r.page < c.n_pages ? r.page : 0) * c.H + h;
+        const char *kr = c.k + (ph * P + (r.base >= 0 ? r.base & (P - 1) : 0) + (col & 3)) * DP * ES + g * 16;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int k = 0; k < KC; ++k) kw[i][k] = *reinterpret_cast<const u32x4 *>(kr + i * 4 * DP * ES + k * 64);
+    };
+    const int tw = t0 + wave;
+    int kblock = 0, vblock = 0; // (sparse) of the round after the next
+    KvRun kr, vr, kr1, vr1;     // of this round and the next
+    {
+        const int kb0 = block_of(tw, ksub), vb0 = block_of(tw, g), kb1 = block_of(tw + 4, ksub), vb1 = block_of(tw + 4, g);
+        kblock = block_of(tw + 8, ksub), vblock = block_of(tw + 8, g);
+        kr.base = base_of(tw, ksub, kb0), vr.base = base_of(tw, g, vb0);
+        kr1.base = base_of(tw + 4, ksub, kb1), vr1.base = base_of(tw + 4, g, vb1);
+        kr.page = page_of(kr.base), vr.page = page_of(vr.base);
+        kr1.page = page_of(kr1.base), vr1.page = page_of(vr1.base);
+    }
+
     // queries, as the right operand
     u32x4 qf[KS];
     const float qscale = a.scale * kLog2e;
@@ -139,45 +217,30 @@ __global__ __launch_bounds__(256) void kv_rows_kernel(KvAttend a)
     for (int d = 0; d < DT; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
     float m = -INFINITY, l = 0.f, vunit = 1e-30f;
 
-    // position and page of the 16 tokens `sub` of tile t; a page that is not there has number n_pages at least
-    auto sub_base = [&](int t, int sub) -> int {
-        if constexpr (SPARSE) {
-            const int at = t * kKvTile + sub * 16, bi = at >> c.logP;
-            const int block = bi < a.n_blocks ? list[bi] : -1;
-            return block < 0 || block > (sq.len - 1) >> c.logP ? -1 : (block << c.logP) + (at & (P - 1));
-        } else {
-            const int base = t * kKvTile + sub * 16;
-            return base < sq.len ? base : -1;
-        }
-    };
-    for (int t = t0 + wave; t < t1; t += 4) {
-        const int kb = sub_base(t, col >> 2), vb = sub_base(t, g);
-        const uint32_t kpage = kb >= 0 ? kv_page(c, table, kb) : c.n_pages, vpage = vb >= 0 ? kv_page(c, table, vb) : c.n_pages;
-        const bool there = vpage < c.n_pages;
-        const size_t kph = (size_t)(kpage < c.n_pages ? kpage : 0) * c.H + h, vph = (size_t)(there ? vpage : 0) * c.H + h;
-        const int koff = kb >= 0 ? kb & (P - 1) : 0, voff = vb >= 0 ? vb & (P - 1) : 0;
-        const char *kr = c.k + (kph * P + koff + (col & 3)) * DP * ES + g * 16;
-        const char *vr = c.v + ((vph * DP + col) * P + voff) * ES;
-
-        u32x4 kw[4][KC];
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int k = 0; k < KC; ++k) kw[i][k] = *reinterpret_cast<const u32x4 *>(kr + i * 4 * DP * ES + k * 64);
+    if (tw < t1) ask_k(kr);
+    for (int t = tw; t < t1; t += 4) {
+        const bool there = vr.page < c.n_pages;
+        const int vb = vr.base;
         f32x4 ksc[4], vsc[4];
-        if constexpr (CODED) {
-            const float *ks = c.ks + vph * P + voff, *vs = c.vs + vph * P + voff;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                ksc[i] = *reinterpret_cast<const f32x4 *>(ks + 4 * i);
-                vsc[i] = *reinterpret_cast<const f32x4 *>(vs + 4 * i);
-            }
-        }
         u32x4 vw[DT][VC];
+        {
+            const size_t vph = (size_t)(there ? vr.page : 0) * c.H + h;
+            const int voff = vb >= 0 ? vb & (P - 1) : 0;
+            if constexpr (CODED) {
+                const float *ks = c.ks + vph * P + voff, *vs = c.vs + vph * P + voff;
 #pragma unroll
-        for (int d = 0; d < DT; ++d)
+                for (int i = 0; i < 4; ++i) {
+                    ksc[i] = *reinterpret_cast<const f32x4 *>(ks + 4 * i);
+                    vsc[i] = *reinterpret_cast<const f32x4 *>(vs + 4 * i);
+                }
+            }
+            const char *v = c.v + ((vph * DP + col) * P + voff) * ES;
 #pragma unroll
-            for (int k = 0; k < VC; ++k) vw[d][k] = *reinterpret_cast<const u32x4 *>(vr + (size_t)d * 16 * P * ES + k * 16);
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int k = 0; k < VC; ++k) vw[d][k] = *reinterpret_cast<const u32x4 *>(v + (size_t)d * 16 * P * ES + k * 16);
+        }
+        __builtin_amdgcn_sched_barrier(0);
 
         f32x4 x[4];
 #pragma unroll
@@ -194,11 +257,23 @@ __global__ __launch_bounds__(256) void kv_rows_kernel(KvAttend a)
                     x[i] = mma<HALF>(f0, qf[k], x[i]);
                 }
             }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        // the next round's K; the pages of the one after it
+        kr = kr1, vr = vr1;
+        ask_k(kr);
+        kr1.base = base_of(t + 8, ksub, kblock), vr1.base = base_of(t + 8, g, vblock);
+        kr1.page = page_of(kr1.base), vr1.page = page_of(vr1.base);
+        kblock = block_of(t + 12, ksub), vblock = block_of(t + 12, g);
+        __builtin_amdgcn_sched_barrier(0);
+
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
             if constexpr (CODED) x[i] *= ksc[i];
             x[i] *= qscale;
         }
         // keys that a query does not see; the values of tokens that no query sees are taken as zeros, whatever lies there
-        const int seen = min(there ? pos : -1, there ? sq.len - 1 : -1) - vb; // of the lane's 16 keys: 0 .. seen
+        const int seen = (there ? min(pos, sq.len - 1) : -1) - vb; // of the lane's 16 keys: 0 .. seen
         const int since = from - vb;
         if (__any(seen < 15 || since > 0 || vb < 0)) {
             const int held = there && vb >= 0 ? sq.len - vb : 0; // of its 16 tokens
@@ -226,7 +301,7 @@ __global__ __launch_bounds__(256) void kv_rows_kernel(KvAttend a)
         }
         float most = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) most = fmaxf(most, fmaxf(fmaxf(x[i][0], x[i][1]), fmaxf(x[i][2], x[i][3])));
+        for (int i = 0; i < 4; ++i) most = max3(most, max3(x[i][0], x[i][1], x[i][2]), x[i][3]);
         most = over_quarters_max(most);
         const float m1 = fmaxf(m, most);
         float fade = __builtin_amdgcn_exp2f(m - (m1 == -INFINITY ? 0.f : m1));
@@ -248,7 +323,7 @@ __global__ __launch_bounds__(256) void kv_rows_kernel(KvAttend a)
         } else if constexpr (CODED) {
             float big = 0.f;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) big = fmaxf(big, fmaxf(fmaxf(vsc[i][0], vsc[i][1]), fmaxf(vsc[i][2], vsc[i][3])));
+            for (int i = 0; i < 4; ++i) big = max3(big, max3(vsc[i][0], vsc[i][1], vsc[i][2]), vsc[i][3]);
             big = fmaxf(over_quarters_max(big), vunit);
             const float per = 1.f / big;
             fade *= vunit * per;
@@ -278,6 +353,7 @@ __global__ __launch_bounds__(256) void kv_rows_kernel(KvAttend a)
                 o[d] = mma<HALF>(f1, pr[1], o[d]);
             }
         }
+        __builtin_amdgcn_sched_barrier(0);
     }
 
     // the four waves' results joined: everything in units of the largest maximum
@@ -285,15 +361,15 @@ __global__ __launch_bounds__(256) void kv_rows_kernel(KvAttend a)
     if constexpr (HALF) m -= kHalfTop;
     const float back = CODED && HALF ? vunit : 1.f;
 #pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) join_o[wave][col][d * 16 + g * 4 + i] = o[d][i] * back;
+    for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4 *>(&join_o[wave][col][d * 16 + g * 4]) = o[d] * back;
     if (g == 0) {
         join_m[wave][col] = m;
         join_l[wave][col] = l;
     }
     __syncthreads();
     const int r = tid >> 4, sub = tid & 15; // 16 threads a row
+    const bool in_row = tile * 16 + r < rows;
+    const int otok = SPARSE ? token0 : sq.first + min(tile * 16 + r, rows - 1) / G, omember = (tile * 16 + r) % G;
     float mm = join_m[0][r];
 #pragma unroll
     for (int w = 1; w < 4; ++w) mm = fmaxf(mm, join_m[w][r]);
@@ -304,43 +380,52 @@ __global__ __launch_bounds__(256) void kv_rows_kernel(KvAttend a)
         f[w] = __builtin_amdgcn_exp2f(join_m[w][r] - mb);
         ll += f[w] * join_l[w][r];
     }
-    const int orow = tile * 16 + r;
-    if (orow >= rows) return;
-    if (a.n_split > 1) {
-        const size_t at = ((size_t)unit * c.H + h) * a.n_split + split;
-        if (sub == 0) {
-            a.part_ml[(at * 16 + r) * 2] = mm;
-            a.part_ml[(at * 16 + r) * 2 + 1] = ll;
-        }
-        float *po = a.part + (at * 16 + r) * DP;
-#pragma unroll
-        for (int d = 0; d < DP; d += 64) {
-            const int dd = d + sub * 4;
-            f32x4 y = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int w = 0; w < 4; ++w)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) y[i] += f[w] * join_o[w][r][dd + i];
-            *reinterpret_cast<f32x4 *>(po + dd) = y;
-        }
-        return;
-    }
-    const int otok = SPARSE ? token0 : sq.first + orow / G, omember = orow % G;
-    const size_t oh = (size_t)otok * c.H * G + h * G + omember;
-    const float inv = ll > 0.f ? 1.f / ll : 0.f;
-#pragma unroll
-    for (int d = 0; d < DP; d += 64) {
-        const int dd = d + sub * 4;
-        if (dd >= c.D) continue;
+    auto joined = [&](int dd) __attribute__((always_inline)) {
         f32x4 y = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int w = 0; w < 4; ++w)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) y[i] += f[w] * join_o[w][r][dd + i];
-        y *= inv;
-        *reinterpret_cast<u32x2 *>(a.out + (oh * c.D + dd) * 2) = u32x2{pack16<T>(y[0], y[1]), pack16<T>(y[2], y[3])};
+        for (int w = 0; w < 4; ++w) y += f[w] * *reinterpret_cast<const f32x4 *>(&join_o[w][r][dd]);
+        return y;
+    };
+    if (a.n_split == 1) {
+        if (in_row) kv_write_row<T, DP>(a, h, otok, omember, sub, mm, ll, joined);
+        return;
     }
-    if (sub == 0 && a.lse) a.lse[oh] = ll > 0.f ? (mm + __builtin_amdgcn_logf(ll)) * kLn2 : -INFINITY;
+    const size_t slot = (size_t)unit * c.H + h, first = slot * a.n_split;
+    if (in_row) {
+        const size_t pr = (first + split) * 16 + r;
+        if (sub == 0) *reinterpret_cast<f32x2 *>(a.part_ml + pr * 2) = f32x2{mm, ll};
+#pragma unroll
+        for (int d = 0; d < DP; d += 64) *reinterpret_cast<f32x4 *>(a.part + pr * DP + d + sub * 4) = joined(d + sub * 4);
+    }
+    if (!a.join_here) return;
+    // the last of the parts joins them all (what this one wrote is seen by it: release, and acquire where it is the last)
+    __syncthreads();
+    if (tid == 0) {
+        __threadfence();
+        arrived = atomicAdd(&a.arrivals[slot], 1u);
+    }
+    __syncthreads();
+    if (arrived != (uint32_t)a.n_split - 1) return;
+    __threadfence();
+    if (tid == 0) a.arrivals[slot] = 0; // for the next call
+    if (!in_row) return;
+    float jm = -INFINITY;
+    for (int s = 0; s < a.n_split; ++s) jm = fmaxf(jm, a.part_ml[((first + s) * 16 + r) * 2]);
+    const float jb = jm == -INFINITY ? 0.f : jm;
+    float jl = 0.f;
+    f32x4 y[DP / 64];
+#pragma unroll
+    for (int d = 0; d < DP / 64; ++d) y[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+    for (int s = 0; s < a.n_split; ++s) {
+        const size_t pr = (first + s) * 16 + r;
+        const f32x2 ml = *reinterpret_cast<const f32x2 *>(a.part_ml + pr * 2);
+        const float w = __builtin_amdgcn_exp2f(ml[0] - jb); // (a part that saw no key has zeros)
+        jl += w * ml[1];
+#pragma unroll
+        for (int d = 0; d < DP / 64; ++d) y[d] += w * *reinterpret_cast<const f32x4 *>(a.part + pr * DP + d * 64 + sub * 4);
+    }
+    kv_write_row<T, DP>(a, h, otok, omember, sub, jm, jl, [&](int dd) __attribute__((always_inline)) { return y[dd / 64]; });
 }
 
 // ------------------------------------------------------------------ long chunks
@@ -393,22 +478,11 @@ __device__ __forceinline__ int lds_piece(int row, int piece)
     return row * CH + (piece ^ (CH == 8 ? (row >> 1) & 7 : row & 15));
 }
 
-// A number that all lanes of a wave have.
-__device__ __forceinline__ int same(int x) { return __builtin_amdgcn_readfirstlane(x); }
-
 // The largest of a number's values in lanes l and l ^ 32.
 __device__ __forceinline__ float over_halves_max(float x)
 {
     const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-
-// The largest of three (without the rounds that fmaxf makes for signalling NaNs).
-__device__ __forceinline__ float max3(float a, float b, float c)
-{
-    float r;
-    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-    return r;
 }
 
 // All waves of the workgroup meet; what they read of or wrote to LDS before is done, loads from memory may still be on their way.
@@ -440,7 +514,7 @@ __device__ __forceinline__ void in_between()
 template <int S, int T, int DP, int NW, bool ONE>
 struct KvTiles {
     static constexpr int ES = KvBytes<S>::v, NT = NW * 64, CH = DP / 8;
-    static constexpr bool CODED = kv_coded<S>;
+    static constexpr bool CODED = kv_coded<S>, UNITS = CODED && T == PK_F16;
     static constexpr int PIECES = kKvTile * DP * ES / 16; // 16-byte pieces of a tile of K, and of one of V
     static constexpr int KP = (PIECES + NT - 1) / NT;     // of a thread
     static constexpr int KR = DP * ES / 16;               // pieces of a row of K
@@ -451,6 +525,7 @@ struct KvTiles {
         u32x4 k[2][kKvTile * CH];
         u32x4 v[2][DP * 8];
         float scales[CODED ? 4 : 1][2][kKvTile];
+        float fade[4], unit[4]; // half precision: what the sums so far are multiplied by, as the unit of V's scales grows with a tile, and that unit
     };
 
     const char *k, *v;
@@ -461,6 +536,7 @@ struct KvTiles {
     uint32_t kpage[PG], vpage[PG], spage; // of K(j), of V(j - 1); of the lane's token of K(j)
     u32x4 kw[KP], vw[KP];
     float ksw, vsw;
+    float unit;       // largest scale of a value so far (of the wave that brings them)
     uint32_t v_in;    // which of the thread's pieces of V(j - 1) lie in pages that the table has
     bool v_there;     // all of the wave's
     uint32_t in_next; // which of K(j)'s four runs of 16 tokens lie in such pages
@@ -469,7 +545,7 @@ struct KvTiles {
     {
         k = c.k, v = c.v, ks = c.ks, vs = c.vs, table = t;
         n_pages = c.n_pages, H = c.H, h = head, P = c.P, logP = c.logP, len = tokens;
-        spage = 0, ksw = 0.f, vsw = 0.f, in_next = 0, v_in = 0, v_there = true;
+        spage = 0, ksw = 0.f, vsw = 0.f, in_next = 0, v_in = 0, v_there = true, unit = 1e-30f;
     }
     // page of a position, of the nearest that the sequence has where it has none there
     __device__ __forceinline__ uint32_t page_of(int pos) const { return (uint32_t)table[min(max(pos, 0), max(len - 1, 0)) >> logP]; }
@@ -520,6 +596,9 @@ struct KvTiles {
         } else {
             v_in = 0;
 #pragma unroll
+            for (int i = 0; i < KP; ++i) asm volatile("" : "+v"(kpage[i]), "+v"(vpage[i]));
+            asm volatile("" : "+v"(spage));
+#pragma unroll
             for (int i = 0; i < KP; ++i) {
                 const int p = tid + i * NT;
                 if (mine) {
@@ -558,7 +637,7 @@ struct KvTiles {
         }
     }
 
-    __device__ __forceinline__ void store(int j, Lds &lds) const
+    __device__ __forceinline__ void store(int j, Lds &lds)
     {
         const int kb = j & 1, vb = kb ^ 1, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
         if (PIECES >= NT || tid < PIECES) {
@@ -581,7 +660,19 @@ struct KvTiles {
         }
         if constexpr (CODED) {
             if (wave == 0) lds.scales[j & 3][0][lane] = ksw;
-            if (wave == NW - 1) lds.scales[j & 3][1][lane] = vsw;
+            if (wave == NW - 1) {
+                if constexpr (UNITS) {
+                    float most = vsw;
+#pragma unroll
+                    for (int d = 1; d < 64; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
+                    most = fmaxf(most, unit);
+                    const float per = 1.f / most;
+                    if (lane == 0) lds.fade[j & 3] = unit * per, lds.unit[j & 3] = most;
+                    unit = most;
+                    vsw *= per;
+                }
+                lds.scales[j & 3][1][lane] = vsw;
+            }
         }
     }
 };
@@ -655,7 +746,7 @@ __global__ __launch_bounds__(NW * 64) void kv_tile_kernel(KvAttend a)
     for (int d = 0; d < DT; ++d)
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
-    float m = -INFINITY, l = 0.f, vunit = 1e-30f;
+    float m = -INFINITY, l = 0.f;
 
     KvTiles<S, T, DP, NW, ONE> in;
     in.begin(c, table, h, sq.len);
@@ -716,16 +807,8 @@ __global__ __launch_bounds__(NW * 64) void kv_tile_kernel(KvAttend a)
         }
         most = max3(most, most2, max3(s[0][15], s[1][15], s[1][15]));
         most = over_halves_max(most);
-        float unit_up = 1.f, per = 1.f;
-        if constexpr (CODED && HALF) {
-            float big = vs[lane];
-#pragma unroll
-            for (int d = 1; d < 64; d *= 2) big = fmaxf(big, __shfl_xor(big, d));
-            big = fmaxf(big, vunit);
-            per = 1.f / big;
-            unit_up = vunit * per;
-            vunit = big;
-        }
+        float unit_up = 1.f;
+        if constexpr (CODED && HALF) unit_up = lds.fade[t & 3];
         if (__any(most > m || unit_up != 1.f)) {
             const float m1 = fmaxf(m, most);
             const float fade = m1 == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - m1) * qscale);
@@ -746,7 +829,7 @@ __global__ __launch_bounds__(NW * 64) void kv_tile_kernel(KvAttend a)
             for (int j = 0; j < 8; ++j) {
                 p[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u >> 1][8 * (u & 1) + j], qscale, -base_m));
                 sum[j & 1] += p[j];
-                if constexpr (CODED) p[j] *= vs[u * 16 + hf * 8 + j] * (HALF ? per : 1.f);
+                if constexpr (CODED) p[j] *= vs[u * 16 + hf * 8 + j];
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -788,7 +871,7 @@ __global__ __launch_bounds__(NW * 64) void kv_tile_kernel(KvAttend a)
     }
     if (!valid) return;
     l += __shfl_xor(l, 32);
-    const float back = CODED && HALF ? vunit : 1.f;
+    const float back = CODED && HALF && t0 < t1 ? lds.unit[(t1 - 1) & 3] : 1.f;
     const float mm = m * qscale - (HALF ? kHalfTop : 0.f); // logarithm of what the weights are in units of
     if (a.n_split > 1) {
         const size_t pr = (((size_t)unit * c.H + h) * a.n_split + split) * BR + (wave * 32 + col);
@@ -818,28 +901,24 @@ __global__ __launch_bounds__(NW * 64) void kv_tile_kernel(KvAttend a)
     if (hf == 0 && a.lse) a.lse[oh] = l > 0.f ? (mm + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
 }
 
-// The parts of a row joined, in order: 16 threads a row.  Parts have BR rows; a workgroup joins 16 of them.
-template <int T, int DP, bool SPARSE, int BR>
+// The parts of a row joined, in order: 16 threads a row.  Parts have BR rows; a workgroup joins 16 of them.  BR 16: the parts of the kernel
+// for few rows, else of the one for many.
+template <int T, int DP, int BR, bool SPARSE>
 __global__ __launch_bounds__(256) void kv_join_kernel(KvAttend a)
 {
-    const int r = (blockIdx.x % (BR / 16)) * 16 + (threadIdx.x >> 4), sub = threadIdx.x & 15, h = blockIdx.y;
-    const KvDev &c = a.c;
-    const int G = a.G;
-    const int at_unit = blockIdx.x / (BR / 16);
-    int unit, tile;
+    const int r = (blockIdx.x % (BR / 16)) * 16 + (threadIdx.x >> 4), sub = threadIdx.x & 15, h = blockIdx.y, unit = blockIdx.x / (BR / 16);
+    KvUnit un;
     if constexpr (BR == 16) {
-        unit = at_unit / a.row_tiles;
-        tile = at_unit - unit * a.row_tiles;
+        const int of = unit / a.row_tiles;
+        un = KvUnit{SPARSE ? kv_seq_of(a.b, of) : of, unit - of * a.row_tiles};
     } else {
-        const KvUnit un = kv_unit<BR>(a, at_unit);
-        if (un.seq < 0) return;
-        unit = un.seq;
-        tile = un.tile;
+        un = kv_unit<BR>(a, unit);
     }
-    const KvSeq sq = kv_seq(a.b, SPARSE ? kv_seq_of(a.b, unit) : unit, c.P);
-    const int rows = SPARSE ? G : sq.m * G, row = tile * BR + r;
+    if (un.seq < 0) return;
+    const KvSeq sq = kv_seq(a.b, un.seq, a.c.P);
+    const int row = un.tile * BR + r, rows = SPARSE ? a.G : sq.m * a.G;
     if (row >= rows || (BR == 16 && !SPARSE && rows > a.few_rows)) return;
-    const size_t at = ((size_t)at_unit * c.H + h) * a.n_split;
+    const size_t at = ((size_t)unit * a.c.H + h) * a.n_split;
     float m = -INFINITY;
     for (int s = 0; s < a.n_split; ++s) m = fmaxf(m, a.part_ml[((at + s) * BR + r) * 2]);
     const float base = m == -INFINITY ? 0.f : m;
@@ -847,33 +926,27 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttend a)
     f32x4 y[DP / 64];
 #pragma unroll
     for (int d = 0; d < DP / 64; ++d) y[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
     for (int s = 0; s < a.n_split; ++s) {
-        const float ms = a.part_ml[((at + s) * BR + r) * 2], f = __builtin_amdgcn_exp2f(ms - base);
-        if (ms == -INFINITY) continue;
-        l += f * a.part_ml[((at + s) * BR + r) * 2 + 1];
+        const size_t pr = (at + s) * BR + r;
+        const f32x2 ml = *reinterpret_cast<const f32x2 *>(a.part_ml + pr * 2);
+        const float w = __builtin_amdgcn_exp2f(ml[0] - base); // (a part that saw no key has zeros)
+        l += w * ml[1];
 #pragma unroll
-        for (int d = 0; d < DP / 64; ++d) y[d] += f * *reinterpret_cast<const f32x4 *>(a.part + ((at + s) * BR + r) * DP + d * 64 + sub * 4);
+        for (int d = 0; d < DP / 64; ++d) y[d] += w * *reinterpret_cast<const f32x4 *>(a.part + pr * DP + d * 64 + sub * 4);
     }
-    const int tok = SPARSE ? unit : sq.first + row / G;
-    const size_t oh = (size_t)tok * c.H * G + h * G + row % G;
-    const float inv = l > 0.f ? 1.f / l : 0.f;
-#pragma unroll
-    for (int d = 0; d < DP / 64; ++d) {
-        const int dd = d * 64 + sub * 4;
-        if (dd >= c.D) continue;
-        y[d] *= inv;
-        *reinterpret_cast<u32x2 *>(a.out + (oh * c.D + dd) * 2) = u32x2{pack16<T>(y[d][0], y[d][1]), pack16<T>(y[d][2], y[d][3])};
-    }
-    if (sub == 0 && a.lse) a.lse[oh] = l > 0.f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+    const int tok = SPARSE ? unit / a.row_tiles : sq.first + row / a.G;
+    kv_write_row<T, DP>(a, h, tok, row % a.G, sub, m, l, [&](int dd) __attribute__((always_inline)) { return y[dd / 64]; });
 }
 
-// Parts that the keys are cut into: enough workgroups for the whole device, within the room for partial results, each of them with `least`
-// tiles of keys.
-void cut(KvAttend &a, int64_t items, int64_t tiles, int br, int num_wg, int least)
+// Parts that the keys are cut into (`tiles` tiles of 64 at most): so many that there are `wgs` workgroups, each with `least` tiles at least;
+// more of them, up to `more_wgs`, where each has `much` tiles, as sequences' lengths differ.  Within the room for partial results.
+void cut(KvAttend &a, int64_t items, int64_t tiles, int rows, int64_t wgs, int least, int64_t more_wgs, int much)
 {
-    const int64_t most = std::min<int64_t>((int64_t)kKvMaxPartials * 16 / br / std::max<int64_t>(items, 1), (num_wg + items - 1) / items);
-    const int64_t want = std::max<int64_t>(std::min(most, tiles / least), 1);
-    a.split_tiles = (int32_t)((tiles + want - 1) / want);
+    const int64_t room = a.part_floats / ((int64_t)rows * a.part_row) / std::max<int64_t>(items, 1);
+    const int64_t want = std::max(std::min((wgs + items - 1) / items, tiles / least), std::min((more_wgs + items - 1) / items, tiles / much));
+    const int64_t n = std::max<int64_t>(std::min(want, room), 1);
+    a.split_tiles = (int32_t)((tiles + n - 1) / n);
     a.n_split = (int32_t)((tiles + a.split_tiles - 1) / a.split_tiles);
 }
 
@@ -885,14 +958,17 @@ hipError_t run(KvAttend a, hipStream_t s)
     const int64_t seqs = SPARSE ? a.b.n_tokens : a.b.n_seqs;
     const int64_t rows = SPARSE ? a.G : (int64_t)a.b.max_new * a.G; // of a sequence at most
     a.few_rows = SPARSE ? INT32_MAX : kFewRows;
+    a.part_row = DP;
     // sequences of few rows: unless all have the same number of new tokens, and that is many
     const bool alike = !SPARSE && (int64_t)a.b.n_seqs * a.b.max_new == a.b.n_tokens;
     if (SPARSE || !alike || rows <= a.few_rows) {
         a.row_tiles = (int32_t)((std::min<int64_t>(rows, a.few_rows) + 15) / 16);
-        const int64_t units = seqs * a.row_tiles;
-        cut(a, units * a.c.H, tiles, 16, 6 * a.num_cu, 4);
-        kv_rows_kernel<S, T, DP, SPARSE><<<dim3((unsigned)(units * a.n_split), a.c.H), 256, 0, s>>>(a);
-        if (a.n_split > 1) kv_join_kernel<T, DP, SPARSE, 16><<<dim3((unsigned)units, a.c.H), 256, 0, s>>>(a);
+        const int64_t units = seqs * a.row_tiles, items = units * a.c.H;
+        cut(a, items, tiles, 16, 2 * a.num_cu, 4, 16 * a.num_cu, 32);
+        // the last part's workgroup joins them where all run at once; its fences cost more than a launch where there are many
+        a.join_here = items * a.n_split <= a.num_cu && items <= kKvArrivals;
+        kv_rows_kernel<S, T, DP, SPARSE><<<dim3((unsigned)(items * a.n_split)), 256, 0, s>>>(a);
+        if (a.n_split > 1 && !a.join_here) kv_join_kernel<T, DP, 16, SPARSE><<<dim3((unsigned)units, a.c.H), 256, 0, s>>>(a);
     }
     if constexpr (!SPARSE) {
         if (rows > a.few_rows) {
@@ -900,11 +976,11 @@ hipError_t run(KvAttend a, hipStream_t s)
             // row tiles of the sequences that have more rows than the others' kernel takes: at most
             const int64_t all = a.b.n_tokens * (int64_t)a.G, longs = std::min<int64_t>(a.b.n_seqs, all / (a.few_rows + 1));
             const int64_t units = alike ? seqs * ((rows + BR - 1) / BR) : std::min(longs * ((rows + BR - 1) / BR), all / BR + longs);
-            cut(a, units * a.c.H, tiles, BR, a.num_cu, 8);
+            cut(a, units * a.c.H, tiles, BR, a.num_cu, 8, (alike ? 1 : 4) * a.num_cu, 16);
             const dim3 grid((unsigned)(units * a.n_split * a.c.H));
             if (a.c.P >= kKvTile) kv_tile_kernel<S, T, DP, NW, true><<<grid, NW * 64, 0, s>>>(a);
             else kv_tile_kernel<S, T, DP, NW, false><<<grid, NW * 64, 0, s>>>(a);
-            if (a.n_split > 1) kv_join_kernel<T, DP, false, BR><<<dim3((unsigned)(units * (BR / 16)), a.c.H), 256, 0, s>>>(a);
+            if (a.n_split > 1) kv_join_kernel<T, DP, BR, false><<<dim3((unsigned)(units * (BR / 16)), a.c.H), 256, 0, s>>>(a);
         }
     }
     return hipGetLastError();
