@@ -132,23 +132,24 @@ __device__ __forceinline__ uint32_t pack16(float a, float b)
     }
 }
 
-// Four codes (one word) as four elements of type T, which holds each of them exactly.
-template <int S, int T>
+// int8 codes are held so that little turns them into operands: the matrix cores take denormal numbers as what they are, and a byte u in
+// the lower half of 16 bits is the number u times the type's smallest (2^-24, 2^-133).  Keys are held with 128 added, which a
+// product's start value takes back (-128 times the sum of the query, whole numbers of that unit: nothing is lost but what 32 bits round);
+// one byte permutation makes two operands.  Values are held as sign and magnitude, as an element that all heavy keys have as zero
+// has to come out of the sum as what the others make of it; a permutation and a mask make two operands, the sign bit in its place.
+// e4m3 codes have an instruction of their own.
+template <int S, int T> constexpr float kv_smallest = S != PK_I8 ? 1.f : T == PK_F16 ? 0x1p-24f : 0x1p-133f;
+
+// Four codes of keys, or of values, as four elements of type T, times the type's smallest number if S is PK_I8.
+template <int S, int T, bool VALUES>
 __device__ __forceinline__ void codes_to(uint32_t w, uint32_t &lo, uint32_t &hi)
 {
-    if constexpr (S == PK_I8 && T == PK_F16) {
-        // code + 128 next to the byte 0x64 is the number 1024 + 128 + code
-        const half2v off = {(_Float16)1152.f, (_Float16)1152.f};
-        w ^= 0x80808080u;
-        const half2v a = __builtin_bit_cast(half2v, __builtin_amdgcn_perm(0x64646464u, w, 0x04010400u)) - off;
-        const half2v b = __builtin_bit_cast(half2v, __builtin_amdgcn_perm(0x64646464u, w, 0x04030402u)) - off;
-        lo = __builtin_bit_cast(uint32_t, a);
-        hi = __builtin_bit_cast(uint32_t, b);
+    if constexpr (S == PK_I8 && VALUES) {
+        lo = __builtin_amdgcn_perm(w, w, 0x01010000u) & 0x807f807fu;
+        hi = __builtin_amdgcn_perm(w, w, 0x03030202u) & 0x807f807fu;
     } else if constexpr (S == PK_I8) {
-        // the upper halves of the codes as floats
-        const float a = (float)(int8_t)w, b = (float)(int8_t)(w >> 8), c = (float)(int8_t)(w >> 16), d = (float)(int8_t)(w >> 24);
-        lo = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
-        hi = __builtin_amdgcn_perm(__float_as_uint(d), __float_as_uint(c), 0x07060302u);
+        lo = __builtin_amdgcn_perm(w, w, 0x0c010c00u);
+        hi = __builtin_amdgcn_perm(w, w, 0x0c030c02u);
     } else if constexpr (T == PK_F16) {
         lo = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.f, false));
         hi = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.f, true));
@@ -158,11 +159,12 @@ __device__ __forceinline__ void codes_to(uint32_t w, uint32_t &lo, uint32_t &hi)
     }
 }
 
-// One code as the number that it stands for (before its scale).
-template <int S>
+// One code of a key, or of a value, as the number that it stands for (before its scale).
+template <int S, bool VALUES>
 __device__ __forceinline__ float code_value(uint8_t c)
 {
-    if constexpr (S == PK_I8) return (float)(int8_t)c;
+    if constexpr (S == PK_I8 && VALUES) return (float)(c & 0x80 ? -(int)(c & 0x7f) : (int)c);
+    else if constexpr (S == PK_I8) return (float)((int)c - 128);
     else {
         const half2v h = __builtin_bit_cast(half2v, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((uint32_t)c, 1.f, false));
         return (float)h[0];
@@ -176,12 +178,15 @@ __device__ __forceinline__ float code_factor(float most, float largest)
     return most > 0.f ? fminf(largest / most, 3.0e38f) : 0.f;
 }
 
-template <int S>
+template <int S, bool VALUES>
 __device__ __forceinline__ uint8_t to_code(float x, float up)
 {
     const float y = fminf(fmaxf(x * up, -kv_largest<S>), kv_largest<S>);
-    if constexpr (S == PK_I8) return (uint8_t)(int8_t)(int)rintf(y);
-    else return (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(y, y, 0, false);
+    if constexpr (S == PK_I8) {
+        const int code = (int)rintf(y);
+        return (uint8_t)(!VALUES ? code + 128 : code < 0 ? 0x80 - code : code);
+    }
+    return (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(y, y, 0, false);
 }
 
 // ------------------------------------------------------------------ launches

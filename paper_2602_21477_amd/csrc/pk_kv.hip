@@ -3,6 +3,7 @@
 #include <algorithm>
 #include <cmath>
 #include <new>
+#include <type_traits>
 
 #include "pk_kv.h"
 
@@ -96,7 +97,7 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(KvDev c, KvBatch b,
                 const float up = code_factor(most, kv_largest<S>);
                 scale = most * (1.f / kv_largest<S>);
 #pragma unroll
-                for (int i = 0; i < E; ++i) codes[i] = (char)to_code<S>(x[i], up);
+                for (int i = 0; i < E; ++i) codes[i] = (char)to_code<S, false>(x[i], up);
                 if (sub == 0) c.ks[ph * c.P + r] = scale;
             } else {
 #pragma unroll
@@ -116,7 +117,7 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(KvDev c, KvBatch b,
                 const float up = code_factor(most, kv_largest<S>);
                 if (sub == 0) c.vs[ph * c.P + r] = most * (1.f / kv_largest<S>);
 #pragma unroll
-                for (int i = 0; i < E; ++i) vt[(at + i) * pitch + r] = (char)to_code<S>(y[i], up);
+                for (int i = 0; i < E; ++i) vt[(at + i) * pitch + r] = (char)to_code<S, true>(y[i], up);
             } else {
 #pragma unroll
                 for (int i = 0; i < E; i += 2) {
@@ -133,7 +134,7 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(KvDev c, KvBatch b,
 #pragma unroll
             for (int i = 0; i < E; ++i) {
                 float z;
-                if constexpr (kv_coded<S>) z = code_value<S>((uint8_t)codes[i]) * scale;
+                if constexpr (kv_coded<S>) z = code_value<S, false>((uint8_t)codes[i]) * scale;
                 else {
                     uint16_t w;
                     __builtin_memcpy(&w, codes + 2 * i, 2);
@@ -220,8 +221,8 @@ __global__ __launch_bounds__(kThreads) void kv_read_kernel(KvDev c, KvBatch b, c
         reinterpret_cast<uint32_t *>(vt + d * vpitch)[w] = reinterpret_cast<const uint32_t *>(vp + (size_t)d * c.P * ES)[w];
     }
     __syncthreads();
-    auto element = [&](const char *at) {
-        if constexpr (kv_coded<S>) return code_value<S>((uint8_t)*at);
+    auto element = [&](const char *at, auto values) {
+        if constexpr (kv_coded<S>) return code_value<S, decltype(values)::value>((uint8_t)*at);
         else if constexpr (S == PK_BF16) return __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t *>(at) << 16);
         else return (float)*reinterpret_cast<const _Float16 *>(at);
     };
@@ -235,8 +236,8 @@ __global__ __launch_bounds__(kThreads) void kv_read_kernel(KvDev c, KvBatch b, c
         }
         const size_t t = (size_t)(q.first + (base + r - (q.len - q.m)));
         const size_t o = ((t * c.H + h) * c.D + d) * TS;
-        float k0 = element(kp + ((size_t)r * DP + d) * ES) * ks, k1 = element(kp + ((size_t)r * DP + d + 1) * ES) * ks;
-        float v0 = element(vt + d * vpitch + r * ES) * vs, v1 = element(vt + (d + 1) * vpitch + r * ES) * vs;
+        float k0 = element(kp + ((size_t)r * DP + d) * ES, std::false_type{}) * ks, k1 = element(kp + ((size_t)r * DP + d + 1) * ES, std::false_type{}) * ks;
+        float v0 = element(vt + d * vpitch + r * ES, std::true_type{}) * vs, v1 = element(vt + (d + 1) * vpitch + r * ES, std::true_type{}) * vs;
         if (!there) k0 = k1 = v0 = v1 = 0.f;
         if constexpr (T == PK_F32) {
             *reinterpret_cast<f32x2 *>(kout + o) = f32x2{k0, k1};

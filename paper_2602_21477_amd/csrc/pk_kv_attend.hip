@@ -8,7 +8,38 @@ namespace pk {
 namespace {
 
 constexpr int kFewRows = 64;     // most rows of queries of a sequence and head that are taken 16 at a time
-constexpr float kHalfTop = 15.f; // logarithm of the largest weight in half precision: 2^-39 of it is the smallest
+
+// How the second product's operands are scaled.  The largest weight is 2^top: in half precision that type has the more of its range
+// below it (2^-39 of it is the smallest), in bfloat16 it keeps the products with denormal codes where 32 bits are normal.  Both times a
+// value's scale goes into the weight in units of the largest seen, so that no size of them overflows.
+template <int S, int T>
+struct KvScaling {
+    static constexpr bool CODED = kv_coded<S>, HALF = T == PK_F16;
+    static constexpr bool TWICE = CODED && !HALF;             // a weight is the sum of two numbers
+    static constexpr bool UNITS = CODED && (HALF || S == PK_I8);
+    static constexpr float top = HALF ? 15.f : S == PK_I8 ? 127.f : 0.f;
+    static constexpr float l_unit = !HALF && S == PK_I8 ? 0x1p-27f : 1.f; // of the sum of weights: it does not overflow
+    // sums of weights, and of products (before the unit), in the end: both as if the largest weight were 1
+    static constexpr float l_back = HALF ? 0x1p-15f : S == PK_I8 ? 0x1p-100f : 1.f;
+    static constexpr float o_back = S != PK_I8 ? l_back : HALF ? 0x1p9f : 0x1p6f;
+};
+
+// A query's part of the scores' scale.  PK_I8: the query times a power of two that keeps its products with denormal codes where 32 bits are
+// normal (half precision needs none), and the start value of a product, from the sum of the scaled query.
+template <int S, int T>
+struct KvQueryScale {
+    float near = 1.f, back = 1.f;
+    __device__ __forceinline__ void largest(float most)
+    {
+        if constexpr (S == PK_I8 && T == PK_F16) back = 0x1p24f;
+        if constexpr (S == PK_I8 && T == PK_BF16) {
+            const int e = (int)((__float_as_uint(most) >> 23) & 0xffu) - 127, f = min(max(100 - e, 6), 127);
+            near = __uint_as_float((uint32_t)(127 + f) << 23);
+            back = __uint_as_float((uint32_t)(127 + 133 - f) << 23);
+        }
+    }
+    __device__ __forceinline__ float start(float sum) const { return S != PK_I8 ? 0.f : -sum * (T == PK_F16 ? 0x1p-17f : 0x1p-126f); }
+};
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 // acc += A (16 rows x 32) B (32 x 16 columns), 16-bit operands
@@ -20,18 +51,18 @@ __device__ __forceinline__ f32x4 mma(u32x4 a, u32x4 b, f32x4 acc)
 }
 
 // Sixteen bytes of a row as operands of a product: one of 8 elements, or two of 8 codes each.
-template <int S, int T>
+template <int S, int T, bool VALUES>
 __device__ __forceinline__ void operands(u32x4 w, u32x4 &first, u32x4 &second)
 {
     if constexpr (kv_coded<S>) {
         uint32_t lo, hi;
-        codes_to<S, T>(w[0], lo, hi);
+        codes_to<S, T, VALUES>(w[0], lo, hi);
         first[0] = lo, first[1] = hi;
-        codes_to<S, T>(w[1], lo, hi);
+        codes_to<S, T, VALUES>(w[1], lo, hi);
         first[2] = lo, first[3] = hi;
-        codes_to<S, T>(w[2], lo, hi);
+        codes_to<S, T, VALUES>(w[2], lo, hi);
         second[0] = lo, second[1] = hi;
-        codes_to<S, T>(w[3], lo, hi);
+        codes_to<S, T, VALUES>(w[3], lo, hi);
         second[2] = lo, second[3] = hi;
     } else {
         first = w;
@@ -89,9 +120,8 @@ __device__ __forceinline__ void kv_write_row(const KvAttend &a, int h, int tok, 
 //     row m of product t is key 16 (m / 4) + 4 t + (m % 4) of the tile, so that lane (column, quarter g) ends up with keys
 //     16 g .. 16 g + 15 of its query, and loads those same 16 tokens of the values' channels
 // One pass with a running maximum and sum per query, in 32 bits.  Products are taken in the queries' type, which holds 8-bit codes
-// exactly; weights are rounded to it for the second one.  With codes a weight carries the value's scale.  In half precision that
-// is in units of the largest scale seen, and the largest weight is 2^kHalfTop, as that type has the more of its range below it; in bfloat16,
-// whose 8 bits are fewer than the codes are worth, a weight is the sum of two numbers, and its product two.
+// exactly; weights, which carry the values' scales, are rounded to it for the second one: in bfloat16, whose 8 bits are fewer than the
+// codes are worth, to the sum of two numbers.
 // Bound by memory: K of a wave's next tile is asked for when the products with this one's are done, V of a tile when its K is about to be
 // used, and the pages of both a round (their blocks, where they are listed, two rounds) earlier, so that a wave always has 8 or 16 KB on
 // its way.  Where the keys are cut into few parts, the workgroup that ends last joins them, in their order: no launch of its own.
@@ -101,7 +131,8 @@ template <int S, int T, int DP, bool SPARSE>
 __global__ __launch_bounds__(256) void kv_rows_kernel(KvAttend a)
 {
     constexpr int ES = KvBytes<S>::v;
-    constexpr bool CODED = kv_coded<S>, HALF = T == PK_F16, TWICE = CODED && !HALF;
+    using Sc = KvScaling<S, T>;
+    constexpr bool CODED = Sc::CODED, HALF = Sc::HALF, TWICE = Sc::TWICE;
     constexpr int EL = 16 / ES;               // elements of a 16-byte load
     constexpr int KC = DP / (4 * EL);         // such loads of a lane for one row of K
     constexpr int KS = DP / 32;               // products over the channels
@@ -171,7 +202,10 @@ __global__ __launch_bounds__(256) void kv_rows_kernel(KvAttend a)
             return in ? (block << c.logP) + (at & (P - 1)) : -1;
         } else return t < t1 && at < sq.len ? at : -1;
     };
-    auto page_of = [&](int base) __attribute__((always_inline)) -> uint32_t { return base >= 0 ? (uint32_t)table[base >> c.logP] : c.n_pages; };
+    auto page_of = [&](int base) __attribute__((always_inline)) -> uint32_t {
+        const uint32_t page = (uint32_t)table[max(base, 0) >> c.logP]; // (asked for whether wanted or not: no branch)
+        return base >= 0 ? page : c.n_pages;
+    };
     u32x4 kw[4][KC];
     auto ask_k = [&](const KvRun &r) __attribute__((always_inline)) {
         const size_t ph = (size_t)(r.page < c.n_pages ? r.page : 0) * c.H + h;
@@ -195,27 +229,37 @@ __global__ __launch_bounds__(256) void kv_rows_kernel(KvAttend a)
 
     // queries, as the right operand
     u32x4 qf[KS];
-    const float qscale = a.scale * kLog2e;
+    float qscale = a.scale * kLog2e, x0;
     {
         const char *qrow = a.q.data + ((size_t)tok * a.q.token_stride + (size_t)(h * G + member) * a.q.head_stride) * 2;
-        float x[KS][8];
+        float x[KS][8], most = 0.f, sum = 0.f;
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
             const int at = CODED ? (k >> 1) * 64 + g * 16 + (k & 1) * 8 : k * 32 + g * 8;
 #pragma unroll
             for (int i = 0; i < 8; ++i) x[k][i] = 0.f;
             if (valid && at < c.D) load_eight<T>(x[k], qrow, at);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) most = fmaxf(most, fabsf(x[k][i]));
         }
+        KvQueryScale<S, T> qs;
+        qs.largest(over_quarters_max(most));
 #pragma unroll
         for (int k = 0; k < KS; ++k)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) qf[k][i] = pack16<T>(x[k][2 * i], x[k][2 * i + 1]);
+            for (int i = 0; i < 8; i += 2) {
+                x[k][i] *= qs.near, x[k][i + 1] *= qs.near;
+                sum += x[k][i] + x[k][i + 1];
+                qf[k][i / 2] = pack16<T>(x[k][i], x[k][i + 1]);
+            }
+        x0 = qs.start(over_quarters_sum(sum));
+        qscale *= qs.back;
     }
 
     f32x4 o[DT];
 #pragma unroll
     for (int d = 0; d < DT; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
-    float m = -INFINITY, l = 0.f, vunit = 1e-30f;
+    float m = -INFINITY, l = 0.f, vunit = 1e-30f, vper = 1e30f; // (of the scales of values: the largest so far, at least this)
 
     if (tw < t1) ask_k(kr);
     for (int t = tw; t < t1; t += 4) {
@@ -245,11 +289,11 @@ __global__ __launch_bounds__(256) void kv_rows_kernel(KvAttend a)
         f32x4 x[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            x[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+            x[i] = f32x4{x0, x0, x0, x0};
 #pragma unroll
             for (int k = 0; k < KC; ++k) {
                 u32x4 f0, f1;
-                operands<S, T>(kw[i][k], f0, f1);
+                operands<S, T, false>(kw[i][k], f0, f1);
                 if constexpr (CODED) {
                     x[i] = mma<HALF>(f0, qf[2 * k], x[i]);
                     x[i] = mma<HALF>(f1, qf[2 * k + 1], x[i]);
@@ -259,12 +303,13 @@ __global__ __launch_bounds__(256) void kv_rows_kernel(KvAttend a)
             }
         }
         __builtin_amdgcn_sched_barrier(0);
-        // the next round's K; the pages of the one after it
+        // the pages of the round after the next (first: whoever waits for them does not wait for K), and the next round's K
         kr = kr1, vr = vr1;
-        ask_k(kr);
         kr1.base = base_of(t + 8, ksub, kblock), vr1.base = base_of(t + 8, g, vblock);
         kr1.page = page_of(kr1.base), vr1.page = page_of(vr1.base);
         kblock = block_of(t + 12, ksub), vblock = block_of(t + 12, g);
+        __builtin_amdgcn_sched_barrier(0);
+        ask_k(kr);
         __builtin_amdgcn_sched_barrier(0);
 
 #pragma unroll
@@ -303,10 +348,26 @@ __global__ __launch_bounds__(256) void kv_rows_kernel(KvAttend a)
 #pragma unroll
         for (int i = 0; i < 4; ++i) most = max3(most, max3(x[i][0], x[i][1], x[i][2]), x[i][3]);
         most = over_quarters_max(most);
-        const float m1 = fmaxf(m, most);
-        float fade = __builtin_amdgcn_exp2f(m - (m1 == -INFINITY ? 0.f : m1));
-        m = m1;
-        const float base = (m1 == -INFINITY ? 0.f : m1) - (HALF ? kHalfTop : 0.f);
+        float big = 0.f;
+        if constexpr (Sc::UNITS) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) big = max3(big, max3(vsc[i][0], vsc[i][1], vsc[i][2]), vsc[i][3]);
+        }
+        if (__any(most > m || big > vunit)) { // else all stays as it is
+            const float m1 = fmaxf(m, most);
+            float fade = m1 == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - m1);
+            m = m1;
+            l *= fade;
+            if constexpr (Sc::UNITS) {
+                big = fmaxf(over_quarters_max(big), vunit);
+                vper = 1.f / big;
+                fade *= vunit * vper;
+                vunit = big;
+            }
+#pragma unroll
+            for (int d = 0; d < DT; ++d) o[d] *= fade;
+        }
+        const float base = (m == -INFINITY ? 0.f : m) - Sc::top;
         f32x4 p[4];
         float sum = 0.f;
 #pragma unroll
@@ -314,22 +375,12 @@ __global__ __launch_bounds__(256) void kv_rows_kernel(KvAttend a)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 p[i][j] = __builtin_amdgcn_exp2f(x[i][j] - base);
-                sum += p[i][j];
+                sum = __builtin_fmaf(p[i][j], Sc::l_unit, sum);
             }
-        l = l * fade + sum;
-        if constexpr (TWICE) {
+        l += sum;
+        if constexpr (CODED) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) p[i] *= vsc[i];
-        } else if constexpr (CODED) {
-            float big = 0.f;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) big = max3(big, max3(vsc[i][0], vsc[i][1], vsc[i][2]), vsc[i][3]);
-            big = fmaxf(over_quarters_max(big), vunit);
-            const float per = 1.f / big;
-            fade *= vunit * per;
-            vunit = big;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) p[i] *= vsc[i] * per;
+            for (int i = 0; i < 4; ++i) p[i] *= Sc::UNITS ? vsc[i] * vper : vsc[i];
         }
         u32x4 pf[2], pr[2]; // weights, and (TWICE) what their rounding left
 #pragma unroll
@@ -342,9 +393,8 @@ __global__ __launch_bounds__(256) void kv_rows_kernel(KvAttend a)
             }
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
-            o[d] *= fade;
             u32x4 f0, f1;
-            operands<S, T>(vw[d][0], f0, f1);
+            operands<S, T, true>(vw[d][0], f0, f1);
             if constexpr (!CODED) f1 = vw[d][VC - 1];
             o[d] = mma<HALF>(f0, pf[0], o[d]);
             o[d] = mma<HALF>(f1, pf[1], o[d]);
@@ -357,9 +407,8 @@ __global__ __launch_bounds__(256) void kv_rows_kernel(KvAttend a)
     }
 
     // the four waves' results joined: everything in units of the largest maximum
-    l = over_quarters_sum(l);
-    if constexpr (HALF) m -= kHalfTop;
-    const float back = CODED && HALF ? vunit : 1.f;
+    l = over_quarters_sum(l) * Sc::l_back;
+    const float back = Sc::UNITS ? Sc::o_back * vunit : Sc::o_back;
 #pragma unroll
     for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4 *>(&join_o[wave][col][d * 16 + g * 4]) = o[d] * back;
     if (g == 0) {
@@ -514,7 +563,7 @@ __device__ __forceinline__ void in_between()
 template <int S, int T, int DP, int NW, bool ONE>
 struct KvTiles {
     static constexpr int ES = KvBytes<S>::v, NT = NW * 64, CH = DP / 8;
-    static constexpr bool CODED = kv_coded<S>, UNITS = CODED && T == PK_F16;
+    static constexpr bool CODED = kv_coded<S>, UNITS = KvScaling<S, T>::UNITS;
     static constexpr int PIECES = kKvTile * DP * ES / 16; // 16-byte pieces of a tile of K, and of one of V
     static constexpr int KP = (PIECES + NT - 1) / NT;     // of a thread
     static constexpr int KR = DP * ES / 16;               // pieces of a row of K
@@ -525,7 +574,7 @@ struct KvTiles {
         u32x4 k[2][kKvTile * CH];
         u32x4 v[2][DP * 8];
         float scales[CODED ? 4 : 1][2][kKvTile];
-        float fade[4], unit[4]; // half precision: what the sums so far are multiplied by, as the unit of V's scales grows with a tile, and that unit
+        float fade[4], unit[4]; // UNITS: what the sums so far are multiplied by, as the unit of V's scales grows with a tile, and that unit
     };
 
     const char *k, *v;
@@ -646,10 +695,10 @@ struct KvTiles {
                 const int p = tid + i * NT;
                 if constexpr (CODED) {
                     u32x4 f0, f1;
-                    operands<S, T>(kw[i], f0, f1);
+                    operands<S, T, false>(kw[i], f0, f1);
                     lds.k[kb][lds_piece<CH>(p / KR, (p % KR) * 2)] = f0;
                     lds.k[kb][lds_piece<CH>(p / KR, (p % KR) * 2 + 1)] = f1;
-                    operands<S, T>(vw[i], f0, f1);
+                    operands<S, T, true>(vw[i], f0, f1);
                     lds.v[vb][lds_piece<8>(p / VR, (p % VR) * 2)] = f0;
                     lds.v[vb][lds_piece<8>(p / VR, (p % VR) * 2 + 1)] = f1;
                 } else {
@@ -694,7 +743,8 @@ template <int S, int T, int DP, int NW, bool ONE>
 __global__ __launch_bounds__(NW * 64) void kv_tile_kernel(KvAttend a)
 {
     constexpr int BR = NW * 32;
-    constexpr bool CODED = kv_coded<S>, HALF = T == PK_F16, TWICE = CODED && !HALF;
+    using Sc = KvScaling<S, T>;
+    constexpr bool CODED = Sc::CODED, HALF = Sc::HALF, TWICE = Sc::TWICE;
     constexpr int KS = DP / 16, DT = DP / 32, CH = DP / 8;
     __shared__ __align__(16) typename KvTiles<S, T, DP, NW, ONE>::Lds lds;
     const int tid = threadIdx.x, wave = same(tid >> 6), lane = tid & 63, col = lane & 31, hf = lane >> 5;
@@ -726,20 +776,33 @@ __global__ __launch_bounds__(NW * 64) void kv_tile_kernel(KvAttend a)
     const int t0 = max(first_of(tile * BR), split * a.split_tiles), t1 = min(last_of(tile * BR + BR - 1), (split + 1) * a.split_tiles);
 
     u32x4 qf[KS];
+    float qscale = a.scale != 0.f ? fabsf(a.scale) * kLog2e : 1.f, s0;
     {
         const char *qrow = a.q.data + ((size_t)tok * a.q.token_stride + (size_t)(h * G + member) * a.q.head_stride) * 2;
         const float sign = a.scale > 0.f ? 1.f : a.scale < 0.f ? -1.f : 0.f;
+        float x[KS][8], most = 0.f, sum = 0.f;
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
-            float x[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = 0.f;
-            if (valid && k * 16 + hf * 8 < c.D) load_eight<T>(x, qrow, k * 16 + hf * 8);
+            for (int i = 0; i < 8; ++i) x[k][i] = 0.f;
+            if (valid && k * 16 + hf * 8 < c.D) load_eight<T>(x[k], qrow, k * 16 + hf * 8);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) qf[k][i] = pack16<T>(x[2 * i] * sign, x[2 * i + 1] * sign);
+            for (int i = 0; i < 8; ++i) most = fmaxf(most, fabsf(x[k][i]));
         }
+        KvQueryScale<S, T> qs;
+        qs.largest(over_halves_max(most));
+        qs.near *= sign;
+#pragma unroll
+        for (int k = 0; k < KS; ++k)
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) {
+                x[k][i] *= qs.near, x[k][i + 1] *= qs.near;
+                sum += x[k][i] + x[k][i + 1];
+                qf[k][i / 2] = pack16<T>(x[k][i], x[k][i + 1]);
+            }
+        s0 = qs.start(sum + __shfl_xor(sum, 32));
+        qscale *= qs.back;
     }
-    const float qscale = a.scale != 0.f ? fabsf(a.scale) * kLog2e : 1.f;
 
     f32x16 o[DT];
 #pragma unroll
@@ -773,7 +836,7 @@ __global__ __launch_bounds__(NW * 64) void kv_tile_kernel(KvAttend a)
 #pragma unroll
         for (int r = 0; r < 2; ++r)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s[r][i] = 0.f;
+            for (int i = 0; i < 16; ++i) s[r][i] = s0;
 #pragma unroll
         for (int k = 0; k < KS; ++k)
 #pragma unroll
@@ -808,7 +871,7 @@ __global__ __launch_bounds__(NW * 64) void kv_tile_kernel(KvAttend a)
         most = max3(most, most2, max3(s[0][15], s[1][15], s[1][15]));
         most = over_halves_max(most);
         float unit_up = 1.f;
-        if constexpr (CODED && HALF) unit_up = lds.fade[t & 3];
+        if constexpr (Sc::UNITS) unit_up = lds.fade[t & 3];
         if (__any(most > m || unit_up != 1.f)) {
             const float m1 = fmaxf(m, most);
             const float fade = m1 == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - m1) * qscale);
@@ -820,7 +883,7 @@ __global__ __launch_bounds__(NW * 64) void kv_tile_kernel(KvAttend a)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) o[d][i] *= f;
         }
-        const float base_m = (m == -INFINITY ? 0.f : m * qscale) - (HALF ? kHalfTop : 0.f);
+        const float base_m = (m == -INFINITY ? 0.f : m * qscale) - Sc::top;
         float sum[2] = {0.f, 0.f};
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
@@ -828,7 +891,7 @@ __global__ __launch_bounds__(NW * 64) void kv_tile_kernel(KvAttend a)
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 p[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u >> 1][8 * (u & 1) + j], qscale, -base_m));
-                sum[j & 1] += p[j];
+                sum[j & 1] = __builtin_fmaf(p[j], Sc::l_unit, sum[j & 1]);
                 if constexpr (CODED) p[j] *= vs[u * 16 + hf * 8 + j];
             }
 #pragma unroll
@@ -870,9 +933,9 @@ __global__ __launch_bounds__(NW * 64) void kv_tile_kernel(KvAttend a)
         if (NW > 4 && !late) meet();
     }
     if (!valid) return;
-    l += __shfl_xor(l, 32);
-    const float back = CODED && HALF && t0 < t1 ? lds.unit[(t1 - 1) & 3] : 1.f;
-    const float mm = m * qscale - (HALF ? kHalfTop : 0.f); // logarithm of what the weights are in units of
+    l = (l + __shfl_xor(l, 32)) * Sc::l_back;
+    const float back = Sc::UNITS && t0 < t1 ? Sc::o_back * lds.unit[(t1 - 1) & 3] : Sc::o_back;
+    const float mm = m * qscale;
     if (a.n_split > 1) {
         const size_t pr = (((size_t)unit * c.H + h) * a.n_split + split) * BR + (wave * 32 + col);
         if (hf == 0) {
