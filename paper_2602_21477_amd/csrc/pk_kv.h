@@ -7,9 +7,12 @@ namespace pk {
 
 // ------------------------------------------------------------------ layout
 // Regions of the arena, each [pages][heads] of one page's
-//   k   [P][DP]      keys, a row per token, zero padded from D to DP channels
-//   v   [DP][P]      values, a row per channel: a matrix product over tokens takes 8 or 16 consecutive tokens of a
-//                    channel per lane straight from memory, with no transposition in the kernels that read it
+//   k, v [P / 16]    runs of 16 tokens, DP channels each (zero padded from D), in the order in which a wave's lanes take them as a
+//                    product's operands, 16 bytes a lane.  Neighbouring lanes have to have neighbouring bytes: a load whose lanes
+//                    lie 16 bytes each in rows of their own is 64 accesses of the first cache, not 16, and bound by them (sparse
+//                    attention of 1024 tokens to 32 blocks each of int8: 1.0 of 1.1 million cycles).
+//                    Keys: groups of four tokens, their rows' 16-byte pieces side by side [4][DP * bytes / 16][4 tokens][16 bytes].
+//                    Values: 16 bytes of one channel, 16 or 8 tokens, the channels side by side [1 or 2][DP][16 bytes].
 //   ks, vs [P]       scales of keys and values (8-bit storages)
 //   bc  [2][DP]      bounds of the keys (largest, smallest value of each channel) in int8, zero padded
 //   bs  [1]          their scale
@@ -21,6 +24,18 @@ struct KvDev {
     uint32_t n_pages;
     int32_t H, D, P, logP;
 };
+
+// Where byte `at` of a token's key lies in its page and head, and a token's value of channel d.
+template <int ES, int DP>
+__device__ __forceinline__ int k_place(int tok, int at)
+{
+    return (tok >> 2) * (DP * ES * 4) + (at >> 4) * 64 + (tok & 3) * 16 + (at & 15);
+}
+template <int ES, int DP>
+__device__ __forceinline__ int v_place(int tok, int d)
+{
+    return (tok * ES >> 4) * (DP * 16) + d * 16 + (tok * ES & 15);
+}
 
 // One call's batch, as the kernels get it.
 struct KvBatch {

@@ -3,7 +3,6 @@
 #include <algorithm>
 #include <cmath>
 #include <new>
-#include <type_traits>
 
 #include "pk_kv.h"
 
@@ -48,31 +47,94 @@ __device__ __forceinline__ void load_row(float (&x)[E], const char *row, int at,
     }
 }
 
+// A page's keys (or values) as they lie in memory, in LDS: values with 16 bytes more for every 8 channels, so that lanes that share
+// a row write to banks of their own.
+template <int ES, int DP>
+__device__ __forceinline__ int v_image(int tok, int d)
+{
+    return (tok * ES >> 4) * (DP * 18) + d * 16 + (d >> 3) * 16 + (tok * ES & 15);
+}
+template <int ES, int DP>
+constexpr size_t image_bytes(int P)
+{
+    return (size_t)P * DP * ES + (size_t)P * ES / 16 * DP * 18;
+}
+
+// What a workgroup does: one page that the batch touches, one head.
+struct KvPage {
+    KvSeq q;
+    int lp, base, p0, p1; // its number in the sequence, its first position, the rows of the batch's new tokens in it
+    uint32_t page;
+};
+__device__ __forceinline__ bool kv_page_of(const KvDev &c, const KvBatch &b, KvPage &g)
+{
+    const int s = blockIdx.z;
+    g.q = kv_seq(b, s, c.P);
+    const int begin = max(g.q.len - g.q.m, 0);
+    g.lp = (begin >> c.logP) + (int)blockIdx.x;
+    if (g.q.m == 0 || ((long long)g.lp << c.logP) >= g.q.len) return false;
+    g.page = (uint32_t)b.tables[(size_t)s * b.table_stride + g.lp];
+    g.base = g.lp << c.logP;
+    g.p0 = max(begin - g.base, 0);
+    g.p1 = min(g.q.len - g.base, c.P);
+    return true;
+}
+
+// E consecutive elements of a row as they are stored: codes with a scale, or 16 bits.
+template <int S, int E, bool VALUES>
+__device__ __forceinline__ float encode(const float (&x)[E], char (&codes)[E * KvBytes<S>::v])
+{
+    if constexpr (kv_coded<S>) {
+        float most = 0.f;
+#pragma unroll
+        for (int i = 0; i < E; ++i) most = fmaxf(most, fabsf(x[i]));
+        most = quarter_max(most);
+        const float up = code_factor(most, kv_largest<S>);
+#pragma unroll
+        for (int i = 0; i < E; ++i) codes[i] = (char)to_code<S, VALUES>(x[i], up);
+        return most * (1.f / kv_largest<S>);
+    } else {
+#pragma unroll
+        for (int i = 0; i < E; i += 2) {
+            const uint32_t w = pack16<S>(x[i], x[i + 1]);
+            __builtin_memcpy(codes + 2 * i, &w, 4);
+        }
+        return 1.f;
+    }
+}
+template <int S, bool VALUES>
+__device__ __forceinline__ float decode(const char *codes, int i)
+{
+    if constexpr (kv_coded<S>) return code_value<S, VALUES>((uint8_t)codes[i]);
+    else {
+        uint16_t w;
+        __builtin_memcpy(&w, codes + 2 * i, 2);
+        if constexpr (S == PK_BF16) return __uint_as_float((uint32_t)w << 16);
+        else return (float)__builtin_bit_cast(_Float16, w);
+    }
+}
+
 // One workgroup: one page that the batch touches, one head.  A row is read by 16 lanes, its largest magnitude found by four
-// exchanges, its codes written as they come; values go through LDS, as their page is held by channels.  The bounds of the page's
+// exchanges; the page's new parts are put together in LDS and go out 16 bytes a lane, in order.  The bounds of the page's
 // keys are made of the rows that the cache holds once the call is over: those of this call from registers, older ones
-// read back.  They depend on the rows alone, not on the calls that brought them.
+// read back.  They depend on the rows alone, not on the calls that brought them.  Bound by memory: every row is read once and
+// its codes written once.
 template <int S, int T, int DP>
 __global__ __launch_bounds__(kThreads) void kv_append_kernel(KvDev c, KvBatch b, KvRows kin, KvRows vin)
 {
     constexpr int ES = KvBytes<S>::v;
     constexpr int E = DP / kRowLanes; // elements of a lane
-    __shared__ __align__(16) char vt[DP * kKvMaxPage * ES];
+    extern __shared__ __align__(16) char image[];
     __shared__ float red[4][2][DP];
-    const int s = blockIdx.z, h = blockIdx.y, tid = threadIdx.x;
-    const KvSeq q = kv_seq(b, s, c.P);
-    const int begin = max(q.len - q.m, 0);
-    const int lp = (begin >> c.logP) + (int)blockIdx.x;
-    if (q.m == 0 || ((long long)lp << c.logP) >= q.len) return;
-    const uint32_t page = (uint32_t)b.tables[(size_t)s * b.table_stride + lp];
-    if (page >= c.n_pages) return;
-    const int base = lp << c.logP;
-    const int p0 = max(begin - base, 0), p1 = min(q.len - base, c.P); // rows of this call in the page
-    const size_t ph = (size_t)page * c.H + h;
+    const int h = blockIdx.y, tid = threadIdx.x;
+    KvPage g;
+    if (!kv_page_of(c, b, g) || g.page >= c.n_pages) return;
+    const int p0 = g.p0, p1 = g.p1;
+    char *kimg = image, *vimg = image + c.P * DP * ES;
+    const size_t ph = (size_t)g.page * c.H + h;
     char *kp = c.k + ph * c.P * DP * ES;
-    char *vp = c.v + ph * DP * c.P * ES;
+    char *vp = c.v + ph * c.P * DP * ES;
     const int sub = tid & (kRowLanes - 1), at = sub * E;
-    const int pitch = c.P * ES;
 
     float hi[E], lo[E];
 #pragma unroll
@@ -83,64 +145,40 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(KvDev c, KvBatch b,
     for (int r0 = 0; r0 < p1; r0 += kRowsAtOnce) {
         const int r = r0 + tid / kRowLanes;
         const bool in = r < p1, fresh = in && r >= p0;
-        float x[E];
         float scale = 1.f;
         char codes[E * ES];
         if (fresh) {
-            const int t = q.first + (base + r - (q.len - q.m));
+            const int t = g.q.first + (g.base + r - (g.q.len - g.q.m));
+            float x[E], y[E];
             load_row<T, E>(x, kin.data + ((size_t)t * kin.token_stride + (size_t)h * kin.head_stride) * (T == PK_F32 ? 4 : 2), at, c.D);
-            if constexpr (kv_coded<S>) {
-                float most = 0.f;
-#pragma unroll
-                for (int i = 0; i < E; ++i) most = fmaxf(most, fabsf(x[i]));
-                most = quarter_max(most);
-                const float up = code_factor(most, kv_largest<S>);
-                scale = most * (1.f / kv_largest<S>);
-#pragma unroll
-                for (int i = 0; i < E; ++i) codes[i] = (char)to_code<S, false>(x[i], up);
-                if (sub == 0) c.ks[ph * c.P + r] = scale;
-            } else {
-#pragma unroll
-                for (int i = 0; i < E; i += 2) {
-                    const uint32_t w = pack16<S>(x[i], x[i + 1]);
-                    __builtin_memcpy(codes + 2 * i, &w, 4);
-                }
-            }
-            __builtin_memcpy(kp + ((size_t)r * DP + at) * ES, codes, E * ES);
-            float y[E];
             load_row<T, E>(y, vin.data + ((size_t)t * vin.token_stride + (size_t)h * vin.head_stride) * (T == PK_F32 ? 4 : 2), at, c.D);
+            const float vscale = encode<S, E, true>(y, codes);
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                if constexpr (ES == 1) vimg[v_image<ES, DP>(r, at + i)] = codes[i];
+                else __builtin_memcpy(vimg + v_image<ES, DP>(r, at + i), codes + 2 * i, 2);
+            }
+            scale = encode<S, E, false>(x, codes);
+            // (a lane's bytes lie in pieces of 16, or in one)
+            constexpr int N = E * ES < 16 ? E * ES : 16;
+#pragma unroll
+            for (int i = 0; i < E * ES; i += N) __builtin_memcpy(kimg + k_place<ES, DP>(r, at * ES + i), codes + i, N);
             if constexpr (kv_coded<S>) {
-                float most = 0.f;
-#pragma unroll
-                for (int i = 0; i < E; ++i) most = fmaxf(most, fabsf(y[i]));
-                most = quarter_max(most);
-                const float up = code_factor(most, kv_largest<S>);
-                if (sub == 0) c.vs[ph * c.P + r] = most * (1.f / kv_largest<S>);
-#pragma unroll
-                for (int i = 0; i < E; ++i) vt[(at + i) * pitch + r] = (char)to_code<S, true>(y[i], up);
-            } else {
-#pragma unroll
-                for (int i = 0; i < E; i += 2) {
-                    const uint32_t w = pack16<S>(y[i], y[i + 1]);
-                    reinterpret_cast<uint16_t *>(vt + (at + i) * pitch)[r] = (uint16_t)w;
-                    reinterpret_cast<uint16_t *>(vt + (at + i + 1) * pitch)[r] = (uint16_t)(w >> 16);
+                if (sub == 0) {
+                    c.ks[ph * c.P + r] = scale;
+                    c.vs[ph * c.P + r] = vscale;
                 }
             }
         } else if (in) {
-            __builtin_memcpy(codes, kp + ((size_t)r * DP + at) * ES, E * ES);
+            constexpr int N = E * ES < 16 ? E * ES : 16;
+#pragma unroll
+            for (int i = 0; i < E * ES; i += N) __builtin_memcpy(codes + i, kp + k_place<ES, DP>(r, at * ES + i), N);
             if constexpr (kv_coded<S>) scale = c.ks[ph * c.P + r];
         }
         if (in) {
 #pragma unroll
             for (int i = 0; i < E; ++i) {
-                float z;
-                if constexpr (kv_coded<S>) z = code_value<S, false>((uint8_t)codes[i]) * scale;
-                else {
-                    uint16_t w;
-                    __builtin_memcpy(&w, codes + 2 * i, 2);
-                    if constexpr (S == PK_BF16) z = __uint_as_float((uint32_t)w << 16);
-                    else z = (float)__builtin_bit_cast(_Float16, w);
-                }
+                const float z = kv_coded<S> ? decode<S, false>(codes, i) * scale : decode<S, false>(codes, i);
                 hi[i] = fmaxf(hi[i], z);
                 lo[i] = fminf(lo[i], z);
             }
@@ -173,78 +211,94 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(KvDev c, KvBatch b,
         const float up = code_factor(most, 127.f);
         constexpr float kSlack = 1.f / 1024.f; // of a step: a bound this little beyond a whole number is that number
         int8_t *bc = c.bc + ph * 2 * DP;
+        char bh[E], bl[E];
 #pragma unroll
         for (int i = 0; i < E; ++i) {
-            bc[at + i] = (int8_t)fminf(fmaxf(ceilf(__fsub_rn(__fmul_rn(hi[i], up), kSlack)), -127.f), 127.f);
-            bc[DP + at + i] = (int8_t)fminf(fmaxf(floorf(__fadd_rn(__fmul_rn(lo[i], up), kSlack)), -127.f), 127.f);
+            bh[i] = (char)(int)fminf(fmaxf(ceilf(__fsub_rn(__fmul_rn(hi[i], up), kSlack)), -127.f), 127.f);
+            bl[i] = (char)(int)fminf(fmaxf(floorf(__fadd_rn(__fmul_rn(lo[i], up), kSlack)), -127.f), 127.f);
         }
+        __builtin_memcpy(bc + at, bh, E);
+        __builtin_memcpy(bc + DP + at, bl, E);
         if (tid == 0) c.bs[ph] = most * (1.f / 127.f);
     }
-    // the values' page by channels: 16 bytes a thread where all of them are new, else one by one
-    constexpr int N = 16 / ES;
-    const int pieces = c.P / N;
-    for (int i = tid; i < DP * pieces; i += kThreads) {
-        const int d = i / pieces, r = (i - d * pieces) * N;
-        if (d >= c.D || r + N <= p0 || r >= p1) continue;
-        if (r >= p0 && r + N <= p1) {
-            *reinterpret_cast<u32x4 *>(vp + (size_t)d * pitch + r * ES) = *reinterpret_cast<const u32x4 *>(vt + d * pitch + r * ES);
+    // keys: a piece is part of one token; values: 16 or 8 tokens of a channel, one by one where not all of them are new
+    constexpr int N = 16 / ES, PIECES = DP * ES / 16;
+    for (int i = (p0 >> 2) * 4 * PIECES + tid; i < ((p1 + 3) >> 2) * 4 * PIECES; i += kThreads) {
+        const int tok = i / (4 * PIECES) * 4 + (i & 3);
+        if (tok >= p0 && tok < p1) *reinterpret_cast<u32x4 *>(kp + (size_t)i * 16) = *reinterpret_cast<const u32x4 *>(kimg + i * 16);
+    }
+    for (int i = p0 / N * DP + tid; i < (p1 + N - 1) / N * DP; i += kThreads) {
+        const int tok = i / DP * N, d = i % DP;
+        if (d >= c.D) continue;
+        const char *from = vimg + v_image<ES, DP>(tok, d);
+        if (tok >= p0 && tok + N <= p1) {
+            *reinterpret_cast<u32x4 *>(vp + (size_t)i * 16) = *reinterpret_cast<const u32x4 *>(from);
         } else {
-            for (int j = max(r, p0); j < min(r + N, p1); ++j) {
-                if constexpr (ES == 1) vp[(size_t)d * pitch + j] = vt[d * pitch + j];
-                else reinterpret_cast<uint16_t *>(vp + (size_t)d * pitch)[j] = reinterpret_cast<const uint16_t *>(vt + d * pitch)[j];
+            for (int j = max(tok, p0); j < min(tok + N, p1); ++j) {
+                if constexpr (ES == 1) vp[(size_t)i * 16 + (j - tok)] = from[j - tok];
+                else reinterpret_cast<uint16_t *>(vp + (size_t)i * 16)[j - tok] = reinterpret_cast<const uint16_t *>(from)[j - tok];
             }
         }
     }
 }
 
-// One workgroup: one page of the batch's tokens, one head.  Keys are rows already; values are turned in LDS.
+// One workgroup: one page of the batch's tokens, one head: the page into LDS as it lies in memory, out of it by rows, 16 lanes each.
 template <int S, int T, int DP>
 __global__ __launch_bounds__(kThreads) void kv_read_kernel(KvDev c, KvBatch b, char *kout, char *vout)
 {
-    constexpr int ES = KvBytes<S>::v, TS = T == PK_F32 ? 4 : 2;
-    __shared__ __align__(16) char vt[DP * (kKvMaxPage * ES + 4)];
-    const int s = blockIdx.z, h = blockIdx.y, tid = threadIdx.x;
-    const KvSeq q = kv_seq(b, s, c.P);
-    const int begin = max(q.len - q.m, 0);
-    const int lp = (begin >> c.logP) + (int)blockIdx.x;
-    if (q.m == 0 || ((long long)lp << c.logP) >= q.len) return;
-    const uint32_t page = (uint32_t)b.tables[(size_t)s * b.table_stride + lp];
-    const int base = lp << c.logP;
-    const int p0 = max(begin - base, 0), p1 = min(q.len - base, c.P);
-    const bool there = page < c.n_pages;
-    const size_t ph = (size_t)(there ? page : 0) * c.H + h;
-    const char *kp = c.k + ph * c.P * DP * ES;
-    const char *vp = c.v + ph * DP * c.P * ES;
-    const int vpitch = c.P * ES + 4;
-    for (int i = tid; i < c.D * (c.P * ES / 4); i += kThreads) {
-        const int d = i / (c.P * ES / 4), w = i - d * (c.P * ES / 4);
-        reinterpret_cast<uint32_t *>(vt + d * vpitch)[w] = reinterpret_cast<const uint32_t *>(vp + (size_t)d * c.P * ES)[w];
-    }
+    constexpr int ES = KvBytes<S>::v, TS = T == PK_F32 ? 4 : 2, E = DP / kRowLanes;
+    extern __shared__ __align__(16) char image[];
+    const int h = blockIdx.y, tid = threadIdx.x;
+    KvPage g;
+    if (!kv_page_of(c, b, g)) return;
+    const bool there = g.page < c.n_pages;
+    char *kimg = image, *vimg = image + c.P * DP * ES;
+    const size_t ph = (size_t)(there ? g.page : 0) * c.H + h;
+    const char *kp = c.k + ph * c.P * DP * ES, *vp = c.v + ph * c.P * DP * ES;
+    constexpr int N = 16 / ES, PIECES = DP * ES / 16;
+    for (int i = (g.p0 >> 2) * 4 * PIECES + tid; i < ((g.p1 + 3) >> 2) * 4 * PIECES; i += kThreads)
+        *reinterpret_cast<u32x4 *>(kimg + i * 16) = *reinterpret_cast<const u32x4 *>(kp + (size_t)i * 16);
+    for (int i = g.p0 / N * DP + tid; i < (g.p1 + N - 1) / N * DP; i += kThreads)
+        *reinterpret_cast<u32x4 *>(vimg + v_image<ES, DP>(i / DP * N, i % DP)) = *reinterpret_cast<const u32x4 *>(vp + (size_t)i * 16);
     __syncthreads();
-    auto element = [&](const char *at, auto values) {
-        if constexpr (kv_coded<S>) return code_value<S, decltype(values)::value>((uint8_t)*at);
-        else if constexpr (S == PK_BF16) return __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t *>(at) << 16);
-        else return (float)*reinterpret_cast<const _Float16 *>(at);
-    };
-    const int pairs = c.D / 2;
-    for (int i = tid; i < (p1 - p0) * pairs; i += kThreads) {
-        const int r = p0 + i / pairs, d = (i % pairs) * 2;
-        float ks = 1.f, vs = 1.f;
+    const int sub = tid & (kRowLanes - 1), at = sub * E;
+    if (at >= c.D) return;
+    for (int r = g.p0 + tid / kRowLanes; r < g.p1; r += kRowsAtOnce) {
+        float ks = there ? 1.f : 0.f, vs = ks;
         if constexpr (kv_coded<S>) {
-            ks = c.ks[ph * c.P + r];
-            vs = c.vs[ph * c.P + r];
+            ks = there ? c.ks[ph * c.P + r] : 0.f;
+            vs = there ? c.vs[ph * c.P + r] : 0.f;
         }
-        const size_t t = (size_t)(q.first + (base + r - (q.len - q.m)));
-        const size_t o = ((t * c.H + h) * c.D + d) * TS;
-        float k0 = element(kp + ((size_t)r * DP + d) * ES, std::false_type{}) * ks, k1 = element(kp + ((size_t)r * DP + d + 1) * ES, std::false_type{}) * ks;
-        float v0 = element(vt + d * vpitch + r * ES, std::true_type{}) * vs, v1 = element(vt + (d + 1) * vpitch + r * ES, std::true_type{}) * vs;
-        if (!there) k0 = k1 = v0 = v1 = 0.f;
-        if constexpr (T == PK_F32) {
-            *reinterpret_cast<f32x2 *>(kout + o) = f32x2{k0, k1};
-            *reinterpret_cast<f32x2 *>(vout + o) = f32x2{v0, v1};
-        } else {
-            *reinterpret_cast<uint32_t *>(kout + o) = pack16<T>(k0, k1);
-            *reinterpret_cast<uint32_t *>(vout + o) = pack16<T>(v0, v1);
+        const size_t t = (size_t)(g.q.first + (g.base + r - (g.q.len - g.q.m)));
+        const size_t o = ((t * c.H + h) * c.D + at) * TS;
+        char codes[E * ES];
+        constexpr int M = E * ES < 16 ? E * ES : 16;
+#pragma unroll
+        for (int i = 0; i < E * ES; i += M) __builtin_memcpy(codes + i, kimg + k_place<ES, DP>(r, at * ES + i), M);
+        float x[E], y[E];
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+            x[i] = there ? decode<S, false>(codes, i) : 0.f;
+            y[i] = there ? decode<S, true>(vimg + v_image<ES, DP>(r, at + i), 0) : 0.f;
+            if constexpr (kv_coded<S>) {
+                x[i] *= ks;
+                y[i] *= vs;
+            }
+        }
+        // (D is a multiple of 8: a lane of 4 or 8 elements has all of them or none, one of 16 its first 8 at least)
+#pragma unroll
+        for (int i = 0; i < E; i += 4) {
+            if (at + i >= c.D) continue;
+            if constexpr (T == PK_F32) {
+                *reinterpret_cast<f32x4 *>(kout + o + i * 4) = f32x4{x[i], x[i + 1], x[i + 2], x[i + 3]};
+                *reinterpret_cast<f32x4 *>(vout + o + i * 4) = f32x4{y[i], y[i + 1], y[i + 2], y[i + 3]};
+            } else if constexpr (E == 4) {
+                *reinterpret_cast<u32x2 *>(kout + o) = u32x2{pack16<T>(x[0], x[1]), pack16<T>(x[2], x[3])};
+                *reinterpret_cast<u32x2 *>(vout + o) = u32x2{pack16<T>(y[0], y[1]), pack16<T>(y[2], y[3])};
+            } else if (i % 8 == 0) {
+                *reinterpret_cast<u32x4 *>(kout + o + i * 2) = u32x4{pack16<T>(x[i], x[i + 1]), pack16<T>(x[i + 2], x[i + 3]), pack16<T>(x[i + 4], x[i + 5]), pack16<T>(x[i + 6], x[i + 7])};
+                *reinterpret_cast<u32x4 *>(vout + o + i * 2) = u32x4{pack16<T>(y[i], y[i + 1]), pack16<T>(y[i + 2], y[i + 3]), pack16<T>(y[i + 4], y[i + 5]), pack16<T>(y[i + 6], y[i + 7])};
+            }
         }
     }
 }
@@ -269,14 +323,26 @@ int touched(const KvDev &c, const KvBatch &b)
     return std::min((b.max_new + c.P - 2) / c.P + 1, b.cols);
 }
 
+// A launch with LDS for a page's keys and values.
+template <typename K, typename... A>
+hipError_t with_image(K kernel, size_t lds, dim3 grid, hipStream_t s, A... args)
+{
+    if (lds > (48u << 10)) {
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        if (e != hipSuccess) return e;
+    }
+    kernel<<<grid, kThreads, lds, s>>>(args...);
+    return hipGetLastError();
+}
+
 template <int S, int T>
 hipError_t append_dp(const KvDev &c, int dp, const KvBatch &b, const KvRows &k, const KvRows &v, hipStream_t s)
 {
+    constexpr int ES = KvBytes<S>::v;
     const dim3 grid(touched(c, b), c.H, b.n_seqs);
-    if (dp == 64) kv_append_kernel<S, T, 64><<<grid, kThreads, 0, s>>>(c, b, k, v);
-    else if (dp == 128) kv_append_kernel<S, T, 128><<<grid, kThreads, 0, s>>>(c, b, k, v);
-    else kv_append_kernel<S, T, 256><<<grid, kThreads, 0, s>>>(c, b, k, v);
-    return hipGetLastError();
+    if (dp == 64) return with_image(kv_append_kernel<S, T, 64>, image_bytes<ES, 64>(c.P), grid, s, c, b, k, v);
+    if (dp == 128) return with_image(kv_append_kernel<S, T, 128>, image_bytes<ES, 128>(c.P), grid, s, c, b, k, v);
+    return with_image(kv_append_kernel<S, T, 256>, image_bytes<ES, 256>(c.P), grid, s, c, b, k, v);
 }
 
 template <int S>
@@ -290,11 +356,11 @@ hipError_t append_s(const KvDev &c, int dp, const KvBatch &b, const KvRows &k, c
 template <int S, int T>
 hipError_t read_dp(const KvDev &c, int dp, const KvBatch &b, char *k, char *v, hipStream_t s)
 {
+    constexpr int ES = KvBytes<S>::v;
     const dim3 grid(touched(c, b), c.H, b.n_seqs);
-    if (dp == 64) kv_read_kernel<S, T, 64><<<grid, kThreads, 0, s>>>(c, b, k, v);
-    else if (dp == 128) kv_read_kernel<S, T, 128><<<grid, kThreads, 0, s>>>(c, b, k, v);
-    else kv_read_kernel<S, T, 256><<<grid, kThreads, 0, s>>>(c, b, k, v);
-    return hipGetLastError();
+    if (dp == 64) return with_image(kv_read_kernel<S, T, 64>, image_bytes<ES, 64>(c.P), grid, s, c, b, k, v);
+    if (dp == 128) return with_image(kv_read_kernel<S, T, 128>, image_bytes<ES, 128>(c.P), grid, s, c, b, k, v);
+    return with_image(kv_read_kernel<S, T, 256>, image_bytes<ES, 256>(c.P), grid, s, c, b, k, v);
 }
 
 template <int S>

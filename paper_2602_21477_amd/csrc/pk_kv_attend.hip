@@ -128,7 +128,7 @@ __device__ __forceinline__ void kv_write_row(const KvAttend &a, int h, int tok, 
 // blockIdx: row tile of a sequence (sparse: of a token), part of its keys, head; the heads fastest, so that each of the chip's eight
 // parts reads few of them.
 template <int S, int T, int DP, bool SPARSE>
-__global__ __launch_bounds__(256) void kv_rows_kernel(KvAttend a)
+__global__ __launch_bounds__(256, DP * KvBytes<S>::v > 128 ? 1 : 2) void kv_rows_kernel(KvAttend a)
 {
     constexpr int ES = KvBytes<S>::v;
     using Sc = KvScaling<S, T>;
@@ -209,11 +209,11 @@ __global__ __launch_bounds__(256) void kv_rows_kernel(KvAttend a)
     u32x4 kw[4][KC];
     auto ask_k = [&](const KvRun &r) __attribute__((always_inline)) {
         const size_t ph = (size_t)(r.page < c.n_pages ? r.page : 0) * c.H + h;
-        const char *kr = c.k + (ph * P + (r.base >= 0 ? r.base & (P - 1) : 0) + (col & 3)) * DP * ES + g * 16;
+        const char *kr = c.k + (ph * P + (r.base >= 0 ? r.base & (P - 1) : 0)) * DP * ES + g * 64 + (col & 3) * 16;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int k = 0; k < KC; ++k) kw[i][k] = *reinterpret_cast<const u32x4 *>(kr + i * 4 * DP * ES + k * 64);
+            for (int k = 0; k < KC; ++k) kw[i][k] = *reinterpret_cast<const u32x4 *>(kr + i * DP * ES * 4 + k * 256);
     };
     const int tw = t0 + wave;
     int kblock = 0, vblock = 0; // (sparse) of the round after the next
@@ -278,11 +278,11 @@ __global__ __launch_bounds__(256) void kv_rows_kernel(KvAttend a)
                     vsc[i] = *reinterpret_cast<const f32x4 *>(vs + 4 * i);
                 }
             }
-            const char *v = c.v + ((vph * DP + col) * P + voff) * ES;
+            const char *v = c.v + (vph * P + voff) * DP * ES + col * 16;
 #pragma unroll
             for (int d = 0; d < DT; ++d)
 #pragma unroll
-                for (int k = 0; k < VC; ++k) vw[d][k] = *reinterpret_cast<const u32x4 *>(v + (size_t)d * 16 * P * ES + k * 16);
+                for (int k = 0; k < VC; ++k) vw[d][k] = *reinterpret_cast<const u32x4 *>(v + d * 256 + k * DP * 16);
         }
         __builtin_amdgcn_sched_barrier(0);
 
@@ -520,11 +520,12 @@ __device__ __forceinline__ KvUnit kv_unit(const KvAttend &a, int unit)
 }
 
 // Where 16-byte piece `piece` of row `row` lies in a tile in LDS: rows of CH pieces, moved about so that 16 lanes that read one piece
-// of 16 neighbouring rows meet all banks.  (Piece p ^ x lies where p does, exclusive-or x.)
+// of 16 neighbouring rows, or write four pieces of four, meet all banks.  (Piece p ^ x lies where p does, exclusive-or x.)
 template <int CH>
 __device__ __forceinline__ int lds_piece(int row, int piece)
 {
-    return row * CH + (piece ^ (CH == 8 ? (row >> 1) & 7 : row & 15));
+    const int x = CH == 8 ? (row >> 1 & 1) << 2 | (row >> 2 & 3) : (row & 3) << 2 | (row >> 2 & 3);
+    return row * CH + (piece ^ x);
 }
 
 // The largest of a number's values in lanes l and l ^ 32.
@@ -567,7 +568,11 @@ struct KvTiles {
     static constexpr int PIECES = kKvTile * DP * ES / 16; // 16-byte pieces of a tile of K, and of one of V
     static constexpr int KP = (PIECES + NT - 1) / NT;     // of a thread
     static constexpr int KR = DP * ES / 16;               // pieces of a row of K
-    static constexpr int VR = kKvTile * ES / 16;          // pieces of a row of V
+    // piece p of a tile in memory: of K piece k_piece of token k_tok; of V channel v_row, tokens from v_tok on
+    static __device__ __forceinline__ int k_tok(int p) { return p / (4 * KR) * 4 + (p & 3); }
+    static __device__ __forceinline__ int k_piece(int p) { return p / 4 % KR; }
+    static __device__ __forceinline__ int v_row(int p) { return p % DP; }
+    static __device__ __forceinline__ int v_tok(int p) { return p / DP * (16 / ES); }
     static constexpr int PG = ONE ? 1 : KP;
     static_assert(PIECES % NT == 0 || PIECES < NT, "");
     struct Lds {
@@ -610,8 +615,8 @@ struct KvTiles {
 #pragma unroll
             for (int i = 0; i < KP; ++i) {
                 const int p = tid + i * NT;
-                kpage[i] = page_of(kb + p / KR);
-                vpage[i] = page_of(vb + (p % VR) * (16 / ES));
+                kpage[i] = page_of(kb + k_tok(p));
+                vpage[i] = page_of(vb + v_tok(p));
             }
             spage = page_of(kb + (tid & 63));
         }
@@ -625,13 +630,13 @@ struct KvTiles {
             // (taken here, not where they were asked for: that would be a wait for all that is on its way)
             asm volatile("" : "+v"(kpage[0]), "+v"(vpage[0]));
             const uint32_t kp = (uint32_t)same((int)kpage[0]), vp = (uint32_t)same((int)vpage[0]);
-            const char *kr = k + (place(kp) * P + (kb & (P - 1))) * DP * ES, *vr = v + (place(vp) * DP * P + (vb & (P - 1))) * ES;
+            const char *kr = k + (place(kp) * P + (kb & (P - 1))) * DP * ES, *vr = v + (place(vp) * P + (vb & (P - 1))) * DP * ES;
             if (mine) {
 #pragma unroll
                 for (int i = 0; i < KP; ++i) {
                     const int p = tid + i * NT;
                     kw[i] = *reinterpret_cast<const u32x4 *>(kr + (uint32_t)(p * 16));
-                    vw[i] = *reinterpret_cast<const u32x4 *>(vr + (uint32_t)((p / VR) * P * ES + (p % VR) * 16));
+                    vw[i] = *reinterpret_cast<const u32x4 *>(vr + (uint32_t)(p * 16));
                 }
             }
             in_next = kp < n_pages ? 15u : 0u;
@@ -651,8 +656,10 @@ struct KvTiles {
             for (int i = 0; i < KP; ++i) {
                 const int p = tid + i * NT;
                 if (mine) {
-                    kw[i] = *reinterpret_cast<const u32x4 *>(k + ((place(kpage[i]) * P + ((kb + p / KR) & (P - 1))) * DP) * ES + (p % KR) * 16);
-                    vw[i] = *reinterpret_cast<const u32x4 *>(v + ((place(vpage[i]) * DP + p / VR) * P + ((vb + (p % VR) * (16 / ES)) & (P - 1))) * ES);
+                    // (a run of 16 tokens lies in one page)
+                    constexpr int RUN = 16 * DP * ES / 16; // pieces of a run
+                    kw[i] = *reinterpret_cast<const u32x4 *>(k + (place(kpage[i]) * P + ((kb + p / RUN * 16) & (P - 1))) * DP * ES + (p % RUN) * 16);
+                    vw[i] = *reinterpret_cast<const u32x4 *>(v + (place(vpage[i]) * P + ((vb + p / RUN * 16) & (P - 1))) * DP * ES + (p % RUN) * 16);
                 }
                 v_in |= (vpage[i] < n_pages ? 1u : 0u) << i;
             }
@@ -675,7 +682,7 @@ struct KvTiles {
         if (vb >= 0 && vb + kKvTile <= len && v_there) return;
 #pragma unroll
         for (int i = 0; i < KP; ++i) {
-            const int p = threadIdx.x + i * NT, held = vb >= 0 && (v_in >> i & 1) ? len - (vb + (p % VR) * (16 / ES)) : 0;
+            const int p = threadIdx.x + i * NT, held = vb >= 0 && (v_in >> i & 1) ? len - (vb + v_tok(p)) : 0;
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
                 uint32_t keep = 0;
@@ -693,17 +700,18 @@ struct KvTiles {
 #pragma unroll
             for (int i = 0; i < KP; ++i) {
                 const int p = tid + i * NT;
+                const int row = k_tok(p), piece = k_piece(p), vrow = v_row(p), vpiece = v_tok(p) / 8;
                 if constexpr (CODED) {
                     u32x4 f0, f1;
                     operands<S, T, false>(kw[i], f0, f1);
-                    lds.k[kb][lds_piece<CH>(p / KR, (p % KR) * 2)] = f0;
-                    lds.k[kb][lds_piece<CH>(p / KR, (p % KR) * 2 + 1)] = f1;
+                    lds.k[kb][lds_piece<CH>(row, piece * 2)] = f0;
+                    lds.k[kb][lds_piece<CH>(row, piece * 2 + 1)] = f1;
                     operands<S, T, true>(vw[i], f0, f1);
-                    lds.v[vb][lds_piece<8>(p / VR, (p % VR) * 2)] = f0;
-                    lds.v[vb][lds_piece<8>(p / VR, (p % VR) * 2 + 1)] = f1;
+                    lds.v[vb][lds_piece<8>(vrow, vpiece)] = f0;
+                    lds.v[vb][lds_piece<8>(vrow, vpiece + 1)] = f1;
                 } else {
-                    lds.k[kb][lds_piece<CH>(p / KR, p % KR)] = kw[i];
-                    lds.v[vb][lds_piece<8>(p / VR, p % VR)] = vw[i];
+                    lds.k[kb][lds_piece<CH>(row, piece)] = kw[i];
+                    lds.v[vb][lds_piece<8>(vrow, vpiece)] = vw[i];
                 }
             }
         }
