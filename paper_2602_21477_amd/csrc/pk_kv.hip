@@ -418,7 +418,7 @@ struct pk_kv {
 namespace {
 
 constexpr uint64_t kKvMagic = 0x70616e63616b7631ull;
-constexpr int64_t kMaxUnits = 1 << 22; // row tiles of a launch: its grid has 32 bits for their threads
+constexpr int64_t kMaxUnits = 1 << 22; // workgroups of a launch before they are cut into parts: a grid has 32 bits for its threads
 constexpr int kMaxHeads = 1024; // key/value heads of a cache, and query heads of one of them
 
 size_t up256(size_t v) { return (v + 255) / 256 * 256; }
@@ -516,9 +516,8 @@ int attend(pk_kv *kv, const pk_kv_batch *batch, const pk_rows *q, int32_t n_q_he
     a.out = static_cast<char *>(out);
     a.lse = lse;
     a.num_cu = kv->num_cu;
-    // (more workgroups than a grid has threads for)
-    if ((blocks ? (int64_t)a.b.n_tokens : (int64_t)a.b.n_seqs) * (((blocks ? a.G : (int64_t)a.b.max_new * a.G) + 15) / 16) * kv->cfg.n_heads > kMaxUnits)
-        return PK_ERR_UNSUPPORTED;
+    const int64_t H = kv->cfg.n_heads, units = blocks ? (int64_t)a.b.n_tokens * ((a.G + 15) / 16) : std::max<int64_t>(a.b.n_seqs * 4, (int64_t)a.b.n_tokens * a.G / 128 + a.b.n_seqs);
+    if (units * H > kMaxUnits) return PK_ERR_UNSUPPORTED;
     a.part = reinterpret_cast<float *>(kv->ws);
     a.part_floats = kKvPartFloats;
     a.part_ml = a.part + kKvPartFloats;
@@ -650,7 +649,8 @@ int pk_kv_select(pk_kv *kv, const pk_kv_batch *batch, const pk_rows *q, int32_t 
     rc = take_queries(kv, q, n_q_heads, &qr, &G);
     if (rc != PK_OK) return rc;
     if (!out_blocks) return PK_ERR_INVALID_ARG;
-    return launch_kv_select(kv->dev, kv->dp, b, qr, q->dtype, G, n_blocks, sink, local, out_blocks, static_cast<hipStream_t>(stream)) == hipSuccess
+    if ((int64_t)b.n_seqs * b.max_new * kv->cfg.n_heads > 4 * kMaxUnits) return PK_ERR_UNSUPPORTED;
+    return launch_kv_select(kv->dev, kv->dp, b, qr, q->dtype, G, n_blocks, sink, local, kv->num_cu, out_blocks, static_cast<hipStream_t>(stream)) == hipSuccess
                ? PK_OK
                : PK_ERR_HIP;
 }

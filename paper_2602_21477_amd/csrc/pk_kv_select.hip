@@ -1,48 +1,66 @@
 // Which blocks of a sequence a query attends to: the ones whose bounds promise the largest scores.
+#include <algorithm>
+
 #include "pk_kv.h"
 
 namespace pk {
 namespace {
 
-constexpr int kThreads = 256;
-
-// The scores' order as whole numbers: larger is better; 0 is for blocks that cannot be chosen.
+// The scores' order as whole numbers: larger is better; 0 is for blocks that cannot be chosen, ~0 for those that are in any case.
+constexpr uint32_t kAlways = 0xffffffffu;
 __device__ __forceinline__ uint32_t score_key(float v)
 {
     const uint32_t b = __float_as_uint(v);
     return max(b ^ ((b >> 31) ? 0xffffffffu : 0x80000000u), 1u);
 }
 
-// One workgroup: one token, one key/value head.
-//   U[block, head] = sum_c max(q_c hi_c, q_c lo_c) = q+ hi + q- lo, whole numbers: int8 products of the rows [hi, lo] of the bounds with
-//   [q+, q-] of the group's queries, 16 blocks by 16 heads at a time
-//   score[block] = max over the group's heads of U scale_q, times the bounds' scale
-// No sum of it is rounded, so the choice is the same whatever computes it.  The keys of the scores stay in LDS; the n-th largest is
-// found by its four bytes, one histogram each, and what is chosen comes out in ascending order.
-template <int T, int DP>
-__global__ __launch_bounds__(kThreads) void kv_select_kernel(KvDev c, KvBatch b, KvRows qin, int G, int n, int sink, int local, int32_t *out)
-{
-    extern __shared__ uint32_t keys[];
-    __shared__ uint32_t hist[256];
-    __shared__ uint32_t found[3], waves[4];
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 15, g = lane >> 4;
-    const int t = blockIdx.x, h = blockIdx.y;
-    const int seq = kv_seq_of(b, t);
-    const KvSeq sq = kv_seq(b, seq, c.P);
-    const int i = t - sq.first, pos = sq.len - sq.m + i;
-    int32_t *o = out + ((size_t)t * c.H + h) * n;
-    const bool none = i < 0 || i >= sq.m || pos < 0;
-    const int mine = none ? -1 : pos >> c.logP, nb = mine + 1;
-    const int32_t *table = b.tables + (size_t)seq * b.table_stride;
-    for (int i0 = tid; i0 < nb; i0 += kThreads) keys[i0] = 0;
-    __syncthreads();
+struct KvSelect {
+    KvDev c;
+    KvBatch b;
+    KvRows q;
+    int32_t G, n, sink, local;
+    int32_t gp;     // columns of a token: its query heads, a power of two of 16 at most
+    int32_t tokens; // of a workgroup: 16 / gp at most, a power of two
+    int32_t groups; // of tokens, of one sequence
+    int32_t room;   // keys of a token in LDS
+    int32_t *out;
+};
 
+// One workgroup: a few tokens of one sequence, one key/value head.
+//   U[block, head] = sum_c max(q_c hi_c, q_c lo_c) = q+ hi + q- lo, whole numbers: int8 products of the rows [hi, lo] of 16 blocks' bounds with
+//   [q+, q-] of 16 columns, the tokens' heads side by side
+//   score[block] = max over a token's heads of U scale_q, times the bounds' scale
+// No sum of it is rounded, so the choice is the same whatever computes it.  A load takes 64 bytes of a row by four neighbouring lanes and goes to
+// the lanes that the product wants by way of LDS.  The keys of the scores stay there; a token's n-th largest is found by its
+// bytes, from the first one in which its keys differ, one histogram each, by the waves that have the token (all of them, where it is the only one); each
+// of these then has a stretch of the blocks, and what is chosen comes out in ascending order.
+// Bound by reading the bounds where there are few tokens (16 waves then), by the steps of the choice where there are many.
+template <int T, int DP, int NW>
+__global__ __launch_bounds__(NW * 64) void kv_select_kernel(KvSelect a)
+{
     constexpr int KS = DP / 64; // products over a half of a row of bounds
-    for (int gt = 0; gt < G; gt += 16) {
-        // the queries' codes: lane (head, g) has channels 64 k + 16 g .. + 15
+    extern __shared__ uint32_t keys[];
+    __shared__ __align__(16) u32x4 turn[NW][64];
+    __shared__ uint32_t hist[NW][256];
+    __shared__ uint32_t counts[NW][3], found[NW][2];
+    const KvDev c = a.c;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 15, g = lane >> 4;
+    const int h = blockIdx.x % c.H, unit = blockIdx.x / c.H, seq = unit / a.groups, first = (unit - seq * a.groups) * a.tokens;
+    const KvSeq sq = kv_seq(a.b, seq, c.P);
+    if (first >= sq.m) return;
+    const int32_t *table = a.b.tables + (size_t)seq * a.b.table_stride;
+    const int start = sq.len - sq.m;
+    const int last_pos = start + min(first + a.tokens, sq.m) - 1, nb = last_pos < 0 ? 0 : (last_pos >> c.logP) + 1; // blocks of its last token
+    const int tk = col / a.gp, member0 = col % a.gp;
+    const int pos = start + first + tk, mine = pos >> c.logP; // (pos < 0: nothing is seen)
+    const bool token_in = tk < a.tokens && first + tk < sq.m;
+
+    for (int gt = 0; gt < a.G; gt += a.gp) {
+        // the queries' codes: lane (column, g) has channels 64 k + 16 g .. + 15
         float x[KS][16], most = 0.f;
-        const bool there = gt + col < G;
-        const char *qrow = qin.data + ((size_t)t * qin.token_stride + (size_t)(h * G + min(gt + col, G - 1)) * qin.head_stride) * 2;
+        const bool in = token_in && gt + member0 < a.G;
+        const int tok = sq.first + min(first + tk, sq.m - 1);
+        const char *qrow = a.q.data + ((size_t)tok * a.q.token_stride + (size_t)(h * a.G + min(gt + member0, a.G - 1)) * a.q.head_stride) * 2;
 #pragma unroll
         for (int k = 0; k < KS; ++k)
 #pragma unroll
@@ -51,7 +69,7 @@ __global__ __launch_bounds__(kThreads) void kv_select_kernel(KvDev c, KvBatch b,
 #pragma unroll
                 for (int j = 0; j < 8; ++j) y[j] = 0.f;
                 const int at = k * 64 + g * 16 + e;
-                if (there && at < c.D) load_eight<T>(y, qrow, at);
+                if (in && at < c.D) load_eight<T>(y, qrow, at);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     x[k][e + j] = y[j];
@@ -76,115 +94,225 @@ __global__ __launch_bounds__(kThreads) void kv_select_kernel(KvDev c, KvBatch b,
                 qp[k][w] = (int)p;
                 qm[k][w] = (int)m;
             }
-        for (int b0 = wave * 16; b0 < nb; b0 += 64) {
-            const int blk = min(b0 + col, nb - 1);
-            const uint32_t page = (uint32_t)table[blk];
-            const size_t ph = (size_t)(page < c.n_pages ? page : 0) * c.H + h;
-            const int8_t *row = c.bc + ph * 2 * DP + g * 16;
+        const int load_row = lane >> 2, load_piece = lane & 3;
+        auto page_at = [&](int b0, int row) __attribute__((always_inline)) -> uint32_t { return (uint32_t)table[min(b0 + row, nb - 1)]; };
+        uint32_t lpage = 0, cpage = 0;
+        if (wave * 16 < nb) {
+            lpage = page_at(wave * 16, load_row);
+            cpage = page_at(wave * 16, col);
+        }
+        for (int b0 = wave * 16; b0 < nb; b0 += NW * 16) {
+            const size_t lph = (size_t)(lpage < c.n_pages ? lpage : 0) * c.H + h;
+            const int8_t *row = c.bc + lph * 2 * DP + load_piece * 16;
+            u32x4 w[2 * KS];
+#pragma unroll
+            for (int k = 0; k < 2 * KS; ++k) w[k] = *reinterpret_cast<const u32x4 *>(row + k * 64);
+            const uint32_t page = cpage;
+            const float bs = c.bs[(size_t)(page < c.n_pages ? page : 0) * c.H + h];
+            if (b0 + NW * 16 < nb) {
+                lpage = page_at(b0 + NW * 16, load_row);
+                cpage = page_at(b0 + NW * 16, col);
+            }
             i32x4 acc = {0, 0, 0, 0};
 #pragma unroll
-            for (int k = 0; k < KS; ++k) {
-                acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(*reinterpret_cast<const i32x4 *>(row + k * 64), qp[k], acc, 0, 0, 0);
-                acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(*reinterpret_cast<const i32x4 *>(row + DP + k * 64), qm[k], acc, 0, 0, 0);
+            for (int k = 0; k < 2 * KS; ++k) {
+                // row r, piece p lies at 4 r + (p ^ (r / 4)): a quarter of a wave reads 16 rows from banks of their own, 2 at a time
+                turn[wave][load_row * 4 + (load_piece ^ (load_row >> 2))] = w[k];
+                __builtin_amdgcn_wave_barrier();
+                const i32x4 f = __builtin_bit_cast(i32x4, turn[wave][col * 4 + (g ^ (col >> 2))]);
+                __builtin_amdgcn_wave_barrier();
+                acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(f, k < KS ? qp[k % KS] : qm[k % KS], acc, 0, 0, 0);
             }
-            const float bs = c.bs[ph];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                float v = there ? (float)acc[j] * qscale : -INFINITY;
-#pragma unroll
-                for (int d = 1; d < 16; d *= 2) v = fmaxf(v, __shfl_xor(v, d));
+                float v = in ? (float)acc[j] * qscale : -INFINITY;
+                for (int d = 1; d < a.gp; d *= 2) v = fmaxf(v, __shfl_xor(v, d));
                 const int at = b0 + g * 4 + j; // its scale and page are with the lane of that column
                 const float scale = __shfl(bs, g * 4 + j);
                 const uint32_t pg = (uint32_t)__shfl((int)page, g * 4 + j);
-                if (col == 0 && at < nb && pg < c.n_pages) {
-                    const uint32_t key = at < sink || at > mine - local ? 0xffffffffu : score_key(v * scale + 0.f); // (no zero of a sign)
-                    keys[at] = max(keys[at], key);
+                if (token_in && member0 == 0 && at < nb) {
+                    uint32_t key = 0;
+                    if (pos >= 0 && at <= mine && pg < c.n_pages)
+                        key = at < a.sink || at > mine - a.local ? kAlways : score_key(v * scale + 0.f); // (no zero of a sign)
+                    uint32_t *k = keys + tk * a.room + at;
+                    *k = gt == 0 ? key : max(*k, key);
                 }
             }
         }
     }
     __syncthreads();
 
-    // the n-th largest key, byte by byte; `need` of the keys equal to it are chosen, the lowest blocks first
-    uint32_t prefix = 0, mask = 0, need = (uint32_t)n;
-    bool all = false;
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        hist[tid] = 0;
-        __syncthreads();
-        for (int i0 = tid; i0 < nb; i0 += kThreads)
-            if (keys[i0] && (keys[i0] & mask) == prefix) atomicAdd(&hist[(keys[i0] >> shift) & 255u], 1u);
-        __syncthreads();
-        // how many lie in bins above this thread's
-        uint32_t own = hist[tid], above = own;
+    // ---- the choice: waves `team` to `team + size - 1` have a token (more tokens than waves: several in turn)
+    const int size = max(NW / a.tokens, 1), turns = max(a.tokens / NW, 1);
+    const int team = wave / size, rank = wave - team * size, members = size * 64, me = rank * 64 + lane;
+    for (int u = 0; u < turns; ++u) {
+        const int t = team + u * NW; // (u > 0 only where a wave has tokens of its own)
+        const bool have = t < a.tokens && first + t < sq.m;
+        const uint32_t *k = keys + (have ? t : 0) * a.room;
+        const int count = have ? nb : 0;
+        // how many there are, how many of them in any case, and the first bit in which the others differ
+        uint32_t always = 0, others = 0, low = 0xffffffffu, high = 0;
+        for (int i = me; i < count; i += members) {
+            const uint32_t key = k[i];
+            if (key == kAlways) ++always;
+            else if (key) {
+                ++others;
+                low = min(low, key);
+                high = max(high, key);
+            }
+        }
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) {
-            const uint32_t v = (uint32_t)__shfl_down((int)above, d);
-            if (lane + d < 64) above += v;
+            always += (uint32_t)__shfl_xor((int)always, d);
+            others += (uint32_t)__shfl_xor((int)others, d);
+            low = min(low, (uint32_t)__shfl_xor((int)low, d));
+            high = max(high, (uint32_t)__shfl_xor((int)high, d));
         }
-        if (lane == 0) waves[wave] = above;
-        if (tid == 0) found[0] = 0xffffffffu;
-        __syncthreads();
-        for (int w = wave + 1; w < 4; ++w) above += waves[w];
-        above -= own;
-        if (above < need && above + own >= need) {
-            found[0] = (uint32_t)tid;
-            found[1] = need - above;
+        if (size > 1) {
+            if (lane == 0) counts[wave][0] = always, counts[wave][1] = others, found[wave][0] = low, found[wave][1] = high;
+            __syncthreads();
+            always = others = high = 0, low = 0xffffffffu;
+            for (int w = 0; w < size; ++w) {
+                always += counts[team * size + w][0];
+                others += counts[team * size + w][1];
+                low = min(low, found[team * size + w][0]);
+                high = max(high, found[team * size + w][1]);
+            }
+            __syncthreads();
         }
-        __syncthreads();
-        if (found[0] == 0xffffffffu) { // fewer than n in all (only in the first round)
-            all = true;
-            break;
+        uint32_t need = (uint32_t)a.n > always ? (uint32_t)a.n - always : 0;
+        // of the keys that are not taken in any case: all where there are no more than that, else those above `bound` and `need` of those equal to it
+        const bool all = others <= need, none = need == 0;
+        int bits = all || none || low == high ? 0 : 32 - __clz((int)(low ^ high));
+        uint32_t mask = bits == 32 ? 0u : ~0u << bits, bound = none ? kAlways : high & mask;
+        uint32_t *hs = hist[team * size];
+        // (every wave of the workgroup goes through four rounds where waves share a token, as they meet in each)
+        for (int round = 0; round < 4; ++round) {
+            if (size == 1 && bits <= 0) break;
+            const int shift = max(bits - 8, 0), width = bits - shift;
+            for (int i = me; i < 256; i += members) hs[i] = 0;
+            if (size > 1) __syncthreads();
+            else __builtin_amdgcn_wave_barrier();
+            if (bits > 0)
+                for (int i = me; i < count; i += members) {
+                    const uint32_t key = k[i];
+                    if (key && key != kAlways && (key & mask) == bound) atomicAdd(&hs[(key >> shift) & ((1u << width) - 1)], 1u);
+                }
+            if (size > 1) __syncthreads();
+            else __builtin_amdgcn_wave_barrier();
+            // how many lie in bins above; a lane has four bins
+            uint32_t own[4], sum = 0;
+#pragma unroll
+            for (int j = 3; j >= 0; --j) {
+                own[j] = hs[lane * 4 + j];
+                sum += own[j];
+            }
+            uint32_t above = sum;
+#pragma unroll
+            for (int d = 1; d < 64; d *= 2) {
+                const uint32_t v = (uint32_t)__shfl_down((int)above, d);
+                if (lane + d < 64) above += v;
+            }
+            above -= sum;
+            int bin = -1;
+            uint32_t left = 0;
+#pragma unroll
+            for (int j = 3; j >= 0; --j) {
+                if (bin < 0 && above < need && above + own[j] >= need) {
+                    bin = lane * 4 + j;
+                    left = need - above;
+                }
+                above += own[j];
+            }
+            const unsigned long long has = __ballot(bin >= 0);
+            if (bits > 0 && has) {
+                const int l = __ffsll(has) - 1;
+                bound |= (uint32_t)__shfl(bin, l) << shift;
+                need = (uint32_t)__shfl((int)left, l);
+                mask |= ((1u << width) - 1) << shift;
+                bits = shift;
+            }
+            if (size > 1) __syncthreads();
         }
-        prefix |= found[0] << shift;
-        mask |= 255u << shift;
-        need = found[1];
-        __syncthreads();
+        // each wave has a stretch of the blocks: what it takes before the equal ones, the equal ones, and where they go
+        const int stretch = (((count + size - 1) / size) + 63) / 64 * 64, i0 = rank * stretch, i1 = min(i0 + stretch, count);
+        uint32_t over = 0, equal = 0;
+        for (int i = i0; i < i1; i += 64) {
+            const uint32_t key = i + lane < i1 ? k[i + lane] : 0;
+            over += (uint32_t)__popcll(__ballot(key == kAlways || (key && (all || key > bound))));
+            equal += (uint32_t)__popcll(__ballot(key && key != kAlways && !all && key == bound));
+        }
+        uint32_t equal_before = 0, place = 0;
+        if (size > 1) {
+            if (lane == 0) counts[wave][0] = over, counts[wave][1] = equal;
+            __syncthreads();
+            for (int w = 0; w < size; ++w) {
+                const uint32_t o = counts[team * size + w][0], e = counts[team * size + w][1];
+                if (w < rank) {
+                    place += o + (equal_before < need ? min(e, need - equal_before) : 0);
+                    equal_before += e;
+                }
+            }
+        }
+        int32_t *o = a.out + ((size_t)(sq.first + min(first + t, sq.m - 1)) * c.H + h) * a.n;
+        const unsigned long long below = (1ull << lane) - 1;
+        for (int i = i0; i < i1; i += 64) {
+            const uint32_t key = i + lane < i1 ? k[i + lane] : 0;
+            const bool is = key && key != kAlways && !all && key == bound;
+            const unsigned long long eq = __ballot(is);
+            const bool take = key == kAlways || (key && !is && (all || key > bound)) || (is && equal_before + (uint32_t)__popcll(eq & below) < need);
+            const unsigned long long tk2 = __ballot(take);
+            const uint32_t to = place + (uint32_t)__popcll(tk2 & below);
+            if (take && to < (uint32_t)a.n) o[to] = i + lane;
+            place += (uint32_t)__popcll(tk2);
+            equal_before += (uint32_t)__popcll(eq);
+        }
+        // the last wave knows how many there are in all
+        if (have && rank == size - 1)
+            for (int i = (int)place + lane; i < a.n; i += 64) o[i] = -1;
+        if (size > 1) __syncthreads();
     }
-    uint32_t done = 0, equal = 0;
-    for (int i0 = 0; i0 < nb; i0 += kThreads) {
-        const uint32_t key = i0 + tid < nb ? keys[i0 + tid] : 0;
-        const bool is = key && !all && key == prefix, over = key && (all || key > prefix);
-        // ranks among the equal ones, then among the chosen ones
-        const unsigned long long eq = __ballot(is);
-        if (lane == 0) waves[wave] = (uint32_t)__popcll(eq);
-        __syncthreads();
-        uint32_t rank = equal + (uint32_t)__popcll(eq & ((1ull << lane) - 1));
-        for (int w = 0; w < wave; ++w) rank += waves[w];
-        equal += waves[0] + waves[1] + waves[2] + waves[3];
-        const bool take = over || (is && rank < need);
-        const unsigned long long tk = __ballot(take);
-        __syncthreads();
-        if (lane == 0) waves[wave] = (uint32_t)__popcll(tk);
-        __syncthreads();
-        uint32_t place = done + (uint32_t)__popcll(tk & ((1ull << lane) - 1));
-        for (int w = 0; w < wave; ++w) place += waves[w];
-        done += waves[0] + waves[1] + waves[2] + waves[3];
-        if (take && place < (uint32_t)n) o[place] = i0 + tid;
-        __syncthreads();
+}
+
+template <int T, int DP, int NW>
+hipError_t run(const KvSelect &a, unsigned grid, size_t lds, hipStream_t s)
+{
+    if (lds > (32u << 10)) {
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&kv_select_kernel<T, DP, NW>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        if (e != hipSuccess) return e;
     }
-    for (int i0 = (int)done + tid; i0 < n; i0 += kThreads) o[i0] = -1;
+    kv_select_kernel<T, DP, NW><<<dim3(grid), NW * 64, lds, s>>>(a);
+    return hipGetLastError();
 }
 
 template <int T, int DP>
-hipError_t run(const KvDev &c, const KvBatch &b, const KvRows &q, int G, int n, int sink, int local, int32_t *out, hipStream_t s)
+hipError_t run_waves(KvSelect a, int num_cu, hipStream_t s)
 {
-    const int64_t keys = ((int64_t)b.max_len + c.P - 1) / c.P;
-    const size_t lds = (size_t)(keys < b.cols ? keys : b.cols) * sizeof(uint32_t);
-    if (lds > (48u << 10)) {
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&kv_select_kernel<T, DP>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-        if (e != hipSuccess) return e;
-    }
-    kv_select_kernel<T, DP><<<dim3((unsigned)b.n_tokens, c.H), kThreads, lds, s>>>(c, b, q, G, n, sink, local, out);
-    return hipGetLastError();
+    const int64_t most = ((int64_t)a.b.max_len + a.c.P - 1) / a.c.P;
+    a.room = (int32_t)std::max<int64_t>(std::min<int64_t>(most, a.b.cols), 1);
+    a.gp = 1;
+    while (a.gp < a.G && a.gp < 16) a.gp *= 2;
+    // as many tokens as 16 columns have, as a sequence has, and as LDS has room for the keys of (two workgroups a CU at least, unless one
+    // token alone takes more)
+    a.tokens = 16 / a.gp;
+    while (a.tokens > 1 && (a.tokens / 2 >= a.b.max_new || (int64_t)a.tokens * a.room * 4 > (48 << 10))) a.tokens /= 2;
+    a.groups = (a.b.max_new + a.tokens - 1) / a.tokens;
+    const int64_t grid = (int64_t)a.b.n_seqs * a.groups * a.c.H;
+    const size_t lds = (size_t)a.tokens * a.room * 4;
+    // few workgroups: 16 waves each, while LDS has room for what they need beside the keys
+    if (grid <= 2 * num_cu && lds <= (120u << 10)) return run<T, DP, 16>(a, (unsigned)grid, lds, s);
+    return run<T, DP, 4>(a, (unsigned)grid, lds, s);
 }
 
 } // namespace
 
 hipError_t launch_kv_select(const KvDev &c, int dp, const KvBatch &b, const KvRows &q, int dtype, int G, int n_blocks, int sink, int local,
-                            int32_t *out, hipStream_t s)
+                            int num_cu, int32_t *out, hipStream_t s)
 {
-    if (dtype == PK_F16) return dp == 64 ? run<PK_F16, 64>(c, b, q, G, n_blocks, sink, local, out, s) : dp == 128 ? run<PK_F16, 128>(c, b, q, G, n_blocks, sink, local, out, s) : run<PK_F16, 256>(c, b, q, G, n_blocks, sink, local, out, s);
-    return dp == 64 ? run<PK_BF16, 64>(c, b, q, G, n_blocks, sink, local, out, s) : dp == 128 ? run<PK_BF16, 128>(c, b, q, G, n_blocks, sink, local, out, s) : run<PK_BF16, 256>(c, b, q, G, n_blocks, sink, local, out, s);
+    KvSelect a{};
+    a.c = c, a.b = b, a.q = q, a.G = G, a.n = n_blocks, a.sink = sink, a.local = local, a.out = out;
+    if (dtype == PK_F16) return dp == 64 ? run_waves<PK_F16, 64>(a, num_cu, s) : dp == 128 ? run_waves<PK_F16, 128>(a, num_cu, s) : run_waves<PK_F16, 256>(a, num_cu, s);
+    return dp == 64 ? run_waves<PK_BF16, 64>(a, num_cu, s) : dp == 128 ? run_waves<PK_BF16, 128>(a, num_cu, s) : run_waves<PK_BF16, 256>(a, num_cu, s);
 }
 
 } // namespace pk
