@@ -126,8 +126,8 @@ __device__ __forceinline__ void kv_write_row(const KvAttend &a, int h, int tok, 
 // used, and the pages of both a round (their blocks, where they are listed, two rounds) earlier, so that a wave always has 8 or 16 KB on
 // its way.  Where the keys are cut into few parts, the workgroup that ends last joins them, in their order: no launch of its own.
 // blockIdx: row tile of a sequence (sparse: of a token), part of its keys, head; the heads fastest, so that each of the chip's eight
-// parts reads few of them.
-template <int S, int T, int DP, bool SPARSE>
+// parts reads few of them.  ONE: a tile of keys lies in one page.
+template <int S, int T, int DP, bool SPARSE, bool ONE>
 __global__ __launch_bounds__(256, DP * KvBytes<S>::v > 128 ? 1 : 2) void kv_rows_kernel(KvAttend a)
 {
     constexpr int ES = KvBytes<S>::v;
@@ -188,7 +188,7 @@ __global__ __launch_bounds__(256, DP * KvBytes<S>::v > 128 ? 1 : 2) void kv_rows
     }
 
     // ---- blocks, pages and K on their way
-    const int ksub = col >> 2; // the lane's run of K's rows; of V's tokens: g
+    const int ksub = ONE ? 0 : col >> 2, vsub = ONE ? 0 : g; // the lane's run of K's rows, and of V's tokens, whose pages it has to know
     auto block_of = [&](int t, int sub) __attribute__((always_inline)) -> int {
         if constexpr (SPARSE) {
             const int bi = min((t * kKvTile + sub * 16) >> c.logP, a.n_blocks - 1);
@@ -206,10 +206,19 @@ __global__ __launch_bounds__(256, DP * KvBytes<S>::v > 128 ? 1 : 2) void kv_rows
         const uint32_t page = (uint32_t)table[max(base, 0) >> c.logP]; // (asked for whether wanted or not: no branch)
         return base >= 0 ? page : c.n_pages;
     };
+    // (ONE: what all lanes have, taken out of a vector register where it is used, not where it is asked for)
+    auto taken = [&](KvRun r) __attribute__((always_inline)) -> KvRun {
+        if constexpr (ONE) {
+            asm volatile("" : "+v"(r.page), "+v"(r.base));
+            r.base = same(r.base);
+            r.page = (uint32_t)same((int)r.page);
+        }
+        return r;
+    };
     u32x4 kw[4][KC];
     auto ask_k = [&](const KvRun &r) __attribute__((always_inline)) {
         const size_t ph = (size_t)(r.page < c.n_pages ? r.page : 0) * c.H + h;
-        const char *kr = c.k + (ph * P + (r.base >= 0 ? r.base & (P - 1) : 0)) * DP * ES + g * 64 + (col & 3) * 16;
+        const char *kr = c.k + (ph * P + (r.base >= 0 ? r.base & (P - 1) : 0)) * DP * ES + (uint32_t)((ONE ? col >> 2 : 0) * 16 * DP * ES + g * 64 + (col & 3) * 16);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -219,18 +228,21 @@ __global__ __launch_bounds__(256, DP * KvBytes<S>::v > 128 ? 1 : 2) void kv_rows
     int kblock = 0, vblock = 0; // (sparse) of the round after the next
     KvRun kr, vr, kr1, vr1;     // of this round and the next
     {
-        const int kb0 = block_of(tw, ksub), vb0 = block_of(tw, g), kb1 = block_of(tw + 4, ksub), vb1 = block_of(tw + 4, g);
-        kblock = block_of(tw + 8, ksub), vblock = block_of(tw + 8, g);
-        kr.base = base_of(tw, ksub, kb0), vr.base = base_of(tw, g, vb0);
-        kr1.base = base_of(tw + 4, ksub, kb1), vr1.base = base_of(tw + 4, g, vb1);
-        kr.page = page_of(kr.base), vr.page = page_of(vr.base);
-        kr1.page = page_of(kr1.base), vr1.page = page_of(vr1.base);
+        const int kb0 = block_of(tw, ksub), vb0 = ONE ? kb0 : block_of(tw, vsub), kb1 = block_of(tw + 4, ksub), vb1 = ONE ? kb1 : block_of(tw + 4, vsub);
+        kblock = block_of(tw + 8, ksub), vblock = ONE ? kblock : block_of(tw + 8, vsub);
+        kr.base = base_of(tw, ksub, kb0), vr.base = base_of(tw, vsub, vb0);
+        kr1.base = base_of(tw + 4, ksub, kb1), vr1.base = base_of(tw + 4, vsub, vb1);
+        kr.page = page_of(kr.base), vr.page = ONE ? kr.page : page_of(vr.base);
+        kr1.page = page_of(kr1.base), vr1.page = ONE ? kr1.page : page_of(vr1.base);
+        kr = taken(kr);
+        if constexpr (ONE) vr = kr;
     }
 
     // queries, as the right operand
     u32x4 qf[KS];
-    float qscale = a.scale * kLog2e, x0;
+    float qscale = a.scale != 0.f ? fabsf(a.scale) * kLog2e : 1.f, x0; // (the query carries the scale's sign)
     {
+        const float sign = a.scale > 0.f ? 1.f : a.scale < 0.f ? -1.f : 0.f;
         const char *qrow = a.q.data + ((size_t)tok * a.q.token_stride + (size_t)(h * G + member) * a.q.head_stride) * 2;
         float x[KS][8], most = 0.f, sum = 0.f;
 #pragma unroll
@@ -244,6 +256,7 @@ __global__ __launch_bounds__(256, DP * KvBytes<S>::v > 128 ? 1 : 2) void kv_rows
         }
         KvQueryScale<S, T> qs;
         qs.largest(over_quarters_max(most));
+        qs.near *= sign;
 #pragma unroll
         for (int k = 0; k < KS; ++k)
 #pragma unroll
@@ -264,21 +277,21 @@ __global__ __launch_bounds__(256, DP * KvBytes<S>::v > 128 ? 1 : 2) void kv_rows
     if (tw < t1) ask_k(kr);
     for (int t = tw; t < t1; t += 4) {
         const bool there = vr.page < c.n_pages;
-        const int vb = vr.base;
+        const int vb = ONE ? (vr.base >= 0 ? vr.base + g * 16 : -1) : vr.base; // the lane's first token
         f32x4 ksc[4], vsc[4];
         u32x4 vw[DT][VC];
         {
             const size_t vph = (size_t)(there ? vr.page : 0) * c.H + h;
-            const int voff = vb >= 0 ? vb & (P - 1) : 0;
+            const int voff = vr.base >= 0 ? vr.base & (P - 1) : 0, vrun = ONE ? g * 16 : 0;
             if constexpr (CODED) {
-                const float *ks = c.ks + vph * P + voff, *vs = c.vs + vph * P + voff;
+                const float *ks = c.ks + vph * P + voff + (uint32_t)vrun, *vs = c.vs + vph * P + voff + (uint32_t)vrun;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     ksc[i] = *reinterpret_cast<const f32x4 *>(ks + 4 * i);
                     vsc[i] = *reinterpret_cast<const f32x4 *>(vs + 4 * i);
                 }
             }
-            const char *v = c.v + (vph * P + voff) * DP * ES + col * 16;
+            const char *v = c.v + (vph * P + voff) * DP * ES + (uint32_t)(vrun * DP * ES + col * 16);
 #pragma unroll
             for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -304,10 +317,10 @@ __global__ __launch_bounds__(256, DP * KvBytes<S>::v > 128 ? 1 : 2) void kv_rows
         }
         __builtin_amdgcn_sched_barrier(0);
         // the pages of the round after the next (first: whoever waits for them does not wait for K), and the next round's K
-        kr = kr1, vr = vr1;
-        kr1.base = base_of(t + 8, ksub, kblock), vr1.base = base_of(t + 8, g, vblock);
-        kr1.page = page_of(kr1.base), vr1.page = page_of(vr1.base);
-        kblock = block_of(t + 12, ksub), vblock = block_of(t + 12, g);
+        kr = taken(kr1), vr = ONE ? kr : vr1;
+        kr1.base = base_of(t + 8, ksub, kblock), vr1.base = base_of(t + 8, vsub, vblock);
+        kr1.page = page_of(kr1.base), vr1.page = ONE ? kr1.page : page_of(vr1.base);
+        kblock = block_of(t + 12, ksub), vblock = ONE ? kblock : block_of(t + 12, vsub);
         __builtin_amdgcn_sched_barrier(0);
         ask_k(kr);
         __builtin_amdgcn_sched_barrier(0);
@@ -315,7 +328,6 @@ __global__ __launch_bounds__(256, DP * KvBytes<S>::v > 128 ? 1 : 2) void kv_rows
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             if constexpr (CODED) x[i] *= ksc[i];
-            x[i] *= qscale;
         }
         // keys that a query does not see; the values of tokens that no query sees are taken as zeros, whatever lies there
         const int seen = (there ? min(pos, sq.len - 1) : -1) - vb; // of the lane's 16 keys: 0 .. seen
@@ -355,7 +367,7 @@ __global__ __launch_bounds__(256, DP * KvBytes<S>::v > 128 ? 1 : 2) void kv_rows
         }
         if (__any(most > m || big > vunit)) { // else all stays as it is
             const float m1 = fmaxf(m, most);
-            float fade = m1 == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - m1);
+            float fade = m1 == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - m1) * qscale);
             m = m1;
             l *= fade;
             if constexpr (Sc::UNITS) {
@@ -367,14 +379,14 @@ __global__ __launch_bounds__(256, DP * KvBytes<S>::v > 128 ? 1 : 2) void kv_rows
 #pragma unroll
             for (int d = 0; d < DT; ++d) o[d] *= fade;
         }
-        const float base = (m == -INFINITY ? 0.f : m) - Sc::top;
+        const float base = (m == -INFINITY ? 0.f : m * qscale) - Sc::top;
         f32x4 p[4];
         float sum = 0.f;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                p[i][j] = __builtin_amdgcn_exp2f(x[i][j] - base);
+                p[i][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i][j], qscale, -base));
                 sum = __builtin_fmaf(p[i][j], Sc::l_unit, sum);
             }
         l += sum;
@@ -389,6 +401,7 @@ __global__ __launch_bounds__(256, DP * KvBytes<S>::v > 128 ? 1 : 2) void kv_rows
             for (int i = 0; i < 4; ++i) {
                 const float p0 = p[2 * u + (i >> 1)][(i & 1) * 2], p1 = p[2 * u + (i >> 1)][(i & 1) * 2 + 1];
                 pf[u][i] = pack16<T>(p0, p1);
+                if constexpr (TWICE) asm("" : "+v"(pf[u][i])); // (its halves are what was rounded: not rounded again)
                 if constexpr (TWICE) pr[u][i] = pack16<T>(p0 - __uint_as_float(pf[u][i] << 16), p1 - __uint_as_float(pf[u][i] & 0xffff0000u));
             }
 #pragma unroll
@@ -412,7 +425,7 @@ __global__ __launch_bounds__(256, DP * KvBytes<S>::v > 128 ? 1 : 2) void kv_rows
 #pragma unroll
     for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4 *>(&join_o[wave][col][d * 16 + g * 4]) = o[d] * back;
     if (g == 0) {
-        join_m[wave][col] = m;
+        join_m[wave][col] = m * qscale;
         join_l[wave][col] = l;
     }
     __syncthreads();
@@ -905,6 +918,7 @@ __global__ __launch_bounds__(NW * 64) void kv_tile_kernel(KvAttend a)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 pf[u][i] = pack16<T>(p[2 * i], p[2 * i + 1]);
+                if constexpr (TWICE) asm("" : "+v"(pf[u][i]));
                 if constexpr (TWICE) pr[u][i] = pack16<T>(p[2 * i] - __uint_as_float(pf[u][i] << 16), p[2 * i + 1] - __uint_as_float(pf[u][i] & 0xffff0000u));
             }
         }
@@ -1038,7 +1052,9 @@ hipError_t run(KvAttend a, hipStream_t s)
         cut(a, items, tiles, 16, 2 * a.num_cu, 4, 16 * a.num_cu, 32);
         // the last part's workgroup joins them where all run at once; its fences cost more than a launch where there are many
         a.join_here = items * a.n_split <= a.num_cu && items <= kKvArrivals;
-        kv_rows_kernel<S, T, DP, SPARSE><<<dim3((unsigned)(items * a.n_split)), 256, 0, s>>>(a);
+        const dim3 grid((unsigned)(items * a.n_split));
+        if (a.c.P >= kKvTile) kv_rows_kernel<S, T, DP, SPARSE, true><<<grid, 256, 0, s>>>(a);
+        else kv_rows_kernel<S, T, DP, SPARSE, false><<<grid, 256, 0, s>>>(a);
         if (a.n_split > 1 && !a.join_here) kv_join_kernel<T, DP, 16, SPARSE><<<dim3((unsigned)units, a.c.H), 256, 0, s>>>(a);
     }
     if constexpr (!SPARSE) {
