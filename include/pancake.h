@@ -499,7 +499,7 @@ int pk_kv_append(pk_kv *kv, const pk_kv_batch *batch, const pk_rows *k, const pk
 int pk_kv_read(pk_kv *kv, const pk_kv_batch *batch, void *k_out, void *v_out, int32_t dtype, void *stream);
 
 /* The bounds of pages: hi, lo DEVICE [n][n_heads][head_dim] float32 (codes times scale); zeros for a page number outside the cache.
- *   pages  DEVICE [n] int32.  Asynchronous. */
+ *   pages  DEVICE [n] int32;  hi, lo 16-byte aligned.  Asynchronous. */
 int pk_kv_bounds(pk_kv *kv, const int32_t *pages, int64_t n, float *hi, float *lo, void *stream);
 
 /*

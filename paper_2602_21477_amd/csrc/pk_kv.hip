@@ -142,47 +142,55 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(KvDev c, KvBatch b,
         hi[i] = -INFINITY;
         lo[i] = INFINITY;
     }
-    for (int r0 = 0; r0 < p1; r0 += kRowsAtOnce) {
+    auto bound = [&](const char *codes, float scale) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+            const float z = kv_coded<S> ? decode<S, false>(codes, i) * scale : decode<S, false>(codes, i);
+            hi[i] = fmaxf(hi[i], z);
+            lo[i] = fminf(lo[i], z);
+        }
+    };
+    constexpr int N = E * ES < 16 ? E * ES : 16; // (a lane's bytes of a row lie in pieces of 16, or in one)
+    // rows that were there, several asked for at once
+    constexpr int AHEAD = 4;
+    for (int r0 = 0; r0 < p0; r0 += AHEAD * kRowsAtOnce) {
+        char codes[AHEAD][E * ES];
+        float scale[AHEAD];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            const int r = min(r0 + k * kRowsAtOnce + tid / kRowLanes, p0 - 1); // (a row twice is no other bound)
+#pragma unroll
+            for (int i = 0; i < E * ES; i += N) __builtin_memcpy(codes[k] + i, kp + k_place<ES, DP>(r, at * ES + i), N);
+            scale[k] = kv_coded<S> ? c.ks[ph * c.P + r] : 1.f;
+        }
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) bound(codes[k], scale[k]);
+    }
+    // new rows
+    for (int r0 = p0 / kRowsAtOnce * kRowsAtOnce; r0 < p1; r0 += kRowsAtOnce) {
         const int r = r0 + tid / kRowLanes;
-        const bool in = r < p1, fresh = in && r >= p0;
-        float scale = 1.f;
+        if (r < p0 || r >= p1) continue;
+        const int t = g.q.first + (g.base + r - (g.q.len - g.q.m));
         char codes[E * ES];
-        if (fresh) {
-            const int t = g.q.first + (g.base + r - (g.q.len - g.q.m));
-            float x[E], y[E];
-            load_row<T, E>(x, kin.data + ((size_t)t * kin.token_stride + (size_t)h * kin.head_stride) * (T == PK_F32 ? 4 : 2), at, c.D);
-            load_row<T, E>(y, vin.data + ((size_t)t * vin.token_stride + (size_t)h * vin.head_stride) * (T == PK_F32 ? 4 : 2), at, c.D);
-            const float vscale = encode<S, E, true>(y, codes);
+        float x[E], y[E];
+        load_row<T, E>(x, kin.data + ((size_t)t * kin.token_stride + (size_t)h * kin.head_stride) * (T == PK_F32 ? 4 : 2), at, c.D);
+        load_row<T, E>(y, vin.data + ((size_t)t * vin.token_stride + (size_t)h * vin.head_stride) * (T == PK_F32 ? 4 : 2), at, c.D);
+        const float vscale = encode<S, E, true>(y, codes);
 #pragma unroll
-            for (int i = 0; i < E; ++i) {
-                if constexpr (ES == 1) vimg[v_image<ES, DP>(r, at + i)] = codes[i];
-                else __builtin_memcpy(vimg + v_image<ES, DP>(r, at + i), codes + 2 * i, 2);
-            }
-            scale = encode<S, E, false>(x, codes);
-            // (a lane's bytes lie in pieces of 16, or in one)
-            constexpr int N = E * ES < 16 ? E * ES : 16;
-#pragma unroll
-            for (int i = 0; i < E * ES; i += N) __builtin_memcpy(kimg + k_place<ES, DP>(r, at * ES + i), codes + i, N);
-            if constexpr (kv_coded<S>) {
-                if (sub == 0) {
-                    c.ks[ph * c.P + r] = scale;
-                    c.vs[ph * c.P + r] = vscale;
-                }
-            }
-        } else if (in) {
-            constexpr int N = E * ES < 16 ? E * ES : 16;
-#pragma unroll
-            for (int i = 0; i < E * ES; i += N) __builtin_memcpy(codes + i, kp + k_place<ES, DP>(r, at * ES + i), N);
-            if constexpr (kv_coded<S>) scale = c.ks[ph * c.P + r];
+        for (int i = 0; i < E; ++i) {
+            if constexpr (ES == 1) vimg[v_image<ES, DP>(r, at + i)] = codes[i];
+            else __builtin_memcpy(vimg + v_image<ES, DP>(r, at + i), codes + 2 * i, 2);
         }
-        if (in) {
+        const float scale = encode<S, E, false>(x, codes);
 #pragma unroll
-            for (int i = 0; i < E; ++i) {
-                const float z = kv_coded<S> ? decode<S, false>(codes, i) * scale : decode<S, false>(codes, i);
-                hi[i] = fmaxf(hi[i], z);
-                lo[i] = fminf(lo[i], z);
+        for (int i = 0; i < E * ES; i += N) __builtin_memcpy(kimg + k_place<ES, DP>(r, at * ES + i), codes + i, N);
+        if constexpr (kv_coded<S>) {
+            if (sub == 0) {
+                c.ks[ph * c.P + r] = scale;
+                c.vs[ph * c.P + r] = vscale;
             }
         }
+        bound(codes, scale);
     }
 #pragma unroll
     for (int i = 0; i < E; ++i) {
@@ -222,19 +230,19 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(KvDev c, KvBatch b,
         if (tid == 0) c.bs[ph] = most * (1.f / 127.f);
     }
     // keys: a piece is part of one token; values: 16 or 8 tokens of a channel, one by one where not all of them are new
-    constexpr int N = 16 / ES, PIECES = DP * ES / 16;
+    constexpr int VN = 16 / ES, PIECES = DP * ES / 16;
     for (int i = (p0 >> 2) * 4 * PIECES + tid; i < ((p1 + 3) >> 2) * 4 * PIECES; i += kThreads) {
         const int tok = i / (4 * PIECES) * 4 + (i & 3);
         if (tok >= p0 && tok < p1) *reinterpret_cast<u32x4 *>(kp + (size_t)i * 16) = *reinterpret_cast<const u32x4 *>(kimg + i * 16);
     }
-    for (int i = p0 / N * DP + tid; i < (p1 + N - 1) / N * DP; i += kThreads) {
-        const int tok = i / DP * N, d = i % DP;
+    for (int i = p0 / VN * DP + tid; i < (p1 + VN - 1) / VN * DP; i += kThreads) {
+        const int tok = i / DP * VN, d = i % DP;
         if (d >= c.D) continue;
         const char *from = vimg + v_image<ES, DP>(tok, d);
-        if (tok >= p0 && tok + N <= p1) {
+        if (tok >= p0 && tok + VN <= p1) {
             *reinterpret_cast<u32x4 *>(vp + (size_t)i * 16) = *reinterpret_cast<const u32x4 *>(from);
         } else {
-            for (int j = max(tok, p0); j < min(tok + N, p1); ++j) {
+            for (int j = max(tok, p0); j < min(tok + VN, p1); ++j) {
                 if constexpr (ES == 1) vp[(size_t)i * 16 + (j - tok)] = from[j - tok];
                 else reinterpret_cast<uint16_t *>(vp + (size_t)i * 16)[j - tok] = reinterpret_cast<const uint16_t *>(from)[j - tok];
             }
@@ -308,12 +316,21 @@ __global__ __launch_bounds__(kThreads) void kv_bounds_kernel(KvDev c, int dp, co
     const size_t n = blockIdx.x;
     const uint32_t page = (uint32_t)pages[n];
     const bool there = page < c.n_pages;
-    for (int i = threadIdx.x; i < c.H * c.D; i += kThreads) {
+    for (int i = threadIdx.x * 4; i < c.H * c.D; i += kThreads * 4) { // (D is a multiple of 8: four channels are of one head)
         const int h = i / c.D, d = i - h * c.D;
         const size_t ph = (size_t)(there ? page : 0) * c.H + h;
         const float s = there ? c.bs[ph] : 0.f;
-        hi[n * c.H * c.D + i] = there ? (float)c.bc[ph * 2 * dp + d] * s : 0.f;
-        lo[n * c.H * c.D + i] = there ? (float)c.bc[(ph * 2 + 1) * dp + d] * s : 0.f;
+        char bh[4], bl[4];
+        __builtin_memcpy(bh, c.bc + ph * 2 * dp + d, 4);
+        __builtin_memcpy(bl, c.bc + (ph * 2 + 1) * dp + d, 4);
+        f32x4 x, y;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            x[j] = there ? (float)(int8_t)bh[j] * s : 0.f;
+            y[j] = there ? (float)(int8_t)bl[j] * s : 0.f;
+        }
+        *reinterpret_cast<f32x4 *>(hi + n * c.H * c.D + i) = x;
+        *reinterpret_cast<f32x4 *>(lo + n * c.H * c.D + i) = y;
     }
 }
 
@@ -612,7 +629,7 @@ int pk_kv_bounds(pk_kv *kv, const int32_t *pages, int64_t n, float *hi, float *l
     if (!live(kv)) return PK_ERR_BAD_HANDLE;
     if (n < 0 || n > 0x7fffffff) return PK_ERR_INVALID_ARG;
     if (n == 0) return PK_OK;
-    if (!pages || !hi || !lo) return PK_ERR_INVALID_ARG;
+    if (!pages || !hi || !lo || ((reinterpret_cast<uintptr_t>(hi) | reinterpret_cast<uintptr_t>(lo)) & 15)) return PK_ERR_INVALID_ARG;
     return launch_kv_bounds(kv->dev, kv->dp, pages, n, hi, lo, static_cast<hipStream_t>(stream)) == hipSuccess ? PK_OK : PK_ERR_HIP;
 }
 
