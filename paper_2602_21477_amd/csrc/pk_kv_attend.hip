@@ -127,7 +127,10 @@ __device__ __forceinline__ void kv_write_row(const KvAttend &a, int h, int tok, 
 // its way.  Where the keys are cut into few parts, the workgroup that ends last joins them, in their order: no launch of its own.
 // blockIdx: row tile of a sequence (sparse: of a token), part of its keys, head; the heads fastest, so that each of the chip's eight
 // parts reads few of them.  ONE: a tile of keys lies in one page.
-template <int S, int T, int DP, bool SPARSE, bool ONE>
+// R: where there are 16 / R queries at most, each of them has R columns, and a column weighs that part of a lane's keys that is its own: a
+// column is a softmax of its own, joined with the others in the end as the waves' are.  For the sparse form, which reads from the
+// caches and is bound by the vector units (1024 tokens, 32 blocks each of int8, 4 heads a group: R 1 403 us, R 4 361 us).
+template <int S, int T, int DP, bool SPARSE, bool ONE, int R>
 __global__ __launch_bounds__(256, DP * KvBytes<S>::v > 128 ? 1 : 2) void kv_rows_kernel(KvAttend a)
 {
     constexpr int ES = KvBytes<S>::v;
@@ -138,6 +141,7 @@ __global__ __launch_bounds__(256, DP * KvBytes<S>::v > 128 ? 1 : 2) void kv_rows
     constexpr int KS = DP / 32;               // products over the channels
     constexpr int DT = DP / 16;               // tiles of 16 channels of the output
     constexpr int VC = CODED ? 1 : 2;         // loads of a lane for 16 tokens of a channel
+    constexpr int RT = 16 / R, NI = 4 / R;    // queries of a tile; of a lane's four groups of four keys, those that its column weighs
     __shared__ __align__(16) float join_o[4][16][DP + 4];
     __shared__ float join_m[4][16], join_l[4][16];
     __shared__ uint32_t arrived;
@@ -161,8 +165,8 @@ __global__ __launch_bounds__(256, DP * KvBytes<S>::v > 128 ? 1 : 2) void kv_rows
     }
     const KvSeq sq = kv_seq(a.b, seq, P);
     const int rows = SPARSE ? G : sq.m * G;
-    if (tile * 16 >= rows || (!SPARSE && rows > a.few_rows)) return;
-    const int row = tile * 16 + col;
+    if (tile * RT >= rows || (!SPARSE && rows > a.few_rows)) return;
+    const int part = R == 1 ? 0 : col / RT, row = tile * RT + col % RT;
     const bool valid = row < rows;
     const int tok = SPARSE ? token0 : sq.first + min(row, rows - 1) / G;
     const int member = min(row, rows - 1) % G;
@@ -181,7 +185,7 @@ __global__ __launch_bounds__(256, DP * KvBytes<S>::v > 128 ? 1 : 2) void kv_rows
         t0 = split * a.split_tiles;
         t1 = min((a.n_blocks * P + kKvTile - 1) / kKvTile, t0 + a.split_tiles);
     } else {
-        const int first_pos = start + (tile * 16) / G, last_pos = start + min(tile * 16 + 15, rows - 1) / G;
+        const int first_pos = start + (tile * RT) / G, last_pos = start + min(tile * RT + RT - 1, rows - 1) / G;
         const int lo = a.window > 0 ? max(first_pos - a.window + 1, 0) / kKvTile : 0;
         t0 = max(lo, split * a.split_tiles);
         t1 = min(last_pos < 0 ? 0 : last_pos / kKvTile + 1, (split + 1) * a.split_tiles);
@@ -278,15 +282,15 @@ __global__ __launch_bounds__(256, DP * KvBytes<S>::v > 128 ? 1 : 2) void kv_rows
     for (int t = tw; t < t1; t += 4) {
         const bool there = vr.page < c.n_pages;
         const int vb = ONE ? (vr.base >= 0 ? vr.base + g * 16 : -1) : vr.base; // the lane's first token
-        f32x4 ksc[4], vsc[4];
+        f32x4 ksc[NI], vsc[NI];
         u32x4 vw[DT][VC];
         {
             const size_t vph = (size_t)(there ? vr.page : 0) * c.H + h;
             const int voff = vr.base >= 0 ? vr.base & (P - 1) : 0, vrun = ONE ? g * 16 : 0;
             if constexpr (CODED) {
-                const float *ks = c.ks + vph * P + voff + (uint32_t)vrun, *vs = c.vs + vph * P + voff + (uint32_t)vrun;
+                const float *ks = c.ks + vph * P + voff + (uint32_t)(vrun + part * NI * 4), *vs = c.vs + vph * P + voff + (uint32_t)(vrun + part * NI * 4);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
+                for (int i = 0; i < NI; ++i) {
                     ksc[i] = *reinterpret_cast<const f32x4 *>(ks + 4 * i);
                     vsc[i] = *reinterpret_cast<const f32x4 *>(vs + 4 * i);
                 }
@@ -299,19 +303,19 @@ __global__ __launch_bounds__(256, DP * KvBytes<S>::v > 128 ? 1 : 2) void kv_rows
         }
         __builtin_amdgcn_sched_barrier(0);
 
-        f32x4 x[4];
+        f32x4 xa[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            x[i] = f32x4{x0, x0, x0, x0};
+            xa[i] = f32x4{x0, x0, x0, x0};
 #pragma unroll
             for (int k = 0; k < KC; ++k) {
                 u32x4 f0, f1;
                 operands<S, T, false>(kw[i][k], f0, f1);
                 if constexpr (CODED) {
-                    x[i] = mma<HALF>(f0, qf[2 * k], x[i]);
-                    x[i] = mma<HALF>(f1, qf[2 * k + 1], x[i]);
+                    xa[i] = mma<HALF>(f0, qf[2 * k], xa[i]);
+                    xa[i] = mma<HALF>(f1, qf[2 * k + 1], xa[i]);
                 } else {
-                    x[i] = mma<HALF>(f0, qf[k], x[i]);
+                    xa[i] = mma<HALF>(f0, qf[k], xa[i]);
                 }
             }
         }
@@ -325,8 +329,15 @@ __global__ __launch_bounds__(256, DP * KvBytes<S>::v > 128 ? 1 : 2) void kv_rows
         ask_k(kr);
         __builtin_amdgcn_sched_barrier(0);
 
+        // the column's keys
+        f32x4 x[NI];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < NI; ++i) {
+            x[i] = xa[i];
+#pragma unroll
+            for (int k = 1; k < R; ++k)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) x[i][j] = part == k ? xa[k * NI + i][j] : x[i][j];
             if constexpr (CODED) x[i] *= ksc[i];
         }
         // keys that a query does not see; the values of tokens that no query sees are taken as zeros, whatever lies there
@@ -334,12 +345,12 @@ __global__ __launch_bounds__(256, DP * KvBytes<S>::v > 128 ? 1 : 2) void kv_rows
         const int since = from - vb;
         if (__any(seen < 15 || since > 0 || vb < 0)) {
             const int held = there && vb >= 0 ? sq.len - vb : 0; // of its 16 tokens
-            const int last = vb >= 0 ? seen : -1;
+            const int last = vb >= 0 ? seen : -1, key0 = part * NI * 4;
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < NI; ++i)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const int key = 4 * i + j;
+                    const int key = key0 + 4 * i + j;
                     x[i][j] = key <= last && key >= since ? x[i][j] : -INFINITY;
                     if constexpr (CODED) vsc[i][j] = key < held ? vsc[i][j] : 0.f;
                 }
@@ -358,12 +369,12 @@ __global__ __launch_bounds__(256, DP * KvBytes<S>::v > 128 ? 1 : 2) void kv_rows
         }
         float most = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) most = max3(most, max3(x[i][0], x[i][1], x[i][2]), x[i][3]);
+        for (int i = 0; i < NI; ++i) most = max3(most, max3(x[i][0], x[i][1], x[i][2]), x[i][3]);
         most = over_quarters_max(most);
         float big = 0.f;
         if constexpr (Sc::UNITS) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) big = max3(big, max3(vsc[i][0], vsc[i][1], vsc[i][2]), vsc[i][3]);
+            for (int i = 0; i < NI; ++i) big = max3(big, max3(vsc[i][0], vsc[i][1], vsc[i][2]), vsc[i][3]);
         }
         if (__any(most > m || big > vunit)) { // else all stays as it is
             const float m1 = fmaxf(m, most);
@@ -380,10 +391,10 @@ __global__ __launch_bounds__(256, DP * KvBytes<S>::v > 128 ? 1 : 2) void kv_rows
             for (int d = 0; d < DT; ++d) o[d] *= fade;
         }
         const float base = (m == -INFINITY ? 0.f : m * qscale) - Sc::top;
-        f32x4 p[4];
+        f32x4 p[NI];
         float sum = 0.f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < NI; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 p[i][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i][j], qscale, -base));
@@ -392,18 +403,31 @@ __global__ __launch_bounds__(256, DP * KvBytes<S>::v > 128 ? 1 : 2) void kv_rows
         l += sum;
         if constexpr (CODED) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) p[i] *= Sc::UNITS ? vsc[i] * vper : vsc[i];
+            for (int i = 0; i < NI; ++i) p[i] *= Sc::UNITS ? vsc[i] * vper : vsc[i];
         }
-        u32x4 pf[2], pr[2]; // weights, and (TWICE) what their rounding left
+        u32x4 pf[2], pr[2]; // weights, and (TWICE) what their rounding left; of other columns' keys zeros
+        uint32_t w[NI][2], r[NI][2];
+#pragma unroll
+        for (int i = 0; i < NI; ++i)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const float p0 = p[i][2 * e], p1 = p[i][2 * e + 1];
+                w[i][e] = pack16<T>(p0, p1);
+                if constexpr (TWICE) {
+                    asm("" : "+v"(w[i][e])); // (its halves are what was rounded: not rounded again)
+                    r[i][e] = pack16<T>(p0 - __uint_as_float(w[i][e] << 16), p1 - __uint_as_float(w[i][e] & 0xffff0000u));
+                }
+            }
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float p0 = p[2 * u + (i >> 1)][(i & 1) * 2], p1 = p[2 * u + (i >> 1)][(i & 1) * 2 + 1];
-                pf[u][i] = pack16<T>(p0, p1);
-                if constexpr (TWICE) asm("" : "+v"(pf[u][i])); // (its halves are what was rounded: not rounded again)
-                if constexpr (TWICE) pr[u][i] = pack16<T>(p0 - __uint_as_float(pf[u][i] << 16), p1 - __uint_as_float(pf[u][i] & 0xffff0000u));
-            }
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const bool mine = R == 1 || part == (2 * u + i) / NI;
+                    pf[u][2 * i + e] = mine ? w[(2 * u + i) % NI][e] : 0u;
+                    if constexpr (TWICE) pr[u][2 * i + e] = mine ? r[(2 * u + i) % NI][e] : 0u;
+                }
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
             u32x4 f0, f1;
@@ -430,22 +454,24 @@ __global__ __launch_bounds__(256, DP * KvBytes<S>::v > 128 ? 1 : 2) void kv_rows
     }
     __syncthreads();
     const int r = tid >> 4, sub = tid & 15; // 16 threads a row
-    const bool in_row = tile * 16 + r < rows;
-    const int otok = SPARSE ? token0 : sq.first + min(tile * 16 + r, rows - 1) / G, omember = (tile * 16 + r) % G;
-    float mm = join_m[0][r];
+    const bool in_row = r < RT && tile * RT + r < rows;
+    const int otok = SPARSE ? token0 : sq.first + min(tile * RT + r, rows - 1) / G, omember = (tile * RT + r) % G;
+    // a row's columns in the four waves: column r + k RT of wave w has f[w + 4 k]
+    const int rr = r % RT;
+    float mm = -INFINITY;
 #pragma unroll
-    for (int w = 1; w < 4; ++w) mm = fmaxf(mm, join_m[w][r]);
+    for (int w = 0; w < 4 * R; ++w) mm = fmaxf(mm, join_m[w & 3][rr + (w >> 2) * RT]);
     const float mb = mm == -INFINITY ? 0.f : mm;
-    float f[4], ll = 0.f;
+    float f[4 * R], ll = 0.f;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-        f[w] = __builtin_amdgcn_exp2f(join_m[w][r] - mb);
-        ll += f[w] * join_l[w][r];
+    for (int w = 0; w < 4 * R; ++w) {
+        f[w] = __builtin_amdgcn_exp2f(join_m[w & 3][rr + (w >> 2) * RT] - mb);
+        ll += f[w] * join_l[w & 3][rr + (w >> 2) * RT];
     }
     auto joined = [&](int dd) __attribute__((always_inline)) {
         f32x4 y = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int w = 0; w < 4; ++w) y += f[w] * *reinterpret_cast<const f32x4 *>(&join_o[w][r][dd]);
+        for (int w = 0; w < 4 * R; ++w) y += f[w] * *reinterpret_cast<const f32x4 *>(&join_o[w & 3][rr + (w >> 2) * RT][dd]);
         return y;
     };
     if (a.n_split == 1) {
@@ -1053,8 +1079,15 @@ hipError_t run(KvAttend a, hipStream_t s)
         // the last part's workgroup joins them where all run at once; its fences cost more than a launch where there are many
         a.join_here = items * a.n_split <= a.num_cu && items <= kKvArrivals;
         const dim3 grid((unsigned)(items * a.n_split));
-        if (a.c.P >= kKvTile) kv_rows_kernel<S, T, DP, SPARSE, true><<<grid, 256, 0, s>>>(a);
-        else kv_rows_kernel<S, T, DP, SPARSE, false><<<grid, 256, 0, s>>>(a);
+        const bool one = a.c.P >= kKvTile;
+        auto launch = [&](auto kernel) { kernel<<<grid, 256, 0, s>>>(a); };
+        if constexpr (SPARSE) {
+            if (a.G <= 4) one ? launch(kv_rows_kernel<S, T, DP, true, true, 4>) : launch(kv_rows_kernel<S, T, DP, true, false, 4>);
+            else if (a.G <= 8) one ? launch(kv_rows_kernel<S, T, DP, true, true, 2>) : launch(kv_rows_kernel<S, T, DP, true, false, 2>);
+            else one ? launch(kv_rows_kernel<S, T, DP, true, true, 1>) : launch(kv_rows_kernel<S, T, DP, true, false, 1>);
+        } else {
+            one ? launch(kv_rows_kernel<S, T, DP, false, true, 1>) : launch(kv_rows_kernel<S, T, DP, false, false, 1>);
+        }
         if (a.n_split > 1 && !a.join_here) kv_join_kernel<T, DP, 16, SPARSE><<<dim3((unsigned)units, a.c.H), 256, 0, s>>>(a);
     }
     if constexpr (!SPARSE) {
