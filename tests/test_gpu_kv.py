@@ -197,6 +197,42 @@ def test_attention(gpu_device, storage, dtype, shape, window):
     assert torch.equal(s.cache.attend(s.q.cuda(), s.batch, scale, window=window), out)
 
 
+PARTS = [
+    # what the kernels cut: a long context of few queries (joined by the last workgroup, and by a launch of their own where there are
+    # many), a chunk over a long context, wide heads, whole chunks from position 0
+    (2, 4, 128, 64, [1], [2100]),
+    (8, 1, 64, 16, [1] * 16, [1100 + 13 * i for i in range(16)]),
+    (1, 4, 64, 32, [70], [2100]),
+    (1, 4, 128, 64, [70, 3], [1601, 900]),
+    (1, 2, 256, 64, [40, 1], [150, 700]),
+    (1, 3, 256, 16, [30], [90]),
+    (2, 1, 128, 128, [300], [300]),
+]
+
+
+@pytest.mark.parametrize("storage,dtype", [("f16", "f16"), ("bf16", "bf16"), ("i8", "bf16"), ("i8", "f16"), ("f8", "bf16"), ("f8", "f16")])
+@pytest.mark.parametrize("shape", PARTS, ids=lambda s: f"{s[:4]} {len(s[4])} of {max(s[4])} at {max(s[5])}")
+def test_attention_in_parts(gpu_device, storage, dtype, shape):
+    H, G, D, P, news, lens = shape
+    s = Setup(storage, dtype, H, G, D, P, news, lens, seed=16)
+    scale = D ** -0.5
+    key = [torch.arange(l) for l in lens]
+    out, lse = s.cache.attend(s.q.cuda(), s.batch, scale, want_lse=True)
+    s.check(out, lse.cpu(), scale, lambda row, i, pos, h: key[i] <= pos)
+    for _ in range(3):
+        assert torch.equal(s.cache.attend(s.q.cuda(), s.batch, scale), out)
+
+
+@pytest.mark.parametrize("storage,dtype", [("bf16", "bf16"), ("i8", "bf16"), ("i8", "f16"), ("f8", "bf16")])
+@pytest.mark.parametrize("scale", [-0.07, 0.0, 3.0])
+def test_scales_of_any_sign(gpu_device, storage, dtype, scale):
+    for news in ([2, 1], [90, 1]):
+        s = Setup(storage, dtype, 1, 2, 64, 32, news, [130, 40], seed=17, spread=0.3)
+        key = [torch.arange(l) for l in s.lens]
+        out, lse = s.cache.attend(s.q.cuda(), s.batch, scale, want_lse=True)
+        s.check(out, lse.cpu(), scale, lambda row, i, pos, h: key[i] <= pos)
+
+
 @pytest.mark.parametrize("storage,dtype", [("bf16", "bf16"), ("f8", "f16"), ("i8", "bf16")])
 def test_attention_without_some_pages(gpu_device, storage, dtype):
     """Pages that the table has not: their keys are not seen, and a query without keys has zeros."""
@@ -307,6 +343,19 @@ def test_selection_and_attention_to_it(gpu_device, storage, dtype, H, G, D, P, n
         key = torch.arange(lens[i])
         return (key <= pos) & torch.isin(key // P, b[row, h][b[row, h] >= 0]) & s.there(i)
     s.check(out, lse.cpu(), scale, seen)
+
+
+@pytest.mark.parametrize("H,G,news,lens,n", [(8, 2, [1] * 20, [3000 + 7 * i for i in range(20)], 12), (2, 1, [33], [5000], 40), (1, 3, [9, 2], [8000, 70], 3)])
+def test_selection_of_many_blocks(gpu_device, H, G, news, lens, n):
+    """Workgroups of four waves and of sixteen, one token each and several, lists of many blocks."""
+    s = Setup("bf16", "bf16", H, G, 64, 16, news, lens, seed=18, spread=0.2)
+    got = s.cache.select(s.q.cuda(), s.batch, n)
+    want, margin = choose(s, n, 1, 2)
+    same = (got.cpu() == want).all(-1)
+    # (the scales are read back with a rounding: a choice may differ where two scores are nearer than that)
+    assert bool(same.all()) or margin < 2.0 ** -20
+    assert float(same.float().mean()) > 0.99
+    assert torch.equal(s.cache.select(s.q.cuda(), s.batch, n), got)
 
 
 def test_equal_blocks_and_empty_lists(gpu_device):
