@@ -15,6 +15,17 @@ __device__ __forceinline__ uint32_t score_key(float v)
     return max(b ^ ((b >> 31) ? 0xffffffffu : 0x80000000u), 1u);
 }
 
+// The largest of `gp` neighbouring lanes (a power of two, 16 at most), in all of them.
+__device__ __forceinline__ float group_max(float v, int gp)
+{
+    auto with = [](float x, int moved) __attribute__((always_inline)) { return fmaxf(x, __int_as_float(moved)); };
+    if (gp > 1) v = with(v, __builtin_amdgcn_update_dpp(0, __float_as_int(v), 0xb1, 0xf, 0xf, true));  // lanes 1 0 3 2
+    if (gp > 2) v = with(v, __builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x4e, 0xf, 0xf, true));  // 2 3 0 1
+    if (gp > 4) v = with(v, __builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x141, 0xf, 0xf, true)); // 7 6 .. 0
+    if (gp > 8) v = with(v, __builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x140, 0xf, 0xf, true)); // 15 14 .. 0
+    return v;
+}
+
 struct KvSelect {
     KvDev c;
     KvBatch b;
@@ -43,7 +54,7 @@ __global__ __launch_bounds__(NW * 64) void kv_select_kernel(KvSelect a)
     extern __shared__ uint32_t keys[];
     __shared__ __align__(16) u32x4 turn[NW][64];
     __shared__ uint32_t hist[NW][256];
-    __shared__ uint32_t counts[NW][3], found[NW][2];
+    __shared__ uint32_t counts[NW][3], found[NW][2], few[NW][64];
     const KvDev c = a.c;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 15, g = lane >> 4;
     const int h = blockIdx.x % c.H, unit = blockIdx.x / c.H, seq = unit / a.groups, first = (unit - seq * a.groups) * a.tokens;
@@ -95,46 +106,51 @@ __global__ __launch_bounds__(NW * 64) void kv_select_kernel(KvSelect a)
                 qp[k][w] = (int)p;
                 qm[k][w] = (int)m;
             }
+        // a lane loads piece `load_piece` of the bounds of block `load_row`, and has the scores of blocks 4 g .. 4 g + 3
         const int load_row = lane >> 2, load_piece = lane & 3;
-        auto page_at = [&](int b0, int row) __attribute__((always_inline)) -> uint32_t { return (uint32_t)table[min(b0 + row, nb - 1)]; };
-        uint32_t lpage = 0, cpage = 0;
-        if (wave * 16 < nb) {
-            lpage = page_at(wave * 16, load_row);
-            cpage = page_at(wave * 16, col);
-        }
+        auto page_at = [&](int at) __attribute__((always_inline)) -> uint32_t { return (uint32_t)table[min(at, nb - 1)]; };
+        uint32_t lpage = 0, pages[4] = {0, 0, 0, 0};
+        auto ask = [&](int b0) __attribute__((always_inline)) {
+            lpage = page_at(b0 + load_row);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) pages[j] = page_at(b0 + g * 4 + j);
+        };
+        if (wave * 16 < nb) ask(wave * 16);
         for (int b0 = wave * 16; b0 < nb; b0 += NW * 16) {
             const size_t lph = (size_t)(lpage < c.n_pages ? lpage : 0) * c.H + h;
             const int8_t *row = c.bc + lph * 2 * DP + load_piece * 16;
             u32x4 w[2 * KS];
 #pragma unroll
             for (int k = 0; k < 2 * KS; ++k) w[k] = *reinterpret_cast<const u32x4 *>(row + k * 64);
-            const uint32_t page = cpage;
-            const float bs = c.bs[(size_t)(page < c.n_pages ? page : 0) * c.H + h];
-            if (b0 + NW * 16 < nb) {
-                lpage = page_at(b0 + NW * 16, load_row);
-                cpage = page_at(b0 + NW * 16, col);
+            float scale[4];
+            bool there[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                there[j] = pages[j] < c.n_pages;
+                scale[j] = c.bs[(size_t)(there[j] ? pages[j] : 0) * c.H + h];
+            }
+            ask(b0 + NW * 16); // (past the last block: the last one's again)
+            // row r, piece p lies at 4 r + (p ^ (r / 4)): a quarter of a wave reads 16 rows from banks of their own, 2 at a time.  A wave's accesses
+            // are in order: the next piece may be written as soon as this one's read is issued
+            i32x4 f[2 * KS];
+#pragma unroll
+            for (int k = 0; k < 2 * KS; ++k) {
+                turn[wave][load_row * 4 + (load_piece ^ (load_row >> 2))] = w[k];
+                __builtin_amdgcn_wave_barrier();
+                f[k] = __builtin_bit_cast(i32x4, turn[wave][col * 4 + (g ^ (col >> 2))]);
+                __builtin_amdgcn_wave_barrier();
             }
             i32x4 acc = {0, 0, 0, 0};
 #pragma unroll
-            for (int k = 0; k < 2 * KS; ++k) {
-                // row r, piece p lies at 4 r + (p ^ (r / 4)): a quarter of a wave reads 16 rows from banks of their own, 2 at a time
-                turn[wave][load_row * 4 + (load_piece ^ (load_row >> 2))] = w[k];
-                __builtin_amdgcn_wave_barrier();
-                const i32x4 f = __builtin_bit_cast(i32x4, turn[wave][col * 4 + (g ^ (col >> 2))]);
-                __builtin_amdgcn_wave_barrier();
-                acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(f, k < KS ? qp[k % KS] : qm[k % KS], acc, 0, 0, 0);
-            }
+            for (int k = 0; k < 2 * KS; ++k) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(f[k], k < KS ? qp[k % KS] : qm[k % KS], acc, 0, 0, 0);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                float v = in ? (float)acc[j] * qscale : -INFINITY;
-                for (int d = 1; d < a.gp; d *= 2) v = fmaxf(v, __shfl_xor(v, d));
-                const int at = b0 + g * 4 + j; // its scale and page are with the lane of that column
-                const float scale = __shfl(bs, g * 4 + j);
-                const uint32_t pg = (uint32_t)__shfl((int)page, g * 4 + j);
+                const float v = group_max(in ? (float)acc[j] * qscale : -INFINITY, a.gp);
+                const int at = b0 + g * 4 + j;
                 if (token_in && member0 == 0 && at < nb) {
                     uint32_t key = 0;
-                    if (pos >= 0 && at <= mine && pg < c.n_pages)
-                        key = at < a.sink || at > mine - a.local ? kAlways : score_key(v * scale + 0.f); // (no zero of a sign)
+                    if (pos >= 0 && at <= mine && there[j])
+                        key = at < a.sink || at > mine - a.local ? kAlways : score_key(v * scale[j] + 0.f); // (no zero of a sign)
                     uint32_t *k = keys + tk * a.room + at;
                     *k = gt == 0 ? key : max(*k, key);
                 }
@@ -187,14 +203,16 @@ __global__ __launch_bounds__(NW * 64) void kv_select_kernel(KvSelect a)
         int bits = all || none || low == high ? 0 : 32 - __clz((int)(low ^ high));
         uint32_t mask = bits == 32 ? 0u : ~0u << bits, bound = none ? kAlways : high & mask;
         uint32_t *hs = hist[team * size];
-        // (every wave of the workgroup goes through four rounds where waves share a token, as they meet in each)
+        uint32_t in_bin = others; // keys that agree with `bound` in `mask`
+        // (where waves share a token, all of the workgroup go through each round, as they meet in it)
         for (int round = 0; round < 4; ++round) {
-            if (size == 1 && bits <= 0) break;
+            const bool go = bits > 0 && in_bin > 64;
+            if (size == 1 ? !go : !__syncthreads_or(go)) break;
             const int shift = max(bits - 8, 0), width = bits - shift;
             for (int i = me; i < 256; i += members) hs[i] = 0;
             if (size > 1) __syncthreads();
             else __builtin_amdgcn_wave_barrier();
-            if (bits > 0)
+            if (go)
                 for (int i = me; i < count; i += members) {
                     const uint32_t key = k[i];
                     if (key && key != kAlways && (key & mask) == bound) atomicAdd(&hs[(key >> shift) & ((1u << width) - 1)], 1u);
@@ -216,22 +234,52 @@ __global__ __launch_bounds__(NW * 64) void kv_select_kernel(KvSelect a)
             }
             above -= sum;
             int bin = -1;
-            uint32_t left = 0;
+            uint32_t left = 0, size_of = 0;
 #pragma unroll
             for (int j = 3; j >= 0; --j) {
                 if (bin < 0 && above < need && above + own[j] >= need) {
                     bin = lane * 4 + j;
                     left = need - above;
+                    size_of = own[j];
                 }
                 above += own[j];
             }
             const unsigned long long has = __ballot(bin >= 0);
-            if (bits > 0 && has) {
+            if (go && has) {
                 const int l = __ffsll(has) - 1;
                 bound |= (uint32_t)__shfl(bin, l) << shift;
                 need = (uint32_t)__shfl((int)left, l);
+                in_bin = (uint32_t)__shfl((int)size_of, l);
                 mask |= ((1u << width) - 1) << shift;
                 bits = shift;
+            }
+        }
+        // 64 keys at most are left: each lane has one and counts those above it
+        const bool last = bits > 0;
+        if (size > 1 ? __syncthreads_or(last) : last) {
+            uint32_t *list = few[team * size], *at = &counts[team * size][2];
+            if (me == 0) *at = 0;
+            if (size > 1) __syncthreads();
+            else __builtin_amdgcn_wave_barrier();
+            if (last)
+                for (int i = me; i < count; i += members) {
+                    const uint32_t key = k[i];
+                    if (key && key != kAlways && (key & mask) == bound) list[atomicAdd(at, 1u)] = key;
+                }
+            if (size > 1) __syncthreads();
+            else __builtin_amdgcn_wave_barrier();
+            if (last) {
+                const uint32_t n = min(in_bin, 64u), own = (uint32_t)lane < n ? list[lane] : 0;
+                uint32_t over = 0, equal = 0;
+                for (uint32_t i = 0; i < n; ++i) {
+                    const uint32_t other = (uint32_t)__builtin_amdgcn_readlane((int)own, (int)i);
+                    over += other > own ? 1u : 0u;
+                    equal += other == own ? 1u : 0u;
+                }
+                const unsigned long long has = __ballot((uint32_t)lane < n && over < need && over + equal >= need);
+                const int l = __ffsll(has) - 1;
+                bound = (uint32_t)__shfl((int)own, l);
+                need -= (uint32_t)__shfl((int)over, l);
             }
             if (size > 1) __syncthreads();
         }
