@@ -446,6 +446,7 @@ typedef struct pk_kv pk_kv;
 
 #define PK_KV_MAX_DIM 256    /* head_dim: a multiple of 8                              */
 #define PK_KV_MAX_SEQS 65535 /* sequences of one batch                                 */
+/* (and 2^30 tokens of a sequence)                                                      */
 
 typedef struct {
     int64_t n_pages;
@@ -461,7 +462,8 @@ typedef struct {
  * offsets[s] .. offsets[s + 1] - 1 of the call's arrays.  Position p lies in page tables[s][p / page_tokens]; an entry outside
  * [0, n_pages) is a page that the sequence has not (or no longer): nothing is written to it, read from it (zeros) or
  * attended to.  Sequences may share pages that neither appends to in this call.
- * The HOST numbers bound what the DEVICE arrays hold: whatever is beyond them is left out.
+ * The HOST numbers bound what the DEVICE arrays hold: whatever is beyond them is left out, and rows of outputs that belong to
+ * no token of a sequence are left as they are.  (max_len may be generous: it fixes how the keys are cut into parts.)
  */
 typedef struct {
     const int32_t *tables;  /* DEVICE [n_seqs] rows of n_cols entries                  */

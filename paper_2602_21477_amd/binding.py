@@ -526,13 +526,16 @@ class KVBatch:
             raise ValueError("a batch has tables [sequence, page], offsets [sequence + 1] and lens [sequence]")
         if not tables.is_cuda or tables.dtype != torch.int32 or (tables.shape[1] > 1 and tables.stride(1) != 1):
             raise ValueError("tables: need an int32 CUDA tensor with its rows' entries side by side")
-        self.tables, self.offsets, self.lens, self.n_tokens = tables, offsets, lens, n_tokens
+        if offsets.device != tables.device or lens.device != tables.device:
+            raise ValueError("tables, offsets and lens are on different devices")
+        self.tables, self.offsets, self.lens, self.n_tokens, self.device = tables, offsets, lens, n_tokens, tables.get_device()
         self.c = pk_kv_batch(tables.data_ptr(), _dev(offsets, torch.int32, "offsets"), _dev(lens, torch.int32, "lens"),
                              tables.stride(0) if n > 1 else max(tables.stride(0), tables.shape[1]), n, tables.shape[1], n_tokens, max_new, max_len)
 
 
 class KVCache:
-    """Convenience owner of one cache's handle and its arena tensor (no arithmetic here)."""
+    """Convenience owner of one cache's handle and its arena tensor (no arithmetic here).  Calls go to the current stream of the
+    cache's device, which has to be the current device."""
 
     def __init__(self, n_pages, n_heads, head_dim, storage=PK_BF16, page_tokens=64, device="cuda"):
         self.cfg = pk_kv_config(n_pages, n_heads, head_dim, page_tokens, storage)
@@ -549,20 +552,27 @@ class KVCache:
         s = t.shape
         if len(s) != 3 or s[0] != batch.n_tokens or s[2] != self.head_dim or (heads and s[1] != heads):
             raise ValueError(f"{what}: need [{batch.n_tokens}, {heads or 'heads'}, {self.head_dim}], got {list(s)}")
-        if t.get_device() != self.device:
-            raise ValueError(f"{what}: is on {t.device}, the cache on {self.arena.device}")
+        if t.get_device() != self.device or batch.device != self.device:
+            raise ValueError(f"{what} is on {t.device}, the batch on device {batch.device}, the cache on {self.arena.device}")
 
     def append(self, k, v, batch):
+        """Writes the batch's new tokens, rows [token, head, channel] of any strides."""
         self._shape(k, batch, self.n_heads, "k")
         self._shape(v, batch, self.n_heads, "v")
         pk_kv_append(self.handle, batch.c, k, v)
 
     def read(self, batch, dtype):
+        """Keys and values of the batch's tokens as they are stored, [token, head, channel] of dtype."""
+        if batch.device != self.device:
+            raise ValueError(f"the batch is on device {batch.device}, the cache on {self.arena.device}")
         k, v = torch.empty((2, batch.n_tokens, self.n_heads, self.head_dim), dtype=dtype, device=self.arena.device).unbind(0)
         pk_kv_read(self.handle, batch.c, k, v)
         return k, v
 
     def bounds(self, pages):
+        """Largest and smallest stored key value of every channel of the pages, [page, head, channel]."""
+        if pages.get_device() != self.device:
+            raise ValueError(f"pages: is on {pages.device}, the cache on {self.arena.device}")
         hi, lo = torch.empty((2, pages.numel(), self.n_heads, self.head_dim), dtype=torch.float32, device=self.arena.device).unbind(0)
         pk_kv_bounds(self.handle, pages, hi, lo)
         return hi, lo
@@ -572,20 +582,23 @@ class KVCache:
         return out, torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if want_lse else None
 
     def attend(self, q, batch, scale, window=0, want_lse=False):
+        """Attention of the new tokens over their sequences: out, or (out, lse)."""
         self._shape(q, batch, 0, "q")
         out, lse = self._outputs(q, want_lse)
         pk_kv_attend(self.handle, batch.c, q, scale, window, out, lse)
         return (out, lse) if want_lse else out
 
     def select(self, q, batch, n_blocks, sink=1, local=2):
+        """Blocks that each new token attends to, [token, key/value head, n_blocks], ascending, padded with -1."""
         self._shape(q, batch, 0, "q")
         blocks = torch.empty((batch.n_tokens, self.n_heads, n_blocks), dtype=torch.int32, device=q.device)
         pk_kv_select(self.handle, batch.c, q, n_blocks, sink, local, blocks)
         return blocks
 
     def attend_blocks(self, q, blocks, batch, scale, want_lse=False):
+        """Attention of the new tokens over listed blocks: out, or (out, lse)."""
         self._shape(q, batch, 0, "q")
-        if blocks.dim() != 3 or blocks.shape[0] != batch.n_tokens or blocks.shape[1] != self.n_heads:
+        if blocks.dim() != 3 or blocks.shape[0] != batch.n_tokens or blocks.shape[1] != self.n_heads or blocks.get_device() != self.device:
             raise ValueError(f"blocks: need [{batch.n_tokens}, {self.n_heads}, blocks], got {list(blocks.shape)}")
         out, lse = self._outputs(q, want_lse)
         pk_kv_attend_blocks(self.handle, batch.c, q, scale, blocks, out, lse)

@@ -436,6 +436,7 @@ namespace {
 
 constexpr uint64_t kKvMagic = 0x70616e63616b7631ull;
 constexpr int64_t kMaxUnits = 1 << 22; // workgroups of a launch before they are cut into parts: a grid has 32 bits for its threads
+constexpr int64_t kMaxTokens = 1 << 30; // of a sequence: positions and what is added to them fit 32 bits
 constexpr int kMaxHeads = 1024; // key/value heads of a cache, and query heads of one of them
 
 size_t up256(size_t v) { return (v + 255) / 256 * 256; }
@@ -480,7 +481,7 @@ bool live(const pk_kv *kv) { return kv && kv->magic == kKvMagic; }
 bool row_type(int32_t t) { return t == PK_F32 || t == PK_F16 || t == PK_BF16; }
 
 // The batch as the kernels get it.  *none: there is nothing to do.
-int take_batch(const pk_kv_batch *b, KvBatch *o, bool *none)
+int take_batch(const pk_kv *kv, const pk_kv_batch *b, KvBatch *o, bool *none)
 {
     if (!b || b->n_seqs < 0 || b->n_tokens < 0 || b->max_new < 0 || b->max_len < 0 || b->n_cols < 0) return PK_ERR_INVALID_ARG;
     if (b->max_new > b->n_tokens) return PK_ERR_INVALID_ARG;
@@ -488,11 +489,12 @@ int take_batch(const pk_kv_batch *b, KvBatch *o, bool *none)
     *none = b->n_seqs == 0 || b->n_tokens == 0 || b->max_new == 0;
     if (*none) return b->n_tokens > 0 ? PK_ERR_INVALID_ARG : PK_OK; // tokens of no sequence
     if (!b->tables || !b->offsets || !b->lens || b->n_cols < 1 || b->table_stride < b->n_cols || b->max_len < 1) return PK_ERR_INVALID_ARG;
+    if (std::min<int64_t>(b->max_len, (int64_t)b->n_cols * kv->cfg.page_tokens) > kMaxTokens) return PK_ERR_UNSUPPORTED;
     *o = KvBatch{b->tables, b->offsets, b->lens, b->n_seqs, b->n_tokens, b->max_new, b->max_len, b->n_cols, b->table_stride};
     return PK_OK;
 }
 
-int take_rows(const pk_rows *r, KvRows *o, int dim)
+int take_rows(const pk_rows *r, KvRows *o)
 {
     if (!r || !r->data || !row_type(r->dtype) || r->token_stride < 0 || r->head_stride < 0) return PK_ERR_INVALID_ARG;
     if (reinterpret_cast<uintptr_t>(r->data) % (r->dtype == PK_F32 ? 4 : 2)) return PK_ERR_INVALID_ARG;
@@ -503,7 +505,7 @@ int take_rows(const pk_rows *r, KvRows *o, int dim)
 // Queries of a 16-bit type; a cache of a 16-bit storage takes its own type only.
 int take_queries(const pk_kv *kv, const pk_rows *q, int32_t n_q_heads, KvRows *o, int *group)
 {
-    const int rc = take_rows(q, o, kv->cfg.head_dim);
+    const int rc = take_rows(q, o);
     if (rc != PK_OK) return rc;
     if (n_q_heads < 1 || n_q_heads % kv->cfg.n_heads) return PK_ERR_INVALID_ARG;
     *group = n_q_heads / kv->cfg.n_heads;
@@ -518,7 +520,7 @@ int attend(pk_kv *kv, const pk_kv_batch *batch, const pk_rows *q, int32_t n_q_he
     if (!live(kv)) return PK_ERR_BAD_HANDLE;
     KvAttend a{};
     bool none;
-    int rc = take_batch(batch, &a.b, &none);
+    int rc = take_batch(kv, batch, &a.b, &none);
     if (rc != PK_OK) return rc;
     if (window < 0 || !std::isfinite(scale)) return PK_ERR_INVALID_ARG;
     if (none) return PK_OK;
@@ -603,11 +605,11 @@ int pk_kv_append(pk_kv *kv, const pk_kv_batch *batch, const pk_rows *k, const pk
     if (!live(kv)) return PK_ERR_BAD_HANDLE;
     KvBatch b;
     bool none;
-    int rc = take_batch(batch, &b, &none);
+    int rc = take_batch(kv, batch, &b, &none);
     if (rc != PK_OK || none) return rc;
     KvRows kr, vr;
-    rc = take_rows(k, &kr, kv->cfg.head_dim);
-    if (rc == PK_OK) rc = take_rows(v, &vr, kv->cfg.head_dim);
+    rc = take_rows(k, &kr);
+    if (rc == PK_OK) rc = take_rows(v, &vr);
     if (rc != PK_OK) return rc;
     if (k->dtype != v->dtype) return PK_ERR_INVALID_ARG;
     return launch_kv_append(kv->dev, kv->cfg.storage, kv->dp, b, kr, vr, k->dtype, static_cast<hipStream_t>(stream)) == hipSuccess ? PK_OK : PK_ERR_HIP;
@@ -618,7 +620,7 @@ int pk_kv_read(pk_kv *kv, const pk_kv_batch *batch, void *k_out, void *v_out, in
     if (!live(kv)) return PK_ERR_BAD_HANDLE;
     KvBatch b;
     bool none;
-    const int rc = take_batch(batch, &b, &none);
+    const int rc = take_batch(kv, batch, &b, &none);
     if (rc != PK_OK || none) return rc;
     if (!k_out || !v_out || !row_type(dtype) || ((reinterpret_cast<uintptr_t>(k_out) | reinterpret_cast<uintptr_t>(v_out)) & 15)) return PK_ERR_INVALID_ARG;
     return launch_kv_read(kv->dev, kv->cfg.storage, kv->dp, b, k_out, v_out, dtype, static_cast<hipStream_t>(stream)) == hipSuccess ? PK_OK : PK_ERR_HIP;
@@ -655,7 +657,7 @@ int pk_kv_select(pk_kv *kv, const pk_kv_batch *batch, const pk_rows *q, int32_t 
     if (!live(kv)) return PK_ERR_BAD_HANDLE;
     KvBatch b;
     bool none;
-    int rc = take_batch(batch, &b, &none);
+    int rc = take_batch(kv, batch, &b, &none);
     if (rc != PK_OK) return rc;
     if (n_blocks < 1 || sink < 0 || local < 1 || (int64_t)sink + local > n_blocks) return PK_ERR_INVALID_ARG;
     if (n_blocks > kKvMaxSelect || (!none && (std::min<int64_t>(b.max_len, (int64_t)b.cols * kv->cfg.page_tokens) + kv->cfg.page_tokens - 1) / kv->cfg.page_tokens > kKvMaxSelect))
