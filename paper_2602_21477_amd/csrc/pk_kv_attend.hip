@@ -7,7 +7,6 @@
 namespace pk {
 namespace {
 
-constexpr int kFewRows = 64;     // most rows of queries of a sequence and head that are taken 16 at a time
 
 // How the second product's operands are scaled.  The largest weight is 2^top: in half precision that type has the more of its range
 // below it (2^-39 of it is the smallest), in bfloat16 it keeps the products with denormal codes where 32 bits are normal.  Both times a
@@ -584,19 +583,29 @@ __device__ __forceinline__ void meet()
     __builtin_amdgcn_sched_barrier(0);
 }
 
-// The order of N products' instructions: their operands are read from LDS AHEAD of them, and what brings the next tiles in (W writes to LDS,
-// L loads) goes between them, one at a time.
-template <int AHEAD, int N, int EACH, int W, int L>
-__device__ __forceinline__ void in_between()
+// The order of a phase's products: N1 operands of EACH products, then N2 of one, read from LDS AHEAD of them.
+template <int AHEAD, int N1, int EACH, int N2>
+__device__ __forceinline__ void reads_ahead()
 {
     __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        __builtin_amdgcn_sched_group_barrier(0x008, EACH, 0);
-        if (i < N - AHEAD) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-        if (i < W) __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);
-        else if (i < W + L) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+    for (int i = 0; i < N1 + N2; ++i) {
+        if (i < N1) __builtin_amdgcn_sched_group_barrier(0x008, EACH, 0);
+        else __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        if (i < N1 + N2 - AHEAD) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
     }
+}
+
+// The largest of a number's values in a wave.
+__device__ __forceinline__ float over_wave_max(float v)
+{
+    auto with = [](float x, int moved) __attribute__((always_inline)) { return fmaxf(x, __int_as_float(moved)); };
+    v = with(v, __builtin_amdgcn_update_dpp(0, __float_as_int(v), 0xb1, 0xf, 0xf, true));  // lanes 1 0 3 2
+    v = with(v, __builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x4e, 0xf, 0xf, true));  // 2 3 0 1
+    v = with(v, __builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x141, 0xf, 0xf, true)); // 7 6 .. 0
+    v = with(v, __builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x140, 0xf, 0xf, true)); // 15 14 .. 0
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return over_halves_max(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
 }
 
 // Tiles on their way into LDS: their pages, then pieces of K(j) and V(j - 1) in registers, then LDS.
@@ -629,7 +638,7 @@ struct KvTiles {
     uint32_t kpage[PG], vpage[PG], spage; // of K(j), of V(j - 1); of the lane's token of K(j)
     u32x4 kw[KP], vw[KP];
     float ksw, vsw;
-    float unit;       // largest scale of a value so far (of the wave that brings them)
+    float unit, fade; // (of the wave that brings them) largest scale of a value so far, and the one before it in units of it
     uint32_t v_in;    // which of the thread's pieces of V(j - 1) lie in pages that the table has
     bool v_there;     // all of the wave's
     uint32_t in_next; // which of K(j)'s four runs of 16 tokens lie in such pages
@@ -638,7 +647,7 @@ struct KvTiles {
     {
         k = c.k, v = c.v, ks = c.ks, vs = c.vs, table = t;
         n_pages = c.n_pages, H = c.H, h = head, P = c.P, logP = c.logP, len = tokens;
-        spage = 0, ksw = 0.f, vsw = 0.f, in_next = 0, v_in = 0, v_there = true, unit = 1e-30f;
+        spage = 0, ksw = 0.f, vsw = 0.f, in_next = 0, v_in = 0, v_there = true, unit = 1e-30f, fade = 1.f;
     }
     // page of a position, of the nearest that the sequence has where it has none there
     __device__ __forceinline__ uint32_t page_of(int pos) const { return (uint32_t)table[min(max(pos, 0), max(len - 1, 0)) >> logP]; }
@@ -670,6 +679,15 @@ struct KvTiles {
             asm volatile("" : "+v"(kpage[0]), "+v"(vpage[0]));
             const uint32_t kp = (uint32_t)same((int)kpage[0]), vp = (uint32_t)same((int)vpage[0]);
             const char *kr = k + (place(kp) * P + (kb & (P - 1))) * DP * ES, *vr = v + (place(vp) * P + (vb & (P - 1))) * DP * ES;
+            in_next = kp < n_pages ? 15u : 0u;
+            if constexpr (CODED) { // (first: loads come back in their order, and the scales are wanted before the rest)
+                const size_t at = place(kp) * P + (kb & (P - 1));
+                const float *ksr = ks + at, *vsr = vs + at;
+                uint32_t by = lane;
+                asm volatile("" : "+v"(by)); // (added to the tile's address: kept as addresses of their own over the loop, these went to scratch)
+                if (wave == 0) ksw = ksr[by];
+                if (wave == 1) vsw = in_next && kb + lane < len ? vsr[by] : 0.f;
+            }
             if (mine) {
 #pragma unroll
                 for (int i = 0; i < KP; ++i) {
@@ -678,14 +696,8 @@ struct KvTiles {
                     vw[i] = *reinterpret_cast<const u32x4 *>(vr + (uint32_t)(p * 16));
                 }
             }
-            in_next = kp < n_pages ? 15u : 0u;
             v_there = vp < n_pages;
             v_in = v_there ? ~0u : 0u;
-            if constexpr (CODED) {
-                const size_t at = place(kp) * P + (kb & (P - 1));
-                if (wave == 0) ksw = ks[at + lane];
-                if (wave == NW - 1) vsw = in_next && kb + lane < len ? vs[at + lane] : 0.f;
-            }
         } else {
             v_in = 0;
 #pragma unroll
@@ -709,8 +721,21 @@ struct KvTiles {
             if constexpr (CODED) {
                 const size_t at = place(spage) * P + ((kb + lane) & (P - 1));
                 if (wave == 0) ksw = ks[at];
-                if (wave == NW - 1) vsw = ok && kb + lane < len ? vs[at] : 0.f;
+                if (wave == 1) vsw = ok && kb + lane < len ? vs[at] : 0.f;
             }
+        }
+    }
+
+    // The scales of the values that were asked for last, in units of the largest so far: by the wave that brings them, when it has time.
+    __device__ __forceinline__ void weigh()
+    {
+        if constexpr (UNITS) {
+            if (same(threadIdx.x >> 6) != 1) return;
+            asm volatile("" : "+v"(vsw)); // (here, not where it was asked for)
+            const float most = fmaxf(over_wave_max(vsw), unit), per = __builtin_amdgcn_rcpf(most);
+            fade = unit * per;
+            unit = most;
+            vsw *= per;
         }
     }
 
@@ -756,18 +781,11 @@ struct KvTiles {
         }
         if constexpr (CODED) {
             if (wave == 0) lds.scales[j & 3][0][lane] = ksw;
-            if (wave == NW - 1) {
-                if constexpr (UNITS) {
-                    float most = vsw;
-#pragma unroll
-                    for (int d = 1; d < 64; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
-                    most = fmaxf(most, unit);
-                    const float per = 1.f / most;
-                    if (lane == 0) lds.fade[j & 3] = unit * per, lds.unit[j & 3] = most;
-                    unit = most;
-                    vsw *= per;
-                }
+            if (wave == 1) {
                 lds.scales[j & 3][1][lane] = vsw;
+                if constexpr (UNITS) {
+                    if (lane == 0) lds.fade[j & 3] = fade, lds.unit[j & 3] = unit;
+                }
             }
         }
     }
@@ -955,11 +973,13 @@ __global__ __launch_bounds__(NW * 64) void kv_tile_kernel(KvAttend a)
         in.lookup(t0);
         in.fetch(t0);
         in.lookup(t0 + 1);
+        in.weigh();
         in.mask(t0);
         in.store(t0, lds);
         uint32_t held = in.in_next;
         in.fetch(t0 + 1);
         in.lookup(t0 + 2);
+        in.weigh();
         meet();
         if (late) meet();
         for (int t = t0; t < t1; ++t) {
@@ -971,9 +991,10 @@ __global__ __launch_bounds__(NW * 64) void kv_tile_kernel(KvAttend a)
             in.lookup(t + 3);
             pv_products(t);
             qk_products(t);
-            in_between<4, 4 * DT + 2 * KS, 1, 0, 0>();
+            reads_ahead<4, 4 * DT, TWICE ? 2 : 1, 2 * KS>();
             meet();
             weights(t, held);
+            in.weigh();
             held = held_next;
             meet();
         }
@@ -1068,7 +1089,11 @@ hipError_t run(KvAttend a, hipStream_t s)
     const int64_t tiles = std::max<int64_t>(((SPARSE ? (int64_t)a.n_blocks * a.c.P : most) + kKvTile - 1) / kKvTile, 1);
     const int64_t seqs = SPARSE ? a.b.n_tokens : a.b.n_seqs;
     const int64_t rows = SPARSE ? a.G : (int64_t)a.b.max_new * a.G; // of a sequence at most
-    a.few_rows = SPARSE ? INT32_MAX : kFewRows;
+    // Most rows of queries of a sequence and head that are taken 16 at a time (above: 256 at a time).  Measured in us, 8 heads of 128 channels, 16
+    // (256) at a time: bf16, 16 sequences of 64 rows over 8192 keys 182 (168), of 128 rows 309 (171), one of 64 rows over 32768 keys 54 (63), of
+    // 128 rows 94 (65).  Codes of 8 bits cost the kernel for many more work for each tile, and half the reads here: int8, 16 sequences of 64 rows
+    // 115 (209), of 128 rows 214 (214), of 256 rows 382 (236); one of 128 rows over 32768 keys 65 (78), of 256 rows 112 (85).
+    a.few_rows = SPARSE ? INT32_MAX : kv_coded<S> ? 128 : 64;
     a.part_row = DP;
     // sequences of few rows: unless all have the same number of new tokens, and that is many
     const bool alike = !SPARSE && (int64_t)a.b.n_seqs * a.b.max_new == a.b.n_tokens;
