@@ -26,13 +26,46 @@ __device__ __forceinline__ float group_max(float v, int gp)
     return v;
 }
 
+// What `f`, whose order does not matter, makes of a number's values in a wave.
+template <class F>
+__device__ __forceinline__ uint32_t over_wave(uint32_t v, F f)
+{
+    v = f(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xb1, 0xf, 0xf, true));  // lanes 1 0 3 2
+    v = f(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4e, 0xf, 0xf, true));  // 2 3 0 1
+    v = f(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xf, 0xf, true)); // 7 6 .. 0
+    v = f(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x140, 0xf, 0xf, true)); // 15 14 .. 0
+    const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    v = f(r[0], r[1]);
+    const auto q = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return f(q[0], q[1]);
+}
+// The sum of the lanes above this one.
+__device__ __forceinline__ uint32_t sum_above(uint32_t v)
+{
+    uint32_t s = v;
+    s += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)s, 0x101, 0xf, 0xf, true); // of the next lane of 16, zero past the last
+    s += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)s, 0x102, 0xf, 0xf, true);
+    s += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)s, 0x104, 0xf, 0xf, true);
+    s += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)s, 0x108, 0xf, 0xf, true);
+    const uint32_t b = (uint32_t)__builtin_amdgcn_readlane((int)s, 16), c = (uint32_t)__builtin_amdgcn_readlane((int)s, 32);
+    const uint32_t d = (uint32_t)__builtin_amdgcn_readlane((int)s, 48);
+    const int g = (int)(threadIdx.x >> 4 & 3);
+    return s - v + (g < 3 ? d : 0) + (g < 2 ? c : 0) + (g < 1 ? b : 0);
+}
+// Four of the keys at once, `step` apart: none (0) from `end` on.
+__device__ __forceinline__ void four_keys(uint32_t (&key)[4], const uint32_t *k, int i, int step, int end)
+{
+#pragma unroll
+    for (int j = 0; j < 4; ++j) key[j] = i + j * step < end ? k[i + j * step] : 0;
+}
+
 struct KvSelect {
     KvDev c;
     KvBatch b;
     KvRows q;
     int32_t G, n, sink, local;
-    int32_t gp;     // columns of a token: its query heads, a power of two of 16 at most
-    int32_t tokens; // of a workgroup: 16 / gp at most, a power of two
+    int32_t gp, log_gp;         // columns of a token: its query heads, a power of two of 16 at most
+    int32_t tokens, log_tokens; // of a workgroup: 16 / gp at most, a power of two
     int32_t groups; // of tokens, of one sequence
     int32_t room;   // keys of a token in LDS
     int32_t *out;
@@ -55,6 +88,7 @@ __global__ __launch_bounds__(NW * 64) void kv_select_kernel(KvSelect a)
     __shared__ __align__(16) u32x4 turn[NW][64];
     __shared__ uint32_t hist[NW][256];
     __shared__ uint32_t counts[NW][3], found[NW][2], few[NW][64];
+    __shared__ uint32_t goes[3][NW]; // whether a token's waves have more to do
     const KvDev c = a.c;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 15, g = lane >> 4;
     const int h = blockIdx.x % c.H, unit = blockIdx.x / c.H, seq = unit / a.groups, first = (unit - seq * a.groups) * a.tokens;
@@ -63,7 +97,7 @@ __global__ __launch_bounds__(NW * 64) void kv_select_kernel(KvSelect a)
     const int32_t *table = a.b.tables + (size_t)seq * a.b.table_stride;
     const int start = sq.len - sq.m;
     const int last_pos = start + min(first + a.tokens, sq.m) - 1, nb = last_pos < 0 ? 0 : (last_pos >> c.logP) + 1; // blocks of its last token
-    const int tk = col / a.gp, member0 = col % a.gp;
+    const int tk = col >> a.log_gp, member0 = col & (a.gp - 1);
     const int pos = start + first + tk, mine = pos >> c.logP; // (pos < 0: nothing is seen)
     const bool token_in = tk < a.tokens && first + tk < sq.m;
 
@@ -159,63 +193,72 @@ __global__ __launch_bounds__(NW * 64) void kv_select_kernel(KvSelect a)
     }
     __syncthreads();
 
-    // ---- the choice: waves `team` to `team + size - 1` have a token (more tokens than waves: several in turn)
-    const int size = min(max(NW / a.tokens, 1), kTeam), turns = max(a.tokens / NW, 1);
-    const int team = wave / size, rank = wave - team * size, members = size * 64, me = rank * 64 + lane;
+    // ---- the choice: waves `team` to `team + size - 1` have a token (more tokens than waves: several in turn, a wave each)
+    constexpr int kLogWaves = NW == 16 ? 4 : 2, kLogTeam = kTeam == 4 ? 2 : 0;
+    static_assert(NW == 1 << kLogWaves && kTeam == 1 << kLogTeam, "");
+    const int log_size = min(max(kLogWaves - a.log_tokens, 0), kLogTeam), size = 1 << log_size, turns = max(a.tokens >> kLogWaves, 1);
+    const int team = wave >> log_size, rank = wave & (size - 1), members = size * 64, me = rank * 64 + lane, teams = NW >> log_size;
+    // where waves share a token, all of the workgroup meet: whether any token's have more to do
+    auto meet = [&](int slot, bool go) __attribute__((always_inline)) {
+        if (me == 0) goes[slot][team] = go;
+        __syncthreads();
+        const uint32_t v = lane < teams ? goes[slot][lane] : 0;
+        return __ballot(v != 0) != 0;
+    };
     for (int u = 0; u < turns; ++u) {
         const int t = team + u * NW; // (u > 0 only where a wave has tokens of its own)
         const bool have = t < a.tokens && first + t < sq.m;
         const uint32_t *k = keys + (have ? t : 0) * a.room;
         const int count = have ? nb : 0;
-        // how many there are, how many of them in any case, and the first bit in which the others differ
-        uint32_t always = 0, others = 0, low = 0xffffffffu, high = 0;
-        for (int i = me; i < count; i += members) {
-            const uint32_t key = k[i];
-            if (key == kAlways) ++always;
-            else if (key) {
-                ++others;
-                low = min(low, key);
-                high = max(high, key);
+        // how many there are, how many of them in any case (both fit 16 bits, as LDS holds them), and the first bit in which the others differ
+        uint32_t both = 0, low = 0xffffffffu, high = 0;
+        for (int i = me; i < count; i += 4 * members) {
+            uint32_t key[4];
+            four_keys(key, k, i, members, count);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const bool other = key[j] && key[j] != kAlways;
+                both += key[j] == kAlways ? 1u : other ? 1u << 16 : 0u;
+                low = min(low, other ? key[j] : 0xffffffffu);
+                high = max(high, other ? key[j] : 0u);
             }
         }
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) {
-            always += (uint32_t)__shfl_xor((int)always, d);
-            others += (uint32_t)__shfl_xor((int)others, d);
-            low = min(low, (uint32_t)__shfl_xor((int)low, d));
-            high = max(high, (uint32_t)__shfl_xor((int)high, d));
-        }
+        both = over_wave(both, [](uint32_t x, uint32_t y) { return x + y; });
+        low = over_wave(low, [](uint32_t x, uint32_t y) { return min(x, y); });
+        high = over_wave(high, [](uint32_t x, uint32_t y) { return max(x, y); });
         if (size > 1) {
-            if (lane == 0) counts[wave][0] = always, counts[wave][1] = others, found[wave][0] = low, found[wave][1] = high;
+            if (lane == 0) counts[wave][0] = both, found[wave][0] = low, found[wave][1] = high;
             __syncthreads();
-            always = others = high = 0, low = 0xffffffffu;
+            both = high = 0, low = 0xffffffffu;
             for (int w = 0; w < size; ++w) {
-                always += counts[team * size + w][0];
-                others += counts[team * size + w][1];
+                both += counts[team * size + w][0];
                 low = min(low, found[team * size + w][0]);
                 high = max(high, found[team * size + w][1]);
             }
-            __syncthreads();
         }
+        const uint32_t always = both & 0xffff, others = both >> 16;
         uint32_t need = (uint32_t)a.n > always ? (uint32_t)a.n - always : 0;
         // of the keys that are not taken in any case: all where there are no more than that, else those above `bound` and `need` of those equal to it
         const bool all = others <= need, none = need == 0;
         int bits = all || none || low == high ? 0 : 32 - __clz((int)(low ^ high));
         uint32_t mask = bits == 32 ? 0u : ~0u << bits, bound = none ? kAlways : high & mask;
-        uint32_t *hs = hist[team * size];
         uint32_t in_bin = others; // keys that agree with `bound` in `mask`
-        // (where waves share a token, all of the workgroup go through each round, as they meet in it)
         for (int round = 0; round < 4; ++round) {
             const bool go = bits > 0 && in_bin > 64;
-            if (size == 1 ? !go : !__syncthreads_or(go)) break;
+            if (size == 1 && !go) break;
+            // (waves that share a token have two histograms in turn: one is cleared while some may still read the other)
+            uint32_t *hs = hist[team * size + (size > 1 ? round & 1 : 0)];
             const int shift = max(bits - 8, 0), width = bits - shift;
             for (int i = me; i < 256; i += members) hs[i] = 0;
-            if (size > 1) __syncthreads();
-            else __builtin_amdgcn_wave_barrier();
+            if (size == 1) __builtin_amdgcn_wave_barrier();
+            else if (!meet(round & 1, go)) break;
             if (go)
-                for (int i = me; i < count; i += members) {
-                    const uint32_t key = k[i];
-                    if (key && key != kAlways && (key & mask) == bound) atomicAdd(&hs[(key >> shift) & ((1u << width) - 1)], 1u);
+                for (int i = me; i < count; i += 4 * members) {
+                    uint32_t key[4];
+                    four_keys(key, k, i, members, count);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (key[j] && key[j] != kAlways && (key[j] & mask) == bound) atomicAdd(&hs[(key[j] >> shift) & ((1u << width) - 1)], 1u);
                 }
             if (size > 1) __syncthreads();
             else __builtin_amdgcn_wave_barrier();
@@ -226,13 +269,7 @@ __global__ __launch_bounds__(NW * 64) void kv_select_kernel(KvSelect a)
                 own[j] = hs[lane * 4 + j];
                 sum += own[j];
             }
-            uint32_t above = sum;
-#pragma unroll
-            for (int d = 1; d < 64; d *= 2) {
-                const uint32_t v = (uint32_t)__shfl_down((int)above, d);
-                if (lane + d < 64) above += v;
-            }
-            above -= sum;
+            uint32_t above = sum_above(sum);
             int bin = -1;
             uint32_t left = 0, size_of = 0;
 #pragma unroll
@@ -256,15 +293,17 @@ __global__ __launch_bounds__(NW * 64) void kv_select_kernel(KvSelect a)
         }
         // 64 keys at most are left: each lane has one and counts those above it
         const bool last = bits > 0;
-        if (size > 1 ? __syncthreads_or(last) : last) {
-            uint32_t *list = few[team * size], *at = &counts[team * size][2];
-            if (me == 0) *at = 0;
-            if (size > 1) __syncthreads();
-            else __builtin_amdgcn_wave_barrier();
+        uint32_t *list = few[team * size], *listed = &counts[team * size][2];
+        if (me == 0) *listed = 0;
+        if (size == 1) __builtin_amdgcn_wave_barrier();
+        if (size > 1 ? meet(2, last) : last) {
             if (last)
-                for (int i = me; i < count; i += members) {
-                    const uint32_t key = k[i];
-                    if (key && key != kAlways && (key & mask) == bound) list[atomicAdd(at, 1u)] = key;
+                for (int i = me; i < count; i += 4 * members) {
+                    uint32_t key[4];
+                    four_keys(key, k, i, members, count);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (key[j] && key[j] != kAlways && (key[j] & mask) == bound) list[atomicAdd(listed, 1u)] = key[j];
                 }
             if (size > 1) __syncthreads();
             else __builtin_amdgcn_wave_barrier();
@@ -281,15 +320,18 @@ __global__ __launch_bounds__(NW * 64) void kv_select_kernel(KvSelect a)
                 bound = (uint32_t)__shfl((int)own, l);
                 need -= (uint32_t)__shfl((int)over, l);
             }
-            if (size > 1) __syncthreads();
         }
         // each wave has a stretch of the blocks: what it takes before the equal ones, the equal ones, and where they go
-        const int stretch = (((count + size - 1) / size) + 63) / 64 * 64, i0 = rank * stretch, i1 = min(i0 + stretch, count);
+        const int stretch = (((count + size - 1) >> log_size) + 63) & ~63, i0 = rank * stretch, i1 = min(i0 + stretch, count);
         uint32_t over = 0, equal = 0;
-        for (int i = i0; i < i1; i += 64) {
-            const uint32_t key = i + lane < i1 ? k[i + lane] : 0;
-            over += (uint32_t)__popcll(__ballot(key == kAlways || (key && (all || key > bound))));
-            equal += (uint32_t)__popcll(__ballot(key && key != kAlways && !all && key == bound));
+        for (int i = i0; i < i1; i += 256) {
+            uint32_t key[4];
+            four_keys(key, k, i + lane, 64, i1);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                over += (uint32_t)__popcll(__ballot(key[j] == kAlways || (key[j] && (all || key[j] > bound))));
+                equal += (uint32_t)__popcll(__ballot(key[j] && key[j] != kAlways && !all && key[j] == bound));
+            }
         }
         uint32_t equal_before = 0, place = 0;
         if (size > 1) {
@@ -305,21 +347,25 @@ __global__ __launch_bounds__(NW * 64) void kv_select_kernel(KvSelect a)
         }
         int32_t *o = a.out + ((size_t)(sq.first + min(first + t, sq.m - 1)) * c.H + h) * a.n;
         const unsigned long long below = (1ull << lane) - 1;
-        for (int i = i0; i < i1; i += 64) {
-            const uint32_t key = i + lane < i1 ? k[i + lane] : 0;
-            const bool is = key && key != kAlways && !all && key == bound;
-            const unsigned long long eq = __ballot(is);
-            const bool take = key == kAlways || (key && !is && (all || key > bound)) || (is && equal_before + (uint32_t)__popcll(eq & below) < need);
-            const unsigned long long tk2 = __ballot(take);
-            const uint32_t to = place + (uint32_t)__popcll(tk2 & below);
-            if (take && to < (uint32_t)a.n) o[to] = i + lane;
-            place += (uint32_t)__popcll(tk2);
-            equal_before += (uint32_t)__popcll(eq);
+        for (int i = i0; i < i1; i += 256) {
+            uint32_t key[4];
+            four_keys(key, k, i + lane, 64, i1);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const bool is = key[j] && key[j] != kAlways && !all && key[j] == bound;
+                const unsigned long long eq = __ballot(is);
+                const uint32_t nth = equal_before + (uint32_t)__popcll(eq & below);
+                const bool take = key[j] == kAlways || (key[j] && !is && (all || key[j] > bound)) || (is && nth < need);
+                const unsigned long long taken = __ballot(take);
+                const uint32_t to = place + (uint32_t)__popcll(taken & below);
+                if (take && to < (uint32_t)a.n) o[to] = i + j * 64 + lane;
+                place += (uint32_t)__popcll(taken);
+                equal_before += (uint32_t)__popcll(eq);
+            }
         }
         // the last wave knows how many there are in all
         if (have && rank == size - 1)
             for (int i = (int)place + lane; i < a.n; i += 64) o[i] = -1;
-        if (size > 1) __syncthreads();
     }
 }
 
@@ -339,12 +385,14 @@ hipError_t run_waves(KvSelect a, int num_cu, hipStream_t s)
 {
     const int64_t most = ((int64_t)a.b.max_len + a.c.P - 1) / a.c.P;
     a.room = (int32_t)std::max<int64_t>(std::min<int64_t>(most, a.b.cols), 1);
-    a.gp = 1;
-    while (a.gp < a.G && a.gp < 16) a.gp *= 2;
+    a.log_gp = 0;
+    while ((1 << a.log_gp) < a.G && a.log_gp < 4) ++a.log_gp;
+    a.gp = 1 << a.log_gp;
     // as many tokens as 16 columns have, as a sequence has, and as LDS has room for the keys of (two workgroups a CU at least, unless one
     // token alone takes more)
     a.tokens = 16 / a.gp;
     while (a.tokens > 1 && (a.tokens / 2 >= a.b.max_new || (int64_t)a.tokens * a.room * 4 > (48 << 10))) a.tokens /= 2;
+    a.log_tokens = __builtin_ctz((unsigned)a.tokens);
     a.groups = (a.b.max_new + a.tokens - 1) / a.tokens;
     const int64_t grid = (int64_t)a.b.n_seqs * a.groups * a.c.H;
     const size_t lds = (size_t)a.tokens * a.room * 4;
