@@ -79,7 +79,9 @@ struct KvSelect {
 // the lanes that the product wants by way of LDS.  The keys of the scores stay there; a token's n-th largest is found by its
 // bytes, from the first one in which its keys differ, one histogram each, by the waves that have the token (all of them, where it is the only one); each
 // of these then has a stretch of the blocks, and what is chosen comes out in ascending order.
-// Bound by reading the bounds where there are few tokens (16 waves then), by the steps of the choice where there are many.
+// Bound by reading the bounds where there are few tokens (16 waves then), by the steps of the choice where there are many.  Measured, 8 heads
+// of 128, 4 query heads each: one token with 313 blocks 12.8 us, 16 tokens with 2048 each 26 us (67 MB of bounds, 13 us at the rate of a large
+// copy), 1024 tokens with 512 52 us.
 template <int T, int DP, int NW>
 __global__ __launch_bounds__(NW * 64) void kv_select_kernel(KvSelect a)
 {
@@ -396,7 +398,8 @@ hipError_t run_waves(KvSelect a, int num_cu, hipStream_t s)
     a.groups = (a.b.max_new + a.tokens - 1) / a.tokens;
     const int64_t grid = (int64_t)a.b.n_seqs * a.groups * a.c.H;
     const size_t lds = (size_t)a.tokens * a.room * 4;
-    // few workgroups: 16 waves each, while LDS has room for what they need beside the keys
+    // few workgroups: 16 waves each, while LDS has room for what they need beside the keys (one token with 313 blocks 12.9 us, 4 waves 13.9; 16
+    // with 2048 26.7, 4 waves 50.7; many workgroups: 1024 tokens with 512 122 us, 4 waves 52.9)
     if (grid <= 2 * num_cu && lds <= (120u << 10)) return run<T, DP, 16>(a, (unsigned)grid, lds, s);
     return run<T, DP, 4>(a, (unsigned)grid, lds, s);
 }
