@@ -807,9 +807,10 @@ struct KvTiles {
 // On its way a tile is in registers, asked for a round before it is written, and is converted to the queries' type once for all waves.
 // The running maximum is of the bare products (the queries carry the scale's sign); O is rescaled only when some query's maximum
 // has grown.  ONE: a tile of keys lies in one page.
-// Measured, bf16, 32 query heads of 128 channels: 4096 tokens over 32768 2.02 - 2.09 ms, 1.0 PFLOP/s, matrix cores busy 45 % of the cycles at
-// a clock that falls to 1.64 GHz, so that fewer cycles no longer give less time (5.9 to 4.4 million cycles: 2.01 to 2.02 ms); a product of
-// 8192 x 8192 x 8192 runs at 1.2 - 1.35 PFLOP/s on such numbers.  First form, each read waited for: 2.71 ms.
+// Measured, bf16, 32 query heads of 128 channels: 4096 tokens over 32768 2.02 - 2.09 ms, 1.0 PFLOP/s.  4.36 million cycles, of which the matrix
+// cores are busy for 45 % and the reads of K and V out of LDS by eight waves take about as many, at 2.08 GHz: the power that the products draw
+// holds the clock there (the same launch over zeros 1.76 ms, at 2.4 GHz).  A product of 8192 x 8192 x 8192 runs at 1.2 - 1.35 PFLOP/s on
+// such numbers, 1.8 on zeros.  First form, each read waited for: 2.71 ms.
 template <int S, int T, int DP, int NW, bool ONE>
 __global__ __launch_bounds__(NW * 64) void kv_tile_kernel(KvAttend a)
 {
