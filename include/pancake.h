@@ -446,7 +446,7 @@ typedef struct pk_kv pk_kv;
 
 #define PK_KV_MAX_DIM 256    /* head_dim: a multiple of 8                              */
 #define PK_KV_MAX_SEQS 65535 /* sequences of one batch                                 */
-/* (and 2^30 tokens of a sequence)                                                      */
+/* (and 2^30 tokens of a sequence, 2^23 pages of it in one append or read)              */
 
 typedef struct {
     int64_t n_pages;

@@ -221,7 +221,7 @@ struct KvAttend {
     uint32_t *arrivals;    // parts of a row tile that have ended, zeros between calls: kKvArrivals of them
     int32_t num_cu;
     // set by the launch
-    int32_t few_rows;      // sequences with more rows of queries than this are taken by the kernel for many
+    int32_t few_rows;      // sequences with more rows of queries than this (kKvFewRows at most) are taken by the kernel for many
     int32_t row_tiles;     // of one sequence (sparse: of one token)
     int32_t part_row;      // floats of a row of partial results
     int32_t join_here;     // the kernel for few rows joins its parts itself
@@ -236,6 +236,7 @@ hipError_t launch_kv_select(const KvDev &c, int dp, const KvBatch &b, const KvRo
 hipError_t launch_kv_attend(const KvAttend &a, int storage, int dp, int dtype, hipStream_t s);
 
 constexpr int kKvTile = 64;          // keys of one step of the attention kernels
+constexpr int kKvFewRows = 128;      // rows of queries of a sequence and head that the kernel for few takes at most
 constexpr int64_t kKvPartFloats = 16 << 20; // partial results that a cache's workspace has room for: 512 workgroups' of 256 rows of 128 channels
 constexpr int kKvArrivals = 4096;
 constexpr int kKvMaxPage = 128;

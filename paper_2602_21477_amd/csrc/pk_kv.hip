@@ -343,7 +343,7 @@ __global__ __launch_bounds__(kThreads) void kv_bounds_kernel(KvDev c, int dp, co
 // pages that one sequence's new tokens can touch
 int touched(const KvDev &c, const KvBatch &b)
 {
-    return std::min((b.max_new + c.P - 2) / c.P + 1, b.cols);
+    return (int)std::min<int64_t>(((int64_t)b.max_new + c.P - 2) / c.P + 1, b.cols);
 }
 
 // A launch with LDS for a page's keys and values.
@@ -442,6 +442,7 @@ namespace {
 
 constexpr uint64_t kKvMagic = 0x70616e63616b7631ull;
 constexpr int64_t kMaxUnits = 1 << 22; // workgroups of a launch before they are cut into parts: a grid has 32 bits for its threads
+constexpr int kMaxTouched = 1 << 23;   // pages of one sequence that a call writes or reads: the same
 constexpr int64_t kMaxTokens = 1 << 30; // of a sequence: positions and what is added to them fit 32 bits
 constexpr int kMaxHeads = 1024; // key/value heads of a cache, and query heads of one of them
 
@@ -541,7 +542,9 @@ int attend(pk_kv *kv, const pk_kv_batch *batch, const pk_rows *q, int32_t n_q_he
     a.out = static_cast<char *>(out);
     a.lse = lse;
     a.num_cu = kv->num_cu;
-    const int64_t H = kv->cfg.n_heads, units = blocks ? (int64_t)a.b.n_tokens * ((a.G + 15) / 16) : std::max<int64_t>(a.b.n_seqs * 4, (int64_t)a.b.n_tokens * a.G / 128 + a.b.n_seqs);
+    const int64_t H = kv->cfg.n_heads, rows = (int64_t)a.b.n_tokens * a.G;
+    const int64_t few = a.b.n_seqs * std::min<int64_t>(((int64_t)a.b.max_new * a.G + 15) / 16, kKvFewRows / 16);
+    const int64_t units = blocks ? (int64_t)a.b.n_tokens * ((a.G + 15) / 16) : std::max<int64_t>(few, rows / 128 + a.b.n_seqs);
     if (units * H > kMaxUnits) return PK_ERR_UNSUPPORTED;
     a.part = reinterpret_cast<float *>(kv->ws);
     a.part_floats = kKvPartFloats;
@@ -618,6 +621,7 @@ int pk_kv_append(pk_kv *kv, const pk_kv_batch *batch, const pk_rows *k, const pk
     if (rc == PK_OK) rc = take_rows(v, &vr);
     if (rc != PK_OK) return rc;
     if (k->dtype != v->dtype) return PK_ERR_INVALID_ARG;
+    if (touched(kv->dev, b) > kMaxTouched) return PK_ERR_UNSUPPORTED;
     return launch_kv_append(kv->dev, kv->cfg.storage, kv->dp, b, kr, vr, k->dtype, static_cast<hipStream_t>(stream)) == hipSuccess ? PK_OK : PK_ERR_HIP;
 }
 
@@ -629,6 +633,7 @@ int pk_kv_read(pk_kv *kv, const pk_kv_batch *batch, void *k_out, void *v_out, in
     const int rc = take_batch(kv, batch, &b, &none);
     if (rc != PK_OK || none) return rc;
     if (!k_out || !v_out || !row_type(dtype) || ((reinterpret_cast<uintptr_t>(k_out) | reinterpret_cast<uintptr_t>(v_out)) & 15)) return PK_ERR_INVALID_ARG;
+    if (touched(kv->dev, b) > kMaxTouched) return PK_ERR_UNSUPPORTED;
     return launch_kv_read(kv->dev, kv->cfg.storage, kv->dp, b, k_out, v_out, dtype, static_cast<hipStream_t>(stream)) == hipSuccess ? PK_OK : PK_ERR_HIP;
 }
 

@@ -1100,7 +1100,7 @@ hipError_t run(KvAttend a, hipStream_t s)
     // (256) at a time: bf16, 16 sequences of 64 rows over 8192 keys 182 (168), of 128 rows 309 (171), one of 64 rows over 32768 keys 54 (63), of
     // 128 rows 94 (65).  Codes of 8 bits cost the kernel for many more work for each tile, and half the reads here: int8, 16 sequences of 64 rows
     // 115 (209), of 128 rows 214 (214), of 256 rows 382 (236); one of 128 rows over 32768 keys 65 (78), of 256 rows 112 (85).
-    a.few_rows = SPARSE ? INT32_MAX : kv_coded<S> ? 128 : 64;
+    a.few_rows = SPARSE ? INT32_MAX : kv_coded<S> ? kKvFewRows : 64;
     a.part_row = DP;
     // sequences of few rows: unless all have the same number of new tokens, and that is many
     const bool alike = !SPARSE && (int64_t)a.b.n_seqs * a.b.max_new == a.b.n_tokens;

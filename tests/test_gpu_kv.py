@@ -224,6 +224,18 @@ def test_attention_in_parts(gpu_device, storage, dtype, shape):
 
 
 @pytest.mark.parametrize("storage,dtype", [("bf16", "bf16"), ("i8", "bf16"), ("i8", "f16"), ("f8", "bf16")])
+@pytest.mark.parametrize("P", [16, 64])
+@pytest.mark.parametrize("news", [[32], [33], [64], [65], [32, 33, 64, 65, 1], [129, 0, 128]], ids=str)
+def test_either_side_of_few_rows(gpu_device, storage, dtype, P, news):
+    """Sequences of 64, 66, 128 and 130 rows of queries: the kernel for few takes 64 of 16 bits at most, 128 of 8."""
+    s = Setup(storage, dtype, 1, 2, 128, P, news, [n + 150 for n in news], seed=21)
+    scale = 128 ** -0.5
+    key = [torch.arange(l) for l in s.lens]
+    out, lse = s.cache.attend(s.q.cuda(), s.batch, scale, want_lse=True)
+    s.check(out, lse.cpu(), scale, lambda row, i, pos, h: key[i] <= pos)
+
+
+@pytest.mark.parametrize("storage,dtype", [("bf16", "bf16"), ("i8", "bf16"), ("i8", "f16"), ("f8", "bf16")])
 @pytest.mark.parametrize("scale", [-0.07, 0.0, 3.0])
 def test_scales_of_any_sign(gpu_device, storage, dtype, scale):
     for news in ([2, 1], [90, 1]):
@@ -496,3 +508,17 @@ def test_refusals(gpu_device):
     nothing = B.KVBatch(s.batch.tables, torch.zeros(2, dtype=torch.int32, device="cuda"), s.batch.lens, 0, 0, 20)
     assert s.cache.attend(q[:0], nothing, 0.1).shape == (0, 4, 64)
     s.cache.append(k[:0], k[:0], nothing)
+
+
+def test_batches_beyond_a_launch_are_refused(gpu_device):
+    """Numbers that no launch could take are refused by the host, before anything runs."""
+    cache = B.KVCache(1, 1, 8, storage=B.PK_F16, page_tokens=16)
+    one = torch.zeros(8, dtype=torch.int32, device="cuda")
+    rows = torch.zeros((1, 1, 8), dtype=torch.float16, device="cuda")
+    most = 2 ** 31 - 1
+    batch = B.pk_kv_batch(one.data_ptr(), one.data_ptr(), one.data_ptr(), 2 ** 26, 1, 2 ** 26, most, most, 2 ** 30)
+    for call in (lambda: B.pk_kv_append(cache.handle, batch, rows, rows), lambda: B.pk_kv_read(cache.handle, batch, rows, rows.clone()),
+                 lambda: B.pk_kv_attend(cache.handle, batch, rows, 1.0, 0, rows.clone())):
+        with pytest.raises(B.PancakeError) as e:
+            call()
+        assert e.value.status == B.PK_ERR_UNSUPPORTED
