@@ -440,7 +440,7 @@ int pk_index_free(pk_index *index);
  * them may be captured into a graph and replayed with other contents of the batch's DEVICE arrays.  Calls on one handle come from one
  * stream at a time; work on different handles may overlap.  Outputs are valid once the stream is synchronised.
  *
- * Inputs must be finite.  What lies in pages beyond a sequence's length may be anything.
+ * Inputs must be finite, and stay so in a 16-bit storage.  What lies in pages beyond a sequence's length may be anything.
  */
 typedef struct pk_kv pk_kv;
 

@@ -488,7 +488,9 @@ __global__ __launch_bounds__(256, DP * KvBytes<S>::v > 128 ? 1 : 2) void kv_rows
         for (int d = 0; d < DP; d += 64) *reinterpret_cast<f32x4 *>(a.part + pr * DP + d + sub * 4) = joined(d + sub * 4);
     }
     if (!a.join_here) return;
-    // the last of the parts joins them all (what this one wrote is seen by it: release, and acquire where it is the last)
+    // The last of the parts joins them all (what this one wrote is seen by it: release, and acquire where it is the last).  The barrier does not
+    // wait for stores to memory, and the release is one wave's: every wave waits for its own first.
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
     if (tid == 0) {
         __threadfence();
