@@ -221,7 +221,7 @@ struct KvAttend {
     uint32_t *arrivals;    // parts of a row tile that have ended, zeros between calls: kKvArrivals of them
     int32_t num_cu;
     // set by the launch
-    int32_t few_rows;      // sequences with more rows of queries than this (kKvFewRows at most) are taken by the kernel for many
+    int32_t few_rows;      // sequences with more rows of queries than this (kKvFewRows at most; 0 where it runs alone) are taken by the kernel for many
     int32_t row_tiles;     // of one sequence (sparse: of one token)
     int32_t part_row;      // floats of a row of partial results
     int32_t join_here;     // the kernel for few rows joins its parts itself

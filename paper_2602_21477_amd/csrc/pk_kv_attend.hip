@@ -1104,7 +1104,8 @@ hipError_t run(KvAttend a, hipStream_t s)
     // 115 (209), of 128 rows 214 (214), of 256 rows 382 (236); one of 128 rows over 32768 keys 65 (78), of 256 rows 112 (85).
     a.few_rows = SPARSE ? INT32_MAX : kv_coded<S> ? kKvFewRows : 64;
     a.part_row = DP;
-    // sequences of few rows: unless all have the same number of new tokens, and that is many
+    // sequences of few rows: unless all may have the same number of new tokens, and that is many.  (The host's numbers are bounds: sequences
+    // that have fewer after all are then the kernel for many's, as are all that have any)
     const bool alike = !SPARSE && (int64_t)a.b.n_seqs * a.b.max_new == a.b.n_tokens;
     if (SPARSE || !alike || rows <= a.few_rows) {
         a.row_tiles = (int32_t)((std::min<int64_t>(rows, a.few_rows) + 15) / 16);
@@ -1133,6 +1134,7 @@ hipError_t run(KvAttend a, hipStream_t s)
             // row tiles of the sequences that have more rows than the others' kernel takes: at most
             const int64_t all = a.b.n_tokens * (int64_t)a.G, longs = std::min<int64_t>(a.b.n_seqs, all / (a.few_rows + 1));
             const int64_t units = alike ? seqs * ((rows + BR - 1) / BR) : std::min(longs * ((rows + BR - 1) / BR), all / BR + longs);
+            if (alike) a.few_rows = 0;
             cut(a, units * a.c.H, tiles, BR, a.num_cu, 8, (alike ? 1 : 4) * a.num_cu, 16);
             const dim3 grid((unsigned)(units * a.n_split * a.c.H));
             if (a.c.P >= kKvTile) kv_tile_kernel<S, T, DP, NW, true><<<grid, NW * 64, 0, s>>>(a);

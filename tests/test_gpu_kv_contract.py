@@ -1,0 +1,68 @@
+"""What the key/value cache's header promises beside the values: host numbers that only bound the device arrays."""
+import math
+
+import pytest
+import torch
+
+from paper_2602_21477_amd import binding as B
+from test_gpu_kv import Setup
+
+pytestmark = pytest.mark.gpu
+
+def causal(s, window=0):
+    key = [torch.arange(l) for l in s.lens]
+    return lambda row, i, pos, h: (key[i] <= pos) & (key[i] > pos - (window or 1 << 30))
+
+
+def padded(x, rows, value=math.nan):
+    """The rows of x, and more behind them that belong to no token."""
+    return torch.cat([x, torch.full((rows - x.shape[0], *x.shape[1:]), value, dtype=x.dtype)]).cuda()
+
+
+def attend(cache, batch, q, scale, window=0):
+    """(out, lse) over outputs that hold NaN."""
+    out, lse = torch.full_like(q, math.nan), torch.full(q.shape[:2], math.nan, device="cuda")
+    B.pk_kv_attend(cache.handle, batch.c, q, scale, window, out, lse)
+    return out, lse
+
+
+# ------------------------------------------------------------------------------- host numbers are bounds
+
+@pytest.mark.parametrize("storage,dtype", [("bf16", "bf16"), ("i8", "bf16"), ("f8", "f16")])
+@pytest.mark.parametrize("P,D", [(64, 128), (16, 64)])
+@pytest.mark.parametrize("news", [[0], [1], [10], [16], [33], [5, 256], [0, 3], [17, 64], [1, 0, 200]], ids=str)
+def test_fewer_tokens_than_the_host_says(gpu_device, storage, dtype, P, D, news):
+    """n_tokens = n_seqs * max_new on the host, sequences of fewer on the device: each of a batch's rows is written, and no other."""
+    s = Setup(storage, dtype, 2, 4, D, P, news, [n + 70 for n in news], seed=31)
+    n = 256 * len(news)
+    batch = B.KVBatch(s.batch.tables, s.batch.offsets, s.batch.lens, n, 256, max(s.lens) + 300)
+    for window in (0, 40):
+        out, lse = attend(s.cache, batch, padded(s.q, n), D ** -0.5, window)
+        s.check(out, lse.cpu(), D ** -0.5, causal(s, window))
+        assert torch.all(out[sum(news):].isnan()) and torch.all(lse[sum(news):].isnan())
+
+
+@pytest.mark.parametrize("storage,dtype", [("bf16", "bf16"), ("i8", "f16")])
+def test_chunks_in_a_graph_follow_the_arrays(gpu_device, storage, dtype):
+    """Chunks captured once, replayed with other offsets and lengths, against 64 bits each time."""
+    s = Setup(storage, dtype, 2, 4, 64, 32, [128, 128], [400, 300], seed=32)
+    offsets, lens = s.batch.offsets.clone(), s.batch.lens.clone()
+    batch = B.KVBatch(s.batch.tables, offsets, lens, 256, 128, 400)
+    q = s.q.cuda()
+    out, lse = torch.empty_like(q), torch.empty(q.shape[:2], device="cuda")
+    B.pk_kv_attend(s.cache.handle, batch.c, q, 0.125, 0, out, lse)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        B.pk_kv_attend(s.cache.handle, batch.c, q, 0.125, 0, out, lse)
+    full = s.q
+    for news, ends in (([128, 128], [400, 300]), ([5, 3], [333, 90]), ([0, 128], [50, 299]), ([128, 1], [128, 300]), ([40, 16], [397, 16])):
+        s.news, s.lens, s.q = news, ends, full[:sum(news)]
+        offsets.copy_(torch.tensor([0, news[0], sum(news)], dtype=torch.int32))
+        lens.copy_(torch.tensor(ends, dtype=torch.int32))
+        out.fill_(math.nan)
+        lse.fill_(math.nan)
+        graph.replay()
+        torch.cuda.synchronize()
+        s.check(out, lse.cpu(), 0.125, causal(s))
+        assert torch.all(out[sum(news):].isnan()) and torch.all(lse[sum(news):].isnan())
