@@ -168,15 +168,14 @@ __global__ __launch_bounds__(256, DP * KvBytes<S>::v > 128 ? 1 : 2) void kv_rows
     const KvSeq sq = kv_seq(a.b, seq, P);
     const int rows = SPARSE ? G : sq.m * G;
     if (tile * RT >= rows || (!SPARSE && rows > a.few_rows)) return;
+    if (SPARSE && (token0 < sq.first || token0 >= sq.first + sq.m)) return; // a token of no sequence: its rows are left as they are
     const int part = R == 1 ? 0 : col / RT, row = tile * RT + col % RT;
     const bool valid = row < rows;
     const int tok = SPARSE ? token0 : sq.first + min(row, rows - 1) / G;
     const int member = min(row, rows - 1) % G;
     const int start = sq.len - sq.m;
-    const int my_pos = start + (tok - sq.first);
-    const bool stray = SPARSE && (tok < sq.first || tok >= sq.first + sq.m); // a token of no sequence
     // columns without a query see every key (what they compute is dropped)
-    const int pos = valid ? (stray ? -1 : my_pos) : 0x7fffffff;
+    const int pos = valid ? start + (tok - sq.first) : 0x7fffffff;
     const int from = valid && !SPARSE && a.window > 0 ? max(pos - a.window + 1, 0) : 0;
     const int32_t *table = a.b.tables + (size_t)seq * a.b.table_stride;
     const int32_t *list = SPARSE ? a.blocks + ((size_t)token0 * c.H + h) * a.n_blocks : nullptr;
@@ -1059,6 +1058,8 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttend a)
     const KvSeq sq = kv_seq(a.b, un.seq, a.c.P);
     const int row = un.tile * BR + r, rows = SPARSE ? a.G : sq.m * a.G;
     if (row >= rows || (BR == 16 && !SPARSE && rows > a.few_rows)) return;
+    const int tok = SPARSE ? unit / a.row_tiles : sq.first + row / a.G;
+    if (SPARSE && (tok < sq.first || tok >= sq.first + sq.m)) return; // (has no parts)
     const size_t at = ((size_t)unit * a.c.H + h) * a.n_split;
     float m = -INFINITY;
     for (int s = 0; s < a.n_split; ++s) m = fmaxf(m, a.part_ml[((at + s) * BR + r) * 2]);
@@ -1076,7 +1077,6 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttend a)
 #pragma unroll
         for (int d = 0; d < DP / 64; ++d) y[d] += w * *reinterpret_cast<const f32x4 *>(a.part + pr * DP + d * 64 + sub * 4);
     }
-    const int tok = SPARSE ? unit / a.row_tiles : sq.first + row / a.G;
     kv_write_row<T, DP>(a, h, tok, row % a.G, sub, m, l, [&](int dd) __attribute__((always_inline)) { return y[dd / 64]; });
 }
 

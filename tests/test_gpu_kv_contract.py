@@ -1,4 +1,5 @@
-"""What the key/value cache's header promises beside the values: host numbers that only bound the device arrays."""
+"""What the key/value cache's header promises beside the values: host numbers that only bound the device arrays, rows of outputs that
+belong to no token."""
 import math
 
 import pytest
@@ -66,3 +67,42 @@ def test_chunks_in_a_graph_follow_the_arrays(gpu_device, storage, dtype):
         torch.cuda.synchronize()
         s.check(out, lse.cpu(), 0.125, causal(s))
         assert torch.all(out[sum(news):].isnan()) and torch.all(lse[sum(news):].isnan())
+
+
+# ------------------------------------------------------------------------------- rows of no token
+
+@pytest.mark.parametrize("storage,dtype", [("bf16", "bf16"), ("i8", "f16")])
+@pytest.mark.parametrize("H,G,news,length,n,max_new", [
+    (2, 4, [3, 1], 300, 4, 3),           # one part
+    (2, 4, [1, 1, 1], 4200, 64, 1),      # parts, joined by the last workgroup
+    (8, 2, [1] * 40, 4200, 64, 1),       # parts, joined by a launch
+    (1, 20, [6, 2], 500, 5, 4),          # the host's max_new is less than what a sequence has: its last rows are left out
+], ids=str)
+def test_rows_of_no_token_are_left(gpu_device, storage, dtype, H, G, news, length, n, max_new):
+    s = Setup(storage, dtype, H, G, 64, 64, news, [length + i for i in range(len(news))], seed=33)
+    total = sum(news) + 5
+    batch = B.KVBatch(s.batch.tables, s.batch.offsets, s.batch.lens, total, max_new, max(s.lens))
+    mine = torch.zeros(total, dtype=torch.bool)
+    at = 0
+    for m in news:
+        mine[at:at + min(m, max_new)] = True
+        at += m
+    q = padded(s.q, total)
+
+    def check(what, fill, filled, call):
+        got = [torch.full(shape, fill, dtype=kind, device="cuda") for shape, kind in filled]
+        call(*got)
+        for x in got:
+            x = x.cpu()
+            left = x[~mine].isnan() if fill != fill else x[~mine] == fill
+            held = x[mine].isnan() if fill != fill else x[mine] == fill
+            assert bool(left.all()), what
+            assert not bool(held.any()), what
+        return got
+    outputs = [((total, H * G, 64), s.kind), ((total, H * G), torch.float32)]
+    blocks, = check("select", -77, [((total, H, n), torch.int32)], lambda b: B.pk_kv_select(s.cache.handle, batch.c, q, n, 1, 2, b))
+    check("attend", math.nan, outputs, lambda out, lse: B.pk_kv_attend(s.cache.handle, batch.c, q, 0.1, 0, out, lse))
+    for listed in (blocks.clamp(min=-1), torch.zeros_like(blocks)):  # (zeros: the rows of no token list a block that there is; so do others, n times)
+        check("attend_blocks", math.nan, outputs, lambda out, lse: B.pk_kv_attend_blocks(s.cache.handle, batch.c, q, 0.1, listed, out, lse))
+    rows = [((total, H, 64), torch.float32)] * 2
+    check("read", math.nan, rows, lambda k, v: B.pk_kv_read(s.cache.handle, batch.c, k, v))
