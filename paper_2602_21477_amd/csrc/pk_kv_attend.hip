@@ -41,6 +41,10 @@ struct KvQueryScale {
 };
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
+// A weight is 2^((x - m) qscale + top) for a score x and the largest m.  As x qscale - (m qscale - top), one operation less, it is off by the
+// rounding of m qscale: 2^-16 at this size of it (powers of two), from 2^24 on more than the type of the weights has room for above top.
+constexpr float kNear = 512.f;
+
 // acc += A (16 rows x 32) B (32 x 16 columns), 16-bit operands
 template <bool HALF>
 __device__ __forceinline__ f32x4 mma(u32x4 a, u32x4 b, f32x4 acc)
@@ -145,7 +149,7 @@ __global__ __launch_bounds__(256, DP * KvBytes<S>::v > 128 ? 1 : 2) void kv_rows
     constexpr int VC = CODED ? 1 : 2;         // loads of a lane for 16 tokens of a channel
     constexpr int RT = 16 / R, NI = 4 / R;    // queries of a tile; of a lane's four groups of four keys, those that its column weighs
     __shared__ __align__(16) float join_o[4][16][DP + 4];
-    __shared__ float join_m[4][16], join_l[4][16];
+    __shared__ float join_m[4][16], join_l[4][16], join_q[16];
     __shared__ uint32_t arrived;
     const int tid = threadIdx.x, wave = same(tid >> 6), lane = tid & 63, col = lane & 15, g = lane >> 4;
     const KvDev c = a.c;
@@ -391,14 +395,15 @@ __global__ __launch_bounds__(256, DP * KvBytes<S>::v > 128 ? 1 : 2) void kv_rows
 #pragma unroll
             for (int d = 0; d < DT; ++d) o[d] *= fade;
         }
-        const float base = (m == -INFINITY ? 0.f : m * qscale) - Sc::top;
+        // (the largest is taken off before the scale, whatever its size: a chunk of the sparse form 1 - 2 % slower, no other call)
+        const float mz = m == -INFINITY ? 0.f : m;
         f32x4 p[NI];
         float sum = 0.f;
 #pragma unroll
         for (int i = 0; i < NI; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                p[i][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i][j], qscale, -base));
+                p[i][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i][j] - mz, qscale, Sc::top));
                 sum = __builtin_fmaf(p[i][j], Sc::l_unit, sum);
             }
         l += sum;
@@ -450,8 +455,9 @@ __global__ __launch_bounds__(256, DP * KvBytes<S>::v > 128 ? 1 : 2) void kv_rows
 #pragma unroll
     for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4 *>(&join_o[wave][col][d * 16 + g * 4]) = o[d] * back;
     if (g == 0) {
-        join_m[wave][col] = m * qscale;
+        join_m[wave][col] = m;
         join_l[wave][col] = l;
+        join_q[col] = qscale; // (the same in all waves)
     }
     __syncthreads();
     const int r = tid >> 4, sub = tid & 15; // 16 threads a row
@@ -462,11 +468,11 @@ __global__ __launch_bounds__(256, DP * KvBytes<S>::v > 128 ? 1 : 2) void kv_rows
     float mm = -INFINITY;
 #pragma unroll
     for (int w = 0; w < 4 * R; ++w) mm = fmaxf(mm, join_m[w & 3][rr + (w >> 2) * RT]);
-    const float mb = mm == -INFINITY ? 0.f : mm;
+    const float mb = mm == -INFINITY ? 0.f : mm, jq = join_q[rr];
     float f[4 * R], ll = 0.f;
 #pragma unroll
     for (int w = 0; w < 4 * R; ++w) {
-        f[w] = __builtin_amdgcn_exp2f(join_m[w & 3][rr + (w >> 2) * RT] - mb);
+        f[w] = __builtin_amdgcn_exp2f((join_m[w & 3][rr + (w >> 2) * RT] - mb) * jq);
         ll += f[w] * join_l[w & 3][rr + (w >> 2) * RT];
     }
     auto joined = [&](int dd) __attribute__((always_inline)) {
@@ -476,13 +482,13 @@ __global__ __launch_bounds__(256, DP * KvBytes<S>::v > 128 ? 1 : 2) void kv_rows
         return y;
     };
     if (a.n_split == 1) {
-        if (in_row) kv_write_row<T, DP>(a, h, otok, omember, sub, mm, ll, joined);
+        if (in_row) kv_write_row<T, DP>(a, h, otok, omember, sub, mm * jq, ll, joined);
         return;
     }
     const size_t slot = (size_t)unit * c.H + h, first = slot * a.n_split;
     if (in_row) {
         const size_t pr = (first + split) * 16 + r;
-        if (sub == 0) *reinterpret_cast<f32x2 *>(a.part_ml + pr * 2) = f32x2{mm, ll};
+        if (sub == 0) *reinterpret_cast<f32x4 *>(a.part_ml + pr * 4) = f32x4{mm, ll, jq, 0.f};
 #pragma unroll
         for (int d = 0; d < DP; d += 64) *reinterpret_cast<f32x4 *>(a.part + pr * DP + d + sub * 4) = joined(d + sub * 4);
     }
@@ -501,7 +507,7 @@ __global__ __launch_bounds__(256, DP * KvBytes<S>::v > 128 ? 1 : 2) void kv_rows
     if (tid == 0) a.arrivals[slot] = 0; // for the next call
     if (!in_row) return;
     float jm = -INFINITY;
-    for (int s = 0; s < a.n_split; ++s) jm = fmaxf(jm, a.part_ml[((first + s) * 16 + r) * 2]);
+    for (int s = 0; s < a.n_split; ++s) jm = fmaxf(jm, a.part_ml[((first + s) * 16 + r) * 4]);
     const float jb = jm == -INFINITY ? 0.f : jm;
     float jl = 0.f;
     f32x4 y[DP / 64];
@@ -510,13 +516,13 @@ __global__ __launch_bounds__(256, DP * KvBytes<S>::v > 128 ? 1 : 2) void kv_rows
 #pragma unroll 8
     for (int s = 0; s < a.n_split; ++s) {
         const size_t pr = (first + s) * 16 + r;
-        const f32x2 ml = *reinterpret_cast<const f32x2 *>(a.part_ml + pr * 2);
-        const float w = __builtin_amdgcn_exp2f(ml[0] - jb); // (a part that saw no key has zeros)
+        const f32x4 ml = *reinterpret_cast<const f32x4 *>(a.part_ml + pr * 4);
+        const float w = __builtin_amdgcn_exp2f((ml[0] - jb) * jq); // (a part that saw no key has zeros)
         jl += w * ml[1];
 #pragma unroll
         for (int d = 0; d < DP / 64; ++d) y[d] += w * *reinterpret_cast<const f32x4 *>(a.part + pr * DP + d * 64 + sub * 4);
     }
-    kv_write_row<T, DP>(a, h, otok, omember, sub, jm, jl, [&](int dd) __attribute__((always_inline)) { return y[dd / 64]; });
+    kv_write_row<T, DP>(a, h, otok, omember, sub, jm * jq, jl, [&](int dd) __attribute__((always_inline)) { return y[dd / 64]; });
 }
 
 // ------------------------------------------------------------------ long chunks
@@ -807,7 +813,9 @@ struct KvTiles {
 // are read by the phases of weights and have four buffers.
 // On its way a tile is in registers, asked for a round before it is written, and is converted to the queries' type once for all waves.
 // The running maximum is of the bare products (the queries carry the scale's sign); O is rescaled only when some query's maximum
-// has grown.  ONE: a tile of keys lies in one page.
+// has grown.  Once a wave has met a maximum beyond kNear, its scores are lessened by it before they are scaled, in the branch that else
+// masks them.  In every tile that cost a long chunk 2.4 % and mixed chunks 4 % (the maximum so far as the products' start value: 2.5 and 5 %, as
+// most tiles raise some query's); so 0.8 and 2 %.  ONE: a tile of keys lies in one page.
 // Measured, bf16, 32 query heads of 128 channels: 4096 tokens over 32768 2.02 - 2.09 ms, 1.0 PFLOP/s.  4.36 million cycles, of which the matrix
 // cores are busy for 45 % and the reads of K and V out of LDS by eight waves take about as many, at 2.08 GHz: the power that the products draw
 // holds the clock there (the same launch over zeros 1.76 ms, at 2.4 GHz).  A product of 8192 x 8192 x 8192 runs at 1.2 - 1.35 PFLOP/s on
@@ -892,6 +900,7 @@ __global__ __launch_bounds__(NW * 64) void kv_tile_kernel(KvAttend a)
 #pragma unroll
     for (int u = 0; u < 4; ++u) pf[u] = pr[u] = u32x4{0u, 0u, 0u, 0u}; // (the first round has no tile before it)
     f32x16 s[2];
+    bool far = false; // whether the wave has met a maximum beyond kNear
     auto pv_products = [&](int t) __attribute__((always_inline)) {
         const int vp = ((t & 1) ^ 1) * DP * 8 + lds_piece<8>(col, hf); // the lane's piece of the first row; the others' from it
 #pragma unroll
@@ -916,6 +925,21 @@ __global__ __launch_bounds__(NW * 64) void kv_tile_kernel(KvAttend a)
             for (int r = 0; r < 2; ++r) s[r] = mma32<HALF>(lds.k[0][(kp ^ (k * 2)) + r * 32 * CH], qf[k], s[r]);
     };
     // (what a lane holds of s: keys 32 r + 16 u + 8 hf + j at 8 u + j)
+    auto take_off = [&](float most) __attribute__((always_inline)) {
+        const float z = most == -INFINITY ? 0.f : most;
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[r][i] -= z;
+    };
+    auto rescale = [&](float fade, float unit_up) __attribute__((always_inline)) {
+        l *= fade;
+        const float f = fade * unit_up;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[d][i] *= f;
+    };
     auto weights = [&](int t, uint32_t held) __attribute__((always_inline)) {
         const int base = t * kKvTile;
         const float *ks = lds.scales[CODED ? t & 3 : 0][0], *vs = lds.scales[CODED ? t & 3 : 0][1];
@@ -925,7 +949,8 @@ __global__ __launch_bounds__(NW * 64) void kv_tile_kernel(KvAttend a)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) s[u >> 1][8 * (u & 1) + j] *= ks[u * 16 + hf * 8 + j];
         }
-        if (held != 15u || __any(base + kKvTile - 1 > pos || base < from)) {
+        float above = m; // what a score has to exceed to be a new maximum
+        if (far || held != 15u || __any(base + kKvTile - 1 > pos || base < from)) {
             const int last = min(pos, sq.len - 1) - base, since = from - base;
 #pragma unroll
             for (int u = 0; u < 4; ++u)
@@ -934,6 +959,16 @@ __global__ __launch_bounds__(NW * 64) void kv_tile_kernel(KvAttend a)
                     const int key = u * 16 + hf * 8 + j;
                     s[u >> 1][8 * (u & 1) + j] = key <= last && key >= since && (held >> u & 1) ? s[u >> 1][8 * (u & 1) + j] : -INFINITY;
                 }
+            if (far) {
+                above = INFINITY;
+                float m1 = m;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) m1 = max3(m1, s[0][i], s[1][i]);
+                m1 = over_halves_max(m1);
+                take_off(m1);
+                rescale(m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - m1) * qscale), 1.f);
+                m = m1;
+            }
         }
         float most = max3(s[0][0], s[0][1], s[0][2]), most2 = max3(s[1][0], s[1][1], s[1][2]);
 #pragma unroll
@@ -945,25 +980,23 @@ __global__ __launch_bounds__(NW * 64) void kv_tile_kernel(KvAttend a)
         most = over_halves_max(most);
         float unit_up = 1.f;
         if constexpr (Sc::UNITS) unit_up = lds.fade[t & 3];
-        if (__any(most > m || unit_up != 1.f)) {
-            const float m1 = fmaxf(m, most);
-            const float fade = m1 == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - m1) * qscale);
+        if (__any(most > above || unit_up != 1.f)) {
+            const float m1 = most > above ? most : m;
+            rescale(m1 == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - m1) * qscale), unit_up);
             m = m1;
-            l *= fade;
-            const float f = fade * unit_up;
-#pragma unroll
-            for (int d = 0; d < DT; ++d)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) o[d][i] *= f;
+            if (!far && __any(fabsf(m == -INFINITY ? 0.f : m) * qscale > kNear)) {
+                far = true;
+                take_off(m);
+            }
         }
-        const float base_m = (m == -INFINITY ? 0.f : m * qscale) - Sc::top;
+        const float c = Sc::top - (far || m == -INFINITY ? 0.f : m * qscale);
         float sum[2] = {0.f, 0.f};
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
             float p[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                p[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u >> 1][8 * (u & 1) + j], qscale, -base_m));
+                p[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u >> 1][8 * (u & 1) + j], qscale, c));
                 sum[j & 1] = __builtin_fmaf(p[j], Sc::l_unit, sum[j & 1]);
                 if constexpr (CODED) p[j] *= vs[u * 16 + hf * 8 + j];
             }
@@ -1012,13 +1045,9 @@ __global__ __launch_bounds__(NW * 64) void kv_tile_kernel(KvAttend a)
     if (!valid) return;
     l = (l + __shfl_xor(l, 32)) * Sc::l_back;
     const float back = Sc::UNITS && t0 < t1 ? Sc::o_back * lds.unit[(t1 - 1) & 3] : Sc::o_back;
-    const float mm = m * qscale;
     if (a.n_split > 1) {
         const size_t pr = (((size_t)unit * c.H + h) * a.n_split + split) * BR + (wave * 32 + col);
-        if (hf == 0) {
-            a.part_ml[pr * 2] = mm;
-            a.part_ml[pr * 2 + 1] = l;
-        }
+        if (hf == 0) *reinterpret_cast<f32x4 *>(a.part_ml + pr * 4) = f32x4{m, l, qscale, 0.f};
 #pragma unroll
         for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -1038,7 +1067,7 @@ __global__ __launch_bounds__(NW * 64) void kv_tile_kernel(KvAttend a)
                 *reinterpret_cast<u32x2 *>(a.out + (oh * c.D + dd) * 2) =
                     u32x2{pack16<T>(o[d][4 * b] * inv, o[d][4 * b + 1] * inv), pack16<T>(o[d][4 * b + 2] * inv, o[d][4 * b + 3] * inv)};
         }
-    if (hf == 0 && a.lse) a.lse[oh] = l > 0.f ? (mm + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+    if (hf == 0 && a.lse) a.lse[oh] = l > 0.f ? (m * qscale + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
 }
 
 // The parts of a row joined, in order: 16 threads a row.  Parts have BR rows; a workgroup joins 16 of them.  BR 16: the parts of the kernel
@@ -1062,7 +1091,7 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttend a)
     if (SPARSE && (tok < sq.first || tok >= sq.first + sq.m)) return; // (has no parts)
     const size_t at = ((size_t)unit * a.c.H + h) * a.n_split;
     float m = -INFINITY;
-    for (int s = 0; s < a.n_split; ++s) m = fmaxf(m, a.part_ml[((at + s) * BR + r) * 2]);
+    for (int s = 0; s < a.n_split; ++s) m = fmaxf(m, a.part_ml[((at + s) * BR + r) * 4]);
     const float base = m == -INFINITY ? 0.f : m;
     float l = 0.f;
     f32x4 y[DP / 64];
@@ -1071,13 +1100,14 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttend a)
 #pragma unroll 8
     for (int s = 0; s < a.n_split; ++s) {
         const size_t pr = (at + s) * BR + r;
-        const f32x2 ml = *reinterpret_cast<const f32x2 *>(a.part_ml + pr * 2);
-        const float w = __builtin_amdgcn_exp2f(ml[0] - base); // (a part that saw no key has zeros)
+        const f32x4 ml = *reinterpret_cast<const f32x4 *>(a.part_ml + pr * 4);
+        const float w = __builtin_amdgcn_exp2f((ml[0] - base) * ml[2]); // (a part that saw no key has zeros)
         l += w * ml[1];
 #pragma unroll
         for (int d = 0; d < DP / 64; ++d) y[d] += w * *reinterpret_cast<const f32x4 *>(a.part + pr * DP + d * 64 + sub * 4);
     }
-    kv_write_row<T, DP>(a, h, tok, row % a.G, sub, m, l, [&](int dd) __attribute__((always_inline)) { return y[dd / 64]; });
+    const float qscale = a.part_ml[(at * BR + r) * 4 + 2];
+    kv_write_row<T, DP>(a, h, tok, row % a.G, sub, m * qscale, l, [&](int dd) __attribute__((always_inline)) { return y[dd / 64]; });
 }
 
 // Parts that the keys are cut into (`tiles` tiles of 64 at most): so many that there are `wgs` workgroups, each with `least` tiles at least;

@@ -1,14 +1,17 @@
 """What the key/value cache's header promises beside the values: host numbers that only bound the device arrays, rows of outputs that
-belong to no token."""
+belong to no token, scores at the ends of what 32 bits hold."""
 import math
 
 import pytest
 import torch
 
 from paper_2602_21477_amd import binding as B
-from test_gpu_kv import Setup
+from test_gpu_kv import U, Setup
 
 pytestmark = pytest.mark.gpu
+
+CODES = [("f16", "f16"), ("bf16", "bf16"), ("i8", "bf16"), ("i8", "f16"), ("f8", "bf16"), ("f8", "f16")]
+
 
 def causal(s, window=0):
     key = [torch.arange(l) for l in s.lens]
@@ -106,3 +109,42 @@ def test_rows_of_no_token_are_left(gpu_device, storage, dtype, H, G, news, lengt
         check("attend_blocks", math.nan, outputs, lambda out, lse: B.pk_kv_attend_blocks(s.cache.handle, batch.c, q, 0.1, listed, out, lse))
     rows = [((total, H, 64), torch.float32)] * 2
     check("read", math.nan, rows, lambda k, v: B.pk_kv_read(s.cache.handle, batch.c, k, v))
+
+
+# ------------------------------------------------------------------------------- ends of 32 bits
+
+# Keys whose channels are all `kc` but the last, and queries of `qc`: every product and every sum of them is a whole number below 2^24 (times the
+# codes' scale, which is 1), so that scores are exact whatever their order, and differ by the last channel times the scale.
+LARGE = {"f16": (1200, 64), "bf16": (1200, 64), "i8": (127, 500), "f8": (448, 256)}
+
+
+@pytest.mark.parametrize("storage,dtype", CODES)
+@pytest.mark.parametrize("news,length", [([1], 90), ([1], 2100), ([150], 700)], ids=str)
+@pytest.mark.parametrize("scale", [0.37, 2.3, 3.7, 47.0, -3.7])
+def test_scores_beyond_24_bits(gpu_device, storage, dtype, news, length, scale):
+    """Finite scores of any size: exact differences between them, some of 10^6 to 10^9, give the weights that they stand for.
+
+    e, the relative error of a weight: 2^-20 for the exponential and the sums, and the differences' rounding (of the scale, and of their product
+    with it): 2^-22 of the largest that has any weight (e^-30 is none)."""
+    kc, qc = LARGE[storage]
+    s = Setup(storage, dtype, 1, 2, 128, 64, news, [length], seed=34)
+    step = torch.arange(length) * 5 // length  # (the maximum grows late: sums so far are rescaled)
+    s.k[0][:] = kc
+    s.k[0][:, 0, 127] = (4 - step if scale < 0 else step).to(s.kind)
+    s.q[:] = qc
+    s.q[:, :, 127] = 1
+    s.write(s.lens, (s.k, s.v))
+    k, v = (x[0].double() for x in s.stored())
+    assert torch.equal(k, s.k[0].double())
+    out, lse = s.cache.attend(s.q.cuda(), s.batch, scale, want_lse=True)
+    out, lse = out.cpu().double(), lse.cpu()
+    u_out, u_w = U[s.kind], 2 * U[torch.float16] if storage in ("i8", "f8") else U[s.kind]
+    e = 2.0 ** -20 + 2.0 ** -22 * min(30.0, 4 * abs(scale))
+    for row, _, pos in s.tokens():
+        for g in range(2):
+            x = (k[:pos + 1, 0] @ s.q[row, g].double()) * scale
+            w = torch.softmax(x, 0)
+            ref, a = w @ v[:pos + 1, 0], w @ v[:pos + 1, 0].abs()
+            assert torch.all((out[row, g] - ref).abs() <= u_out * ref.abs() + (u_w + e) * (1 + u_out) * a + 2.0 ** -24), (row, g)
+            full = float(torch.logsumexp(x, 0))
+            assert abs(float(lse[row, g]) - full) <= e + 2.0 ** -20 * abs(full), (row, g)
