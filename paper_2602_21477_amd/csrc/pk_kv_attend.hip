@@ -387,10 +387,12 @@ __global__ __launch_bounds__(256, DP * KvBytes<S>::v > 128 ? 1 : 2) void kv_rows
             m = m1;
             l *= fade;
             if constexpr (Sc::UNITS) {
-                big = fmaxf(over_quarters_max(big), vunit);
-                vper = 1.f / big;
-                fade *= vunit * vper;
-                vunit = big;
+                big = over_quarters_max(big);
+                if (big > vunit) { // (else what is there stays: a unit times its rounded inverse need not be 1)
+                    vper = 1.f / big;
+                    fade *= vunit * vper;
+                    vunit = big;
+                }
             }
 #pragma unroll
             for (int d = 0; d < DT; ++d) o[d] *= fade;
@@ -743,7 +745,7 @@ struct KvTiles {
             if (same(threadIdx.x >> 6) != 1) return;
             asm volatile("" : "+v"(vsw)); // (here, not where it was asked for)
             const float most = fmaxf(over_wave_max(vsw), unit), per = __builtin_amdgcn_rcpf(most);
-            fade = unit * per;
+            fade = most > unit ? unit * per : 1.f; // (a unit times its rounded inverse need not be 1, and that in every tile: 2^-10 of O in 2^20 keys)
             unit = most;
             vsw *= per;
         }

@@ -1,12 +1,12 @@
 """What the key/value cache's header promises beside the values: host numbers that only bound the device arrays, rows of outputs that
-belong to no token, scores at the ends of what 32 bits hold."""
+belong to no token, scores and lengths at the ends of what 32 bits hold."""
 import math
 
 import pytest
 import torch
 
 from paper_2602_21477_amd import binding as B
-from test_gpu_kv import U, Setup
+from test_gpu_kv import STORAGES, U, Setup
 
 pytestmark = pytest.mark.gpu
 
@@ -148,3 +148,29 @@ def test_scores_beyond_24_bits(gpu_device, storage, dtype, news, length, scale):
             assert torch.all((out[row, g] - ref).abs() <= u_out * ref.abs() + (u_w + e) * (1 + u_out) * a + 2.0 ** -24), (row, g)
             full = float(torch.logsumexp(x, 0))
             assert abs(float(lse[row, g]) - full) <= e + 2.0 ** -20 * abs(full), (row, g)
+
+
+@pytest.mark.parametrize("storage", ["i8", "f8"])
+def test_a_long_sum_in_one_part_keeps_its_size(gpu_device, storage):
+    """2^20 keys of equal weight whose values are equal: the sum of weights that are 2^15 exactly times codes that are whole numbers needs no
+    rounding, so a result is the value itself: its own rounding, and 2^-20 for the scales and the division.  Heads differ in their values' scale."""
+    H, G, D, P, n, m, seqs = 64, 4, 64, 128, 1 << 20, 64, 8
+    cache = B.KVCache(1, H, D, storage=STORAGES[storage], page_tokens=P)
+    gen = torch.Generator().manual_seed(35)
+    one = torch.full((D,), 64.0)
+    one[0] = 127.0 if storage == "i8" else 448.0
+    v = (one * (torch.rand(H, 1, generator=gen) + 0.1) * 0.01).expand(P, H, D)
+    # every page of every sequence is the one page that there is
+    def batch(m, length, seqs):
+        tables = torch.zeros((seqs, length // P), dtype=torch.int32, device="cuda")
+        offsets = torch.arange(seqs + 1, dtype=torch.int32, device="cuda") * m
+        return B.KVBatch(tables, offsets, torch.full((seqs,), length, dtype=torch.int32, device="cuda"), seqs * m, m, length)
+    one_page = batch(P, P, 1)
+    cache.append(torch.zeros(P, H, D, device="cuda"), v.contiguous().cuda(), one_page)
+    held = cache.read(one_page, torch.float32)[1][0].cpu().double()  # [head, channel]
+    q = torch.zeros(seqs * m, H * G, D, dtype=torch.float16, device="cuda")
+    out, lse = cache.attend(q, batch(m, n, seqs), 0.125, want_lse=True)
+    off = (out.cpu().double().view(-1, H, G, D) - held[:, None]).abs() / held[:, None]
+    assert float(off.max()) <= 2.0 ** -11 + 2.0 ** -20
+    pos = n - m + torch.arange(m).repeat(seqs)
+    assert torch.allclose(lse.cpu().double(), torch.log(pos + 1.0).double()[:, None].expand(-1, H * G), rtol=2.0 ** -20, atol=0)
