@@ -536,7 +536,7 @@ int attend(pk_kv *kv, const pk_kv_batch *batch, const pk_rows *q, int32_t n_q_he
     if (!out || reinterpret_cast<uintptr_t>(out) % 16) return PK_ERR_INVALID_ARG;
     a.c = kv->dev;
     a.scale = scale;
-    a.window = window;
+    a.window = (int32_t)std::min<int64_t>(window, kMaxTokens); // (a position before the first one less the window fits 32 bits too)
     a.blocks = blocks;
     a.n_blocks = n_blocks;
     a.out = static_cast<char *>(out);

@@ -174,3 +174,13 @@ def test_a_long_sum_in_one_part_keeps_its_size(gpu_device, storage):
     assert float(off.max()) <= 2.0 ** -11 + 2.0 ** -20
     pos = n - m + torch.arange(m).repeat(seqs)
     assert torch.allclose(lse.cpu().double(), torch.log(pos + 1.0).double()[:, None].expand(-1, H * G), rtol=2.0 ** -20, atol=0)
+
+
+def test_windows_as_long_as_32_bits_have(gpu_device):
+    """The longest window is none, also where a sequence has more new tokens than it holds (positions before the first are left out)."""
+    for news, lens in (([40, 3], [100, 90]), ([24, 200], [20, 150])):
+        s = Setup("bf16", "bf16", 1, 4, 64, 16, news, [max(n, l) for n, l in zip(news, lens)], seed=36)
+        batch = B.KVBatch(s.batch.tables, s.batch.offsets, torch.tensor(lens, dtype=torch.int32, device="cuda"), sum(news), max(news), max(lens))
+        want, got = (attend(s.cache, batch, s.q.cuda(), 0.1, window) for window in (0, 2 ** 31 - 1))
+        for a, b in zip(want, got):
+            assert not bool(a.isnan().any()) and torch.equal(a, b)
