@@ -525,7 +525,8 @@ int pk_kv_attend(pk_kv *kv, const pk_kv_batch *batch, const pk_rows *q, int32_t 
  * Ties go to the lower block.  No sum in it is rounded: the choice depends on nothing but the inputs.
  *   sink >= 0, local >= 1, sink + local <= n_blocks
  *   out_blocks  DEVICE [n_tokens][n_heads][n_blocks] int32: block numbers (position / page_tokens), ascending, then -1
- * PK_ERR_UNSUPPORTED where a sequence may have more than 32768 blocks.  Asynchronous.
+ * PK_ERR_UNSUPPORTED where a sequence may have more than 32768 blocks, and where no launch has the workgroups, which needs n_heads *
+ * (n_tokens + n_seqs) of 2^24 and more.  Asynchronous.
  */
 int pk_kv_select(pk_kv *kv, const pk_kv_batch *batch, const pk_rows *q, int32_t n_q_heads, int32_t n_blocks, int32_t sink, int32_t local,
                  int32_t *out_blocks, void *stream);

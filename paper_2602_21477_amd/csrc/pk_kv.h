@@ -233,6 +233,7 @@ hipError_t launch_kv_read(const KvDev &c, int storage, int dp, const KvBatch &b,
 hipError_t launch_kv_bounds(const KvDev &c, int dp, const int32_t *pages, int64_t n, float *hi, float *lo, hipStream_t s);
 hipError_t launch_kv_select(const KvDev &c, int dp, const KvBatch &b, const KvRows &q, int dtype, int G, int n_blocks, int sink, int local,
                             int num_cu, int32_t *out, hipStream_t s);
+int64_t kv_select_workgroups(const KvDev &c, const KvBatch &b, int G); // of that launch, of 256 threads at least
 hipError_t launch_kv_attend(const KvAttend &a, int storage, int dp, int dtype, hipStream_t s);
 
 constexpr int kKvTile = 64;          // keys of one step of the attention kernels

@@ -442,6 +442,7 @@ namespace {
 
 constexpr uint64_t kKvMagic = 0x70616e63616b7631ull;
 constexpr int64_t kMaxUnits = 1 << 22; // workgroups of a launch before they are cut into parts: a grid has 32 bits for its threads
+constexpr int64_t kMaxGroups = (1 << 24) - 1; // workgroups of 256 threads of a launch: the same
 constexpr int kMaxTouched = 1 << 23;   // pages of one sequence that a call writes or reads: the same
 constexpr int64_t kMaxTokens = 1 << 30; // of a sequence: positions and what is added to them fit 32 bits
 constexpr int kMaxHeads = 1024; // key/value heads of a cache, and query heads of one of them
@@ -679,7 +680,7 @@ int pk_kv_select(pk_kv *kv, const pk_kv_batch *batch, const pk_rows *q, int32_t 
     rc = take_queries(kv, q, n_q_heads, &qr, &G);
     if (rc != PK_OK) return rc;
     if (!out_blocks) return PK_ERR_INVALID_ARG;
-    if ((int64_t)b.n_seqs * b.max_new * kv->cfg.n_heads > 4 * kMaxUnits) return PK_ERR_UNSUPPORTED;
+    if (kv_select_workgroups(kv->dev, b, G) > kMaxGroups) return PK_ERR_UNSUPPORTED;
     return launch_kv_select(kv->dev, kv->dp, b, qr, q->dtype, G, n_blocks, sink, local, kv->num_cu, out_blocks, static_cast<hipStream_t>(stream)) == hipSuccess
                ? PK_OK
                : PK_ERR_HIP;

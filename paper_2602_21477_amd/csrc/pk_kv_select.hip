@@ -59,6 +59,27 @@ __device__ __forceinline__ void four_keys(uint32_t (&key)[4], const uint32_t *k,
     for (int j = 0; j < 4; ++j) key[j] = i + j * step < end ? k[i + j * step] : 0;
 }
 
+// Groups of 2^log_tokens tokens counted over a batch: the first one of sequence s.  There is room between it and the next sequence's for all
+// that the sequence can make: with o = a t + r and o' = a' t + r' its offset and the next one's, ceil((o' - o) / t) <= a' - a + 1.
+__device__ __forceinline__ int first_group(const KvBatch &b, int s, int log_tokens)
+{
+    return (min(max(b.offsets[s], 0), b.n_tokens) >> log_tokens) + s;
+}
+// The sequence that group `unit` is one of, by all lanes of a wave: 64 at once, so that 4096 sequences take two steps.
+__device__ __forceinline__ int group_seq(const KvBatch &b, int unit, int log_tokens)
+{
+    const int lane = threadIdx.x & 63;
+    int lo = 0, n = b.n_seqs;
+    while (n > 1) {
+        const int step = (n + 63) >> 6;
+        const bool upto = lane * step < n && first_group(b, lo + lane * step, log_tokens) <= unit;
+        const int last = max(__popcll(__ballot(upto)) - 1, 0) * step;
+        lo += last;
+        n = min(step, n - last);
+    }
+    return lo;
+}
+
 struct KvSelect {
     KvDev c;
     KvBatch b;
@@ -66,7 +87,7 @@ struct KvSelect {
     int32_t G, n, sink, local;
     int32_t gp, log_gp;         // columns of a token: its query heads, a power of two of 16 at most
     int32_t tokens, log_tokens; // of a workgroup: 16 / gp at most, a power of two
-    int32_t groups; // of tokens, of one sequence
+    int32_t groups; // of tokens: of one sequence at most; 0: counted over the batch, and looked up
     int32_t room;   // keys of a token in LDS
     int32_t *out;
 };
@@ -93,9 +114,11 @@ __global__ __launch_bounds__(NW * 64) void kv_select_kernel(KvSelect a)
     __shared__ uint32_t goes[3][NW]; // whether a token's waves have more to do
     const KvDev c = a.c;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 15, g = lane >> 4;
-    const int h = blockIdx.x % c.H, unit = blockIdx.x / c.H, seq = unit / a.groups, first = (unit - seq * a.groups) * a.tokens;
+    const int h = blockIdx.x % c.H, unit = blockIdx.x / c.H;
+    const int seq = a.groups > 0 ? unit / a.groups : group_seq(a.b, unit, a.log_tokens);
+    const int first = (unit - (a.groups > 0 ? seq * a.groups : first_group(a.b, seq, a.log_tokens))) * a.tokens;
     const KvSeq sq = kv_seq(a.b, seq, c.P);
-    if (first >= sq.m) return;
+    if (first < 0 || first >= sq.m) return;
     const int32_t *table = a.b.tables + (size_t)seq * a.b.table_stride;
     const int start = sq.len - sq.m;
     const int last_pos = start + min(first + a.tokens, sq.m) - 1, nb = last_pos < 0 ? 0 : (last_pos >> c.logP) + 1; // blocks of its last token
@@ -382,8 +405,8 @@ hipError_t run(const KvSelect &a, unsigned grid, size_t lds, hipStream_t s)
     return hipGetLastError();
 }
 
-template <int T, int DP>
-hipError_t run_waves(KvSelect a, int num_cu, hipStream_t s)
+// How the batch is cut: tokens of a workgroup, and workgroups of a head.
+int64_t cut(KvSelect &a)
 {
     const int64_t most = ((int64_t)a.b.max_len + a.c.P - 1) / a.c.P;
     a.room = (int32_t)std::max<int64_t>(std::min<int64_t>(most, a.b.cols), 1);
@@ -395,8 +418,17 @@ hipError_t run_waves(KvSelect a, int num_cu, hipStream_t s)
     a.tokens = 16 / a.gp;
     while (a.tokens > 1 && (a.tokens / 2 >= a.b.max_new || (int64_t)a.tokens * a.room * 4 > (48 << 10))) a.tokens /= 2;
     a.log_tokens = __builtin_ctz((unsigned)a.tokens);
-    a.groups = (a.b.max_new + a.tokens - 1) / a.tokens;
-    const int64_t grid = (int64_t)a.b.n_seqs * a.groups * a.c.H;
+    // the longest sequence's groups for every one, found by a division; or, where these are more than all tokens can make (a chunk among many
+    // sequences), counted over the batch
+    const int64_t each = (int64_t)a.b.max_new / a.tokens + (a.b.max_new % a.tokens != 0), all = a.b.n_tokens / a.tokens + (int64_t)a.b.n_seqs;
+    a.groups = a.b.n_seqs * each <= all ? (int32_t)each : 0;
+    return std::min(a.b.n_seqs * each, all);
+}
+
+template <int T, int DP>
+hipError_t run_waves(KvSelect a, int num_cu, hipStream_t s)
+{
+    const int64_t grid = cut(a) * a.c.H;
     const size_t lds = (size_t)a.tokens * a.room * 4;
     // few workgroups: 16 waves each, while LDS has room for what they need beside the keys (one token with 313 blocks 12.9 us, 4 waves 13.9; 16
     // with 2048 26.7, 4 waves 50.7; many workgroups: 1024 tokens with 512 122 us, 4 waves 52.9)
@@ -405,6 +437,13 @@ hipError_t run_waves(KvSelect a, int num_cu, hipStream_t s)
 }
 
 } // namespace
+
+int64_t kv_select_workgroups(const KvDev &c, const KvBatch &b, int G)
+{
+    KvSelect a{};
+    a.c = c, a.b = b, a.G = G;
+    return cut(a) * c.H;
+}
 
 hipError_t launch_kv_select(const KvDev &c, int dp, const KvBatch &b, const KvRows &q, int dtype, int G, int n_blocks, int sink, int local,
                             int num_cu, int32_t *out, hipStream_t s)

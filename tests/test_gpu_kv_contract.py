@@ -1,12 +1,12 @@
 """What the key/value cache's header promises beside the values: host numbers that only bound the device arrays, rows of outputs that
-belong to no token, scores and lengths at the ends of what 32 bits hold."""
+belong to no token, scores and lengths at the ends of what 32 bits hold, batches as ragged as they come, exact choices."""
 import math
 
 import pytest
 import torch
 
 from paper_2602_21477_amd import binding as B
-from test_gpu_kv import STORAGES, U, Setup
+from test_gpu_kv import STORAGES, U, Setup, bounds_of, definition
 
 pytestmark = pytest.mark.gpu
 
@@ -184,3 +184,76 @@ def test_windows_as_long_as_32_bits_have(gpu_device):
         want, got = (attend(s.cache, batch, s.q.cuda(), 0.1, window) for window in (0, 2 ** 31 - 1))
         for a, b in zip(want, got):
             assert not bool(a.isnan().any()) and torch.equal(a, b)
+
+
+# ------------------------------------------------------------------------------- choices
+
+def chosen(s, n, sink, local):
+    """The choice by its definition, from the rows that were written, in the 32 bits that it is stated in: nothing is read back."""
+    want = torch.full((sum(s.news), s.H, n), -1, dtype=torch.int32)
+    x = s.q.float()
+    top = x.abs().amax(-1, keepdim=True)
+    up = torch.where(top > 0, torch.full_like(top, 127.0) / top, torch.zeros_like(top))
+    code, qs = (x * up).round().clamp(-127, 127).double(), (top * torch.tensor(1.0 / 127.0))[..., 0]
+    bounds = []
+    for i, l in enumerate(s.lens):
+        held = definition(s.k[i], s.storage, s.kind)
+        bounds.append([bounds_of(held[j:j + s.P]) for j in range(0, l, s.P)])
+    for row, i, pos in s.tokens():
+        mine = pos // s.P
+        for h in range(s.H):
+            hi, lo, scale = (torch.stack([b[j][h] for b in bounds[i][:mine + 1]]) for j in range(3))
+            c = code[row, h * s.G:(h + 1) * s.G]
+            u = c.clamp(min=0) @ hi.double().T + c.clamp(max=0) @ lo.double().T
+            score = (u.float() * qs[row, h * s.G:(h + 1) * s.G, None]).amax(0) * scale[:, 0]
+            score[:sink] = math.inf
+            score[max(mine + 1 - local, 0):] = math.inf
+            take = torch.sort(score, descending=True, stable=True).indices[:n].sort().values
+            want[row, h, :len(take)] = take.int()
+    return want
+
+
+@pytest.mark.parametrize("storage,dtype", [("bf16", "bf16"), ("i8", "f16")])
+@pytest.mark.parametrize("H,G,news,lens,n", [
+    (8, 2, [1] * 20, [3000 + 7 * i for i in range(20)], 12),
+    (2, 1, [33], [5000], 40),
+    (1, 3, [9, 2], [8000, 70], 3),
+    (2, 4, [37, 1, 0, 1, 1, 1, 6, 1], [1200, 900, 5, 1, 333, 17, 640, 1024], 7),  # few of the tokens' places for so many sequences are taken
+    (1, 20, [1, 1, 1, 11], [900, 1, 30, 500], 6),
+    (1, 2, [1] * 90 + [45] + [0, 2] * 30, [40 + i for i in range(90)] + [300] + [3, 170] * 30, 4),
+], ids=str)
+def test_every_choice_is_exact(gpu_device, storage, dtype, H, G, news, lens, n):
+    s = Setup(storage, dtype, H, G, 64, 16, news, lens, seed=37, spread=0.2)
+    assert torch.equal(s.cache.select(s.q.cuda(), s.batch, n).cpu(), chosen(s, n, 1, 2))
+
+
+def test_a_chunk_among_many_sequences(gpu_device):
+    """64 sequences of 8 heads, one with a chunk of 32769 tokens: the same choices as of each sequence by itself."""
+    H, P, D, n = 8, 128, 8, 3
+    lens = [32769 + 200] + [1 + 37 * i for i in range(63)]
+    news = [32769] + [1] * 63
+    pages = [-(-l // P) for l in lens]
+    cache = B.KVCache(sum(pages), H, D, storage=B.PK_F16, page_tokens=P)
+    gen = torch.Generator("cuda").manual_seed(38)
+    tables = torch.zeros((64, max(pages)), dtype=torch.int32)
+    at = 0
+    for i, p in enumerate(pages):
+        tables[i, :p] = torch.arange(at, at + p, dtype=torch.int32)
+        at += p
+    tables = tables.cuda()
+
+    def batch(which, m):
+        offsets = torch.tensor([0] + [m[i] for i in which]).cumsum(0).int().cuda()
+        t = tables[which[0]:which[-1] + 1]
+        return B.KVBatch(t, offsets, torch.tensor([lens[i] for i in which], dtype=torch.int32, device="cuda"), sum(m[i] for i in which), max(m[i] for i in which),
+                         max(lens[i] for i in which))
+    for i in range(64):
+        rows = torch.randn(lens[i], H, D, generator=gen, device="cuda").half()
+        cache.append(rows, rows, batch([i], lens))
+    q = torch.randn(sum(news), H, D, generator=gen, device="cuda").half()
+    got = cache.select(q, batch(list(range(64)), news), n)
+    at = 0
+    for i in range(64):
+        assert torch.equal(got[at:at + news[i]], cache.select(q[at:at + news[i]], batch([i], news), n)), i
+        at += news[i]
+    cache.close()
