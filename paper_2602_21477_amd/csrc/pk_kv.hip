@@ -315,28 +315,30 @@ __global__ __launch_bounds__(kThreads) void kv_read_kernel(KvDev c, KvBatch b, c
     }
 }
 
-// The bounds of listed pages as numbers, a page a workgroup.  Small: 64 pages of 8 heads 2.8 us, which is a launch
-// and two loads, 1024 pages 5.9 us.
-__global__ __launch_bounds__(kThreads) void kv_bounds_kernel(KvDev c, int dp, const int32_t *pages, float *hi, float *lo)
+// The bounds of listed pages as numbers, a page a workgroup (and every kMaxBounds-th after it: a grid has 32 bits for its threads).  Small: 64
+// pages of 8 heads 2.8 us, which is a launch and two loads, 1024 pages 5.9 us.
+constexpr int64_t kMaxBounds = 1 << 20;
+__global__ __launch_bounds__(kThreads) void kv_bounds_kernel(KvDev c, int dp, const int32_t *pages, int64_t n_listed, float *hi, float *lo)
 {
-    const size_t n = blockIdx.x;
-    const uint32_t page = (uint32_t)pages[n];
-    const bool there = page < c.n_pages;
-    for (int i = threadIdx.x * 4; i < c.H * c.D; i += kThreads * 4) { // (D is a multiple of 8: four channels are of one head)
-        const int h = i / c.D, d = i - h * c.D;
-        const size_t ph = (size_t)(there ? page : 0) * c.H + h;
-        const float s = there ? c.bs[ph] : 0.f;
-        char bh[4], bl[4];
-        __builtin_memcpy(bh, c.bc + ph * 2 * dp + d, 4);
-        __builtin_memcpy(bl, c.bc + (ph * 2 + 1) * dp + d, 4);
-        f32x4 x, y;
+    for (size_t n = blockIdx.x; n < (size_t)n_listed; n += kMaxBounds) {
+        const uint32_t page = (uint32_t)pages[n];
+        const bool there = page < c.n_pages;
+        for (int i = threadIdx.x * 4; i < c.H * c.D; i += kThreads * 4) { // (D is a multiple of 8: four channels are of one head)
+            const int h = i / c.D, d = i - h * c.D;
+            const size_t ph = (size_t)(there ? page : 0) * c.H + h;
+            const float s = there ? c.bs[ph] : 0.f;
+            char bh[4], bl[4];
+            __builtin_memcpy(bh, c.bc + ph * 2 * dp + d, 4);
+            __builtin_memcpy(bl, c.bc + (ph * 2 + 1) * dp + d, 4);
+            f32x4 x, y;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            x[j] = there ? (float)(int8_t)bh[j] * s : 0.f;
-            y[j] = there ? (float)(int8_t)bl[j] * s : 0.f;
+            for (int j = 0; j < 4; ++j) {
+                x[j] = there ? (float)(int8_t)bh[j] * s : 0.f;
+                y[j] = there ? (float)(int8_t)bl[j] * s : 0.f;
+            }
+            *reinterpret_cast<f32x4 *>(hi + n * c.H * c.D + i) = x;
+            *reinterpret_cast<f32x4 *>(lo + n * c.H * c.D + i) = y;
         }
-        *reinterpret_cast<f32x4 *>(hi + n * c.H * c.D + i) = x;
-        *reinterpret_cast<f32x4 *>(lo + n * c.H * c.D + i) = y;
     }
 }
 
@@ -419,7 +421,7 @@ hipError_t launch_kv_read(const KvDev &c, int storage, int dp, const KvBatch &b,
 
 hipError_t launch_kv_bounds(const KvDev &c, int dp, const int32_t *pages, int64_t n, float *hi, float *lo, hipStream_t s)
 {
-    kv_bounds_kernel<<<dim3((unsigned)n), kThreads, 0, s>>>(c, dp, pages, hi, lo);
+    kv_bounds_kernel<<<dim3((unsigned)std::min(n, kMaxBounds)), kThreads, 0, s>>>(c, dp, pages, n, hi, lo);
     return hipGetLastError();
 }
 

@@ -257,3 +257,14 @@ def test_a_chunk_among_many_sequences(gpu_device):
         assert torch.equal(got[at:at + news[i]], cache.select(q[at:at + news[i]], batch([i], news), n)), i
         at += news[i]
     cache.close()
+
+
+def test_bounds_of_more_pages_than_a_launch_has_workgroups(gpu_device):
+    """2^24 and a few, of three pages and of numbers that there are no pages for: each as it is by itself."""
+    s = Setup("i8", "bf16", 1, 1, 8, 16, [40], [40], seed=39)
+    few = torch.tensor(s.tables[0].tolist() + [-1, 10 ** 9], dtype=torch.int32, device="cuda")
+    want = s.cache.bounds(few)
+    n = 2 ** 24 + 5
+    which = torch.randint(0, 5, (n,), generator=torch.Generator("cuda").manual_seed(39), device="cuda")
+    for got, x in zip(s.cache.bounds(few[which]), want):
+        assert torch.equal(got, x[which])
