@@ -512,7 +512,8 @@ int pk_kv_bounds(pk_kv *kv, const int32_t *pages, int64_t n, float *hi, float *l
  * Sums, maxima and lse are held in 32 bits; the weights are rounded to 16 for the product with the values.
  *   q    PK_F16 or PK_BF16; the storage's own type where that is one of the two (else PK_ERR_UNSUPPORTED)
  *   out  DEVICE [n_tokens][n_q_heads][head_dim] of q's type, 16-byte aligned;  lse  DEVICE [n_tokens][n_q_heads] or NULL
- * Equal calls give equal bits.  Asynchronous.
+ * PK_ERR_UNSUPPORTED also where no launch has the workgroups: 8 n_seqs n_heads of 2^24 and more, or n_tokens n_q_heads / 128 + n_seqs n_heads
+ * of 2^23 - 1.  Equal calls give equal bits.  Asynchronous.
  */
 int pk_kv_attend(pk_kv *kv, const pk_kv_batch *batch, const pk_rows *q, int32_t n_q_heads, float scale, int32_t window, void *out,
                  float *lse, void *stream);
@@ -532,7 +533,8 @@ int pk_kv_select(pk_kv *kv, const pk_kv_batch *batch, const pk_rows *q, int32_t 
                  int32_t *out_blocks, void *stream);
 
 /*
- * As pk_kv_attend without a window, over the keys of listed blocks alone.
+ * As pk_kv_attend without a window, over the keys of listed blocks alone.  PK_ERR_UNSUPPORTED from 2^24 workgroups on: one for a token, head
+ * and 16 query heads of it.
  *   blocks  DEVICE [n_tokens][n_heads][n_blocks] int32, in any order, no block twice in a row; numbers that the sequence
  *           has no block for (-1 among them) are left out
  */

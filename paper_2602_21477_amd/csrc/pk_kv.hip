@@ -443,8 +443,7 @@ struct pk_kv {
 namespace {
 
 constexpr uint64_t kKvMagic = 0x70616e63616b7631ull;
-constexpr int64_t kMaxUnits = 1 << 22; // workgroups of a launch before they are cut into parts: a grid has 32 bits for its threads
-constexpr int64_t kMaxGroups = (1 << 24) - 1; // workgroups of 256 threads of a launch: the same
+constexpr int64_t kMaxGroups = (1 << 24) - 1; // workgroups of 256 threads of a launch (of 512: half as many): a grid has 32 bits for its threads
 constexpr int kMaxTouched = 1 << 23;   // pages of one sequence that a call writes or reads: the same
 constexpr int64_t kMaxTokens = 1 << 30; // of a sequence: positions and what is added to them fit 32 bits
 constexpr int kMaxHeads = 1024; // key/value heads of a cache, and query heads of one of them
@@ -546,9 +545,9 @@ int attend(pk_kv *kv, const pk_kv_batch *batch, const pk_rows *q, int32_t n_q_he
     a.lse = lse;
     a.num_cu = kv->num_cu;
     const int64_t H = kv->cfg.n_heads, rows = (int64_t)a.b.n_tokens * a.G;
-    const int64_t few = a.b.n_seqs * std::min<int64_t>(((int64_t)a.b.max_new * a.G + 15) / 16, kKvFewRows / 16);
-    const int64_t units = blocks ? (int64_t)a.b.n_tokens * ((a.G + 15) / 16) : std::max<int64_t>(few, rows / 128 + a.b.n_seqs);
-    if (units * H > kMaxUnits) return PK_ERR_UNSUPPORTED;
+    const int64_t few = blocks ? (int64_t)a.b.n_tokens * ((a.G + 15) / 16) : a.b.n_seqs * std::min<int64_t>(((int64_t)a.b.max_new * a.G + 15) / 16, kKvFewRows / 16);
+    const int64_t many = blocks ? 0 : rows / 128 + a.b.n_seqs;
+    if (few * H > kMaxGroups || many * H > kMaxGroups / 2) return PK_ERR_UNSUPPORTED;
     a.part = reinterpret_cast<float *>(kv->ws);
     a.part_floats = kKvPartFloats;
     a.part_ml = a.part + kKvPartFloats;

@@ -268,3 +268,23 @@ def test_bounds_of_more_pages_than_a_launch_has_workgroups(gpu_device):
     which = torch.randint(0, 5, (n,), generator=torch.Generator("cuda").manual_seed(39), device="cuda")
     for got, x in zip(s.cache.bounds(few[which]), want):
         assert torch.equal(got, x[which])
+
+
+def test_many_tokens_and_heads(gpu_device):
+    """600 000 tokens of 8 heads that attend to a block each: as each part of them by itself."""
+    H, D, P, n = 8, 8, 16, 600_000
+    cache = B.KVCache(64, H, D, storage=B.PK_F16, page_tokens=P)
+    gen = torch.Generator("cuda").manual_seed(40)
+    tables = torch.arange(64, dtype=torch.int32, device="cuda").repeat(n // 64 // P + 1)[None]
+    one = B.KVBatch(tables, torch.tensor([0, 1024], dtype=torch.int32, device="cuda"), torch.tensor([1024], dtype=torch.int32, device="cuda"), 1024, 1024, 1024)
+    rows = torch.randn(1024, H, D, generator=gen, device="cuda").half()
+    cache.append(rows, rows, one)
+    q = torch.randn(n, H, D, generator=gen, device="cuda").half()
+    blocks = (torch.arange(n, device="cuda", dtype=torch.int32) // P)[:, None, None].expand(n, H, 1).contiguous()
+
+    def batch(length, m):
+        return B.KVBatch(tables, torch.tensor([0, m], dtype=torch.int32, device="cuda"), torch.tensor([length], dtype=torch.int32, device="cuda"), m, m, length)
+    out = cache.attend_blocks(q, blocks, batch(n, n), 0.3)
+    for at in (0, 299_000, n - 1000):
+        assert torch.equal(out[at:at + 1000], cache.attend_blocks(q[at:at + 1000], blocks[at:at + 1000], batch(at + 1000, 1000), 0.3))
+    cache.close()
