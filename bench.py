@@ -38,12 +38,13 @@ MEASURED_STREAM_SOURCE = "profiles/scan_kernel_c4_ip.md section 3 (scan load pat
 
 
 def kernel_sources_sha():
-    """Hash of the library's sources: a profile's counter figures only describe the kernels they were taken from."""
+    """Hash of the sources of the index's kernels: a profile's counter figures only describe the kernels they were taken from.  The
+    key/value cache's files (pk_kv*) hold none of them, and nothing of theirs is included by the others."""
     import hashlib
     h = hashlib.sha256()
     csrc = os.path.join(ROOT, "paper_2602_21477_amd", "csrc")
     for name in sorted(os.listdir(csrc)):
-        if name.endswith((".hip", ".h")):
+        if name.endswith((".hip", ".h")) and not name.startswith("pk_kv"):
             h.update(name.encode())
             h.update(open(os.path.join(csrc, name), "rb").read())
     return h.hexdigest()[:16]
