@@ -216,7 +216,8 @@ struct KvAttend {
     int32_t n_blocks;
     char *out;            // [n_tokens][H * G][D]
     float *lse;           // [n_tokens][H * G] or null
-    float *part, *part_ml; // room for partial results: part_floats of O, and four floats for each row (maximum, sum, the scores' scale)
+    float *part, *part_ml, *part_q; // room for partial results: part_floats of O, two floats for each row of them (maximum and sum), one for
+                                    // each row that has parts (the scores' scale)
     int64_t part_floats;
     uint32_t *arrivals;    // parts of a row tile that have ended, zeros between calls: kKvArrivals of them
     int32_t num_cu;

@@ -551,7 +551,8 @@ int attend(pk_kv *kv, const pk_kv_batch *batch, const pk_rows *q, int32_t n_q_he
     a.part = reinterpret_cast<float *>(kv->ws);
     a.part_floats = kKvPartFloats;
     a.part_ml = a.part + kKvPartFloats;
-    a.arrivals = reinterpret_cast<uint32_t *>(a.part_ml + kKvPartFloats / kv->dp * 4);
+    a.part_q = a.part_ml + kKvPartFloats / kv->dp * 2;
+    a.arrivals = reinterpret_cast<uint32_t *>(a.part_q + kKvPartFloats / kv->dp);
     return launch_kv_attend(a, kv->cfg.storage, kv->dp, q->dtype, s) == hipSuccess ? PK_OK : PK_ERR_HIP;
 }
 
@@ -583,7 +584,7 @@ int pk_kv_create(const pk_kv_config *cfg, void *arena, size_t arena_bytes, pk_kv
         return PK_ERR_HIP;
     }
     void *p = nullptr;
-    const size_t parts = (size_t)(kKvPartFloats + kKvPartFloats / kv->dp * 4) * sizeof(float);
+    const size_t parts = (size_t)(kKvPartFloats + kKvPartFloats / kv->dp * 3) * sizeof(float);
     if (hipMalloc(&p, parts + kKvArrivals * sizeof(uint32_t)) != hipSuccess) {
         (void)hipGetLastError();
         delete kv;

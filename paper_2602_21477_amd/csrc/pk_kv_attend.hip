@@ -116,6 +116,47 @@ __device__ __forceinline__ void kv_write_row(const KvAttend &a, int h, int tok, 
     if (sub == 0 && a.lse) a.lse[oh] = l > 0.f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
 }
 
+// The parts of row r of a tile of BR rows joined, from part `first` on and in order: their largest maximum, and sums and 4 channels in 64 in its
+// units.  Several at a time are asked for before any is used: one after the other they cost a latency each (64 parts of 8 heads: the join 12 us, else 40).
+template <int DP, int BR>
+__device__ __forceinline__ void kv_join_parts(const KvAttend &a, size_t first, int r, int sub, float qscale, float &m, float &l, f32x4 (&y)[DP / 64])
+{
+    constexpr int AT_ONCE = 8;
+    const int n = a.n_split;
+    m = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int d = 0; d < DP / 64; ++d) y[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < n; s += AT_ONCE) {
+        float x[AT_ONCE];
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) x[k] = a.part_ml[((first + min(s + k, n - 1)) * BR + r) * 2];
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) m = fmaxf(m, x[k]);
+    }
+    const float base = m == -INFINITY ? 0.f : m;
+    for (int s = 0; s < n; s += AT_ONCE) {
+        f32x2 ml[AT_ONCE];
+        f32x4 v[AT_ONCE][DP / 64];
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) {
+            const size_t pr = (first + min(s + k, n - 1)) * BR + r;
+            ml[k] = *reinterpret_cast<const f32x2 *>(a.part_ml + pr * 2);
+#pragma unroll
+            for (int d = 0; d < DP / 64; ++d) v[k][d] = *reinterpret_cast<const f32x4 *>(a.part + pr * DP + d * 64 + sub * 4);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) {
+            if (s + k >= n) break;
+            const float w = __builtin_amdgcn_exp2f((ml[k][0] - base) * qscale); // (a part that saw no key has zeros)
+            l += w * ml[k][1];
+#pragma unroll
+            for (int d = 0; d < DP / 64; ++d) y[d] += w * v[k][d];
+        }
+    }
+}
+
 // Rows of 16 queries that share a key/value head (query heads of its group, several tokens' where the group is small) against
 // keys that four waves of a workgroup take in turns, 64 at a time, with no LDS until they join their results:
 //   S^T = K Q^T   rows are keys, columns queries; the products' operands come from memory as they lie there
@@ -490,7 +531,8 @@ __global__ __launch_bounds__(256, DP * KvBytes<S>::v > 128 ? 1 : 2) void kv_rows
     const size_t slot = (size_t)unit * c.H + h, first = slot * a.n_split;
     if (in_row) {
         const size_t pr = (first + split) * 16 + r;
-        if (sub == 0) *reinterpret_cast<f32x4 *>(a.part_ml + pr * 4) = f32x4{mm, ll, jq, 0.f};
+        if (sub == 0) *reinterpret_cast<f32x2 *>(a.part_ml + pr * 2) = f32x2{mm, ll};
+        if (sub == 0 && split == 0) a.part_q[slot * 16 + r] = jq;
 #pragma unroll
         for (int d = 0; d < DP; d += 64) *reinterpret_cast<f32x4 *>(a.part + pr * DP + d + sub * 4) = joined(d + sub * 4);
     }
@@ -508,22 +550,9 @@ __global__ __launch_bounds__(256, DP * KvBytes<S>::v > 128 ? 1 : 2) void kv_rows
     __threadfence();
     if (tid == 0) a.arrivals[slot] = 0; // for the next call
     if (!in_row) return;
-    float jm = -INFINITY;
-    for (int s = 0; s < a.n_split; ++s) jm = fmaxf(jm, a.part_ml[((first + s) * 16 + r) * 4]);
-    const float jb = jm == -INFINITY ? 0.f : jm;
-    float jl = 0.f;
+    float jm, jl;
     f32x4 y[DP / 64];
-#pragma unroll
-    for (int d = 0; d < DP / 64; ++d) y[d] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
-    for (int s = 0; s < a.n_split; ++s) {
-        const size_t pr = (first + s) * 16 + r;
-        const f32x4 ml = *reinterpret_cast<const f32x4 *>(a.part_ml + pr * 4);
-        const float w = __builtin_amdgcn_exp2f((ml[0] - jb) * jq); // (a part that saw no key has zeros)
-        jl += w * ml[1];
-#pragma unroll
-        for (int d = 0; d < DP / 64; ++d) y[d] += w * *reinterpret_cast<const f32x4 *>(a.part + pr * DP + d * 64 + sub * 4);
-    }
+    kv_join_parts<DP, 16>(a, first, r, sub, jq, jm, jl, y);
     kv_write_row<T, DP>(a, h, otok, omember, sub, jm * jq, jl, [&](int dd) __attribute__((always_inline)) { return y[dd / 64]; });
 }
 
@@ -1049,7 +1078,10 @@ __global__ __launch_bounds__(NW * 64) void kv_tile_kernel(KvAttend a)
     const float back = Sc::UNITS && t0 < t1 ? Sc::o_back * lds.unit[(t1 - 1) & 3] : Sc::o_back;
     if (a.n_split > 1) {
         const size_t pr = (((size_t)unit * c.H + h) * a.n_split + split) * BR + (wave * 32 + col);
-        if (hf == 0) *reinterpret_cast<f32x4 *>(a.part_ml + pr * 4) = f32x4{m, l, qscale, 0.f};
+        if (hf == 0) {
+            *reinterpret_cast<f32x2 *>(a.part_ml + pr * 2) = f32x2{m, l};
+            if (split == 0) a.part_q[((size_t)unit * c.H + h) * BR + (wave * 32 + col)] = qscale;
+        }
 #pragma unroll
         for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -1092,23 +1124,10 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttend a)
     const int tok = SPARSE ? unit / a.row_tiles : sq.first + row / a.G;
     if (SPARSE && (tok < sq.first || tok >= sq.first + sq.m)) return; // (has no parts)
     const size_t at = ((size_t)unit * a.c.H + h) * a.n_split;
-    float m = -INFINITY;
-    for (int s = 0; s < a.n_split; ++s) m = fmaxf(m, a.part_ml[((at + s) * BR + r) * 4]);
-    const float base = m == -INFINITY ? 0.f : m;
-    float l = 0.f;
+    const float qscale = a.part_q[((size_t)unit * a.c.H + h) * BR + r];
+    float m, l;
     f32x4 y[DP / 64];
-#pragma unroll
-    for (int d = 0; d < DP / 64; ++d) y[d] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
-    for (int s = 0; s < a.n_split; ++s) {
-        const size_t pr = (at + s) * BR + r;
-        const f32x4 ml = *reinterpret_cast<const f32x4 *>(a.part_ml + pr * 4);
-        const float w = __builtin_amdgcn_exp2f((ml[0] - base) * ml[2]); // (a part that saw no key has zeros)
-        l += w * ml[1];
-#pragma unroll
-        for (int d = 0; d < DP / 64; ++d) y[d] += w * *reinterpret_cast<const f32x4 *>(a.part + pr * DP + d * 64 + sub * 4);
-    }
-    const float qscale = a.part_ml[(at * BR + r) * 4 + 2];
+    kv_join_parts<DP, BR>(a, at, r, sub, qscale, m, l, y);
     kv_write_row<T, DP>(a, h, tok, row % a.G, sub, m * qscale, l, [&](int dd) __attribute__((always_inline)) { return y[dd / 64]; });
 }
 
