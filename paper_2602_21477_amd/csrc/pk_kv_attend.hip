@@ -845,8 +845,9 @@ struct KvTiles {
 // On its way a tile is in registers, asked for a round before it is written, and is converted to the queries' type once for all waves.
 // The running maximum is of the bare products (the queries carry the scale's sign); O is rescaled only when some query's maximum
 // has grown.  Once a wave has met a maximum beyond kNear, its scores are lessened by it before they are scaled, in the branch that else
-// masks them.  In every tile that cost a long chunk 2.4 % and mixed chunks 4 % (the maximum so far as the products' start value: 2.5 and 5 %, as
-// most tiles raise some query's); so 0.8 and 2 %.  ONE: a tile of keys lies in one page.
+// masks them.  In every tile that cost a long chunk 2.2 % and mixed chunks 2.7 % (the maximum so far as the products' start value: 2.5 and 5 %,
+// as most tiles raise some query's); so 0.1 - 0.4 and 1 %.  Of 256 channels, which leave no register, in every tile all the same: 2048 tokens
+// over 8192, bf16, 702 us, in the branch 749, not at all 690.  ONE: a tile of keys lies in one page.
 // Measured, bf16, 32 query heads of 128 channels: 4096 tokens over 32768 2.02 - 2.09 ms, 1.0 PFLOP/s.  4.36 million cycles, of which the matrix
 // cores are busy for 45 % and the reads of K and V out of LDS by eight waves take about as many, at 2.08 GHz: the power that the products draw
 // holds the clock there (the same launch over zeros 1.76 ms, at 2.4 GHz).  A product of 8192 x 8192 x 8192 runs at 1.2 - 1.35 PFLOP/s on
@@ -858,6 +859,7 @@ __global__ __launch_bounds__(NW * 64) void kv_tile_kernel(KvAttend a)
     using Sc = KvScaling<S, T>;
     constexpr bool CODED = Sc::CODED, HALF = Sc::HALF, TWICE = Sc::TWICE;
     constexpr int KS = DP / 16, DT = DP / 32, CH = DP / 8;
+    constexpr bool ALWAYS = DP == 256; // the maximum is taken off in every tile
     __shared__ __align__(16) typename KvTiles<S, T, DP, NW, ONE>::Lds lds;
     const int tid = threadIdx.x, wave = same(tid >> 6), lane = tid & 63, col = lane & 31, hf = lane >> 5;
     const int late = NW > 4 ? wave >> 2 : 0;
@@ -1015,12 +1017,13 @@ __global__ __launch_bounds__(NW * 64) void kv_tile_kernel(KvAttend a)
             const float m1 = most > above ? most : m;
             rescale(m1 == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - m1) * qscale), unit_up);
             m = m1;
-            if (!far && __any(fabsf(m == -INFINITY ? 0.f : m) * qscale > kNear)) {
+            if (!ALWAYS && !far && __any(fabsf(m == -INFINITY ? 0.f : m) * qscale > kNear)) {
                 far = true;
                 take_off(m);
             }
         }
-        const float c = Sc::top - (far || m == -INFINITY ? 0.f : m * qscale);
+        if constexpr (ALWAYS) take_off(m);
+        const float c = Sc::top - (ALWAYS || far || m == -INFINITY ? 0.f : m * qscale);
         float sum[2] = {0.f, 0.f};
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
