@@ -288,3 +288,49 @@ def test_many_tokens_and_heads(gpu_device):
     for at in (0, 299_000, n - 1000):
         assert torch.equal(out[at:at + 1000], cache.attend_blocks(q[at:at + 1000], blocks[at:at + 1000], batch(at + 1000, 1000), 0.3))
     cache.close()
+
+
+@pytest.mark.parametrize("storage,dtype", [("bf16", "bf16"), ("i8", "f16")])
+def test_a_step_in_a_graph_follows_offsets(gpu_device, storage, dtype):
+    """Append, selection and attention to it, captured once for up to 64 tokens of four sequences (no more than 40 of one), replayed with other
+    offsets and lengths: the cache's rows, the choices and the results are what they are by their definitions, each time."""
+    s = Setup(storage, dtype, 2, 2, 64, 16, [16] * 4, [400, 330, 90, 500], seed=41)
+    H, D, n = s.H, s.D, 5
+    offsets, lens = s.batch.offsets.clone(), s.batch.lens.clone()
+    batch = B.KVBatch(s.batch.tables, offsets, lens, 64, 40, 500)
+    whole, keys, values = s.q, s.k, s.v
+    q, k, v = s.q.cuda(), *(torch.zeros(64, H, D, dtype=s.kind, device="cuda") for _ in range(2))
+    blocks, out = torch.empty(64, H, n, dtype=torch.int32, device="cuda"), torch.empty_like(q)
+
+    def step():
+        B.pk_kv_append(s.cache.handle, batch.c, k, v)
+        B.pk_kv_select(s.cache.handle, batch.c, q, n, 1, 2, blocks)
+        B.pk_kv_attend_blocks(s.cache.handle, batch.c, q, 0.125, blocks, out)
+    step()
+    s.cache.arena.fill_(0xff)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    have = [0, 0, 0, 0]
+    for news in ([16] * 4, [40, 0, 1, 23], [1, 40, 0, 3], [0, 1, 33, 30], [5] * 4, [1] * 4, [0, 0, 0, 40]):
+        s.news, s.lens = news, [a + m for a, m in zip(have, news)]
+        rows = sum(news)
+        s.q, s.k, s.v = whole[:rows], [x[:l] for x, l in zip(keys, s.lens)], [x[:l] for x, l in zip(values, s.lens)]
+        offsets.copy_(torch.tensor([0] + news).cumsum(0).int())
+        lens.copy_(torch.tensor(s.lens, dtype=torch.int32))
+        k[:rows] = torch.cat([x[a:] for x, a in zip(s.k, have)]).cuda()
+        v[:rows] = torch.cat([x[a:] for x, a in zip(s.v, have)]).cuda()
+        k[rows:], v[rows:] = math.nan, math.nan
+        blocks.fill_(-77)
+        out.fill_(math.nan)
+        graph.replay()
+        torch.cuda.synchronize()
+        for got, x in zip(s.cache.read(s.make_batch(s.lens, s.lens), torch.float32), (s.k, s.v)):
+            assert torch.equal(got.cpu(), definition(torch.cat(x), storage, s.kind))
+        assert torch.equal(blocks[:rows].cpu(), chosen(s, n, 1, 2))
+        assert torch.all(blocks[rows:] == -77) and torch.all(out[rows:].isnan())
+        b = blocks.cpu()
+        key = [torch.arange(l) for l in s.lens]
+        s.check(out, None, 0.125, lambda row, i, pos, h: (key[i] <= pos) & torch.isin(key[i] // 16, b[row, h][b[row, h] >= 0]))
+        have = s.lens
