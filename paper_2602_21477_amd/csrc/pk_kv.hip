@@ -119,9 +119,10 @@ __device__ __forceinline__ float decode(const char *codes, int i)
 // keys are made of the rows that the cache holds once the call is over: those of this call from registers, older ones
 // read back.  They depend on the rows alone, not on the calls that brought them.  Every row is read once
 // and its codes written once, in the order of memory: without the page put together in LDS first, values went out a byte at a time (a
-// prompt of 65536 tokens with its reading back 245 us, with it 199).  Measured: 65536 tokens of 8 heads of 128 from half precision to int8,
-// 403 MB in 107 - 120 us, 3.4 - 3.8 TB/s, the vector units (maxima, codes, bounds) two thirds busy; one token of each of 64 sequences 6.7 us,
-// of which most is the older rows of 512 pages read back for their bounds, after two dependent loads.
+// prompt of 65536 tokens with its reading back 245 us, with it 199).  Measured (medians): 65536 tokens of 8 heads of 128 from half precision to int8,
+// 403 MB in 117 us, 3.4 TB/s, the vector units (maxima, codes, bounds) two thirds busy; from bf16 to bf16, 537 MB in 128 us, 4.2 TB/s; of 64
+// channels 165 - 174 us, 1.2 - 1.5 TB/s.  One token of each of 64 sequences 7.1 us, of which most is the older rows of 512 pages read
+// back for their bounds, after two dependent loads.
 template <int S, int T, int DP>
 __global__ __launch_bounds__(kThreads) void kv_append_kernel(KvDev c, KvBatch b, KvRows kin, KvRows vin)
 {
@@ -254,7 +255,8 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(KvDev c, KvBatch b,
 }
 
 // One workgroup: one page of the batch's tokens, one head: the page into LDS as it lies in memory, out of it by rows, 16 lanes each.
-// Bound by memory: 131071 tokens of 8 heads of 128 from e4m3 to half precision, 805 MB in 152 - 167 us, 4.8 - 5.3 TB/s.
+// Bound by memory: 131071 tokens of 8 heads of 128 from e4m3 to half precision, 805 MB in 168 us (median), 4.8 TB/s; 65536 from bf16 to bf16,
+// 537 MB in 121 us, 4.4 TB/s.
 template <int S, int T, int DP>
 __global__ __launch_bounds__(kThreads) void kv_read_kernel(KvDev c, KvBatch b, char *kout, char *vout)
 {
@@ -316,7 +318,7 @@ __global__ __launch_bounds__(kThreads) void kv_read_kernel(KvDev c, KvBatch b, c
 }
 
 // The bounds of listed pages as numbers, a page a workgroup (and every kMaxBounds-th after it: a grid has 32 bits for its threads).  Small: 64
-// pages of 8 heads 2.8 us, which is a launch and two loads, 1024 pages 5.9 us.
+// pages of 8 heads 3.0 us, which is a launch and two loads, 1024 pages 5.8 us.
 constexpr int64_t kMaxBounds = 1 << 20;
 __global__ __launch_bounds__(kThreads) void kv_bounds_kernel(KvDev c, int dp, const int32_t *pages, int64_t n_listed, float *hi, float *lo)
 {

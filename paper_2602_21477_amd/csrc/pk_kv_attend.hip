@@ -11,6 +11,9 @@ namespace {
 // How the second product's operands are scaled.  The largest weight is 2^top: in half precision that type has the more of its range
 // below it (2^-39 of it is the smallest), in bfloat16 it keeps the products with denormal codes where 32 bits are normal.  Both times a
 // value's scale goes into the weight in units of the largest seen, so that no size of them overflows.
+// One rounding of a weight is of the size of the result's own: against 64 bits a result is off by 2.1e-3, with weights of 32 bits by 1.6e-3
+// (one bfloat16 token), by 2.9e-4 and 2.1e-4 (half precision over e4m3).  A second part would be the second product once more: only where
+// bfloat16 has fewer bits than the codes are worth.
 template <int S, int T>
 struct KvScaling {
     static constexpr bool CODED = kv_coded<S>, HALF = T == PK_F16;
@@ -171,11 +174,13 @@ __device__ __forceinline__ void kv_join_parts(const KvAttend &a, size_t first, i
 // its way.  Where the keys are cut into few parts, the workgroup that ends last joins them, in their order: no launch of its own.
 // blockIdx: row tile of a sequence (sparse: of a token), part of its keys, head; the heads fastest, so that each of the chip's eight
 // parts reads few of them.  ONE: a tile of keys lies in one page.
-// Measured, 8 heads of 128, 4 query heads each: one token of each of 48 sequences of up to 32768 tokens, int8, 1.22 GB in 233 - 240 us,
-// 5.1 TB/s (without what is asked for ahead 446); one token of 1025, bf16, 9.5 us, a chain of lengths, pages, keys and the join.
+// Measured (medians), 8 heads of 128, 4 query heads each: one token of each of 48 sequences of up to 32768 tokens, int8, 1.22 GB in 235 us,
+// 5.2 TB/s (without what is asked for ahead 446); one token of 1025, bf16, 9.2 us, a chain of lengths, pages, keys and the join.
+// Of 256 channels at 16 bits K and V do not fit the 512 registers of one wave a SIMD: 70 - 96 of them go to scratch, 268 - 376 bytes a lane (48
+// sequences of 8192 bf16 tokens, a token each, 787 us, 4.1 TB/s; int8, with no scratch, 296 us, 5.5 TB/s).
 // R: where there are 16 / R queries at most, each of them has R columns, and a column weighs that part of a lane's keys that is its own: a
 // column is a softmax of its own, joined with the others in the end as the waves' are.  For the sparse form, which reads from the
-// caches and is bound by the vector units (1024 tokens, 32 blocks each of int8: 4 query heads a group, R 1 403 us, R 4 352 - 361; 2, R 1 412,
+// caches and is bound by the vector units (1024 tokens, 32 blocks each of int8: 4 query heads a group, R 1 403 us, R 4 352 - 362; 2, R 1 412,
 // R 4 373; 8, R 1 423, R 2 393).
 template <int S, int T, int DP, bool SPARSE, bool ONE, int R>
 __global__ __launch_bounds__(256, DP * KvBytes<S>::v > 128 ? 1 : 2) void kv_rows_kernel(KvAttend a)
@@ -848,9 +853,9 @@ struct KvTiles {
 // masks them.  In every tile that cost a long chunk 2.2 % and mixed chunks 2.7 % (the maximum so far as the products' start value: 2.5 and 5 %,
 // as most tiles raise some query's); so 0.1 - 0.4 and 1 %.  Of 256 channels, which leave no register, in every tile all the same: 2048 tokens
 // over 8192, bf16, 702 us, in the branch 749, not at all 690.  ONE: a tile of keys lies in one page.
-// Measured, bf16, 32 query heads of 128 channels: 4096 tokens over 32768 2.02 - 2.09 ms, 1.0 PFLOP/s.  4.36 million cycles, of which the matrix
-// cores are busy for 45 % and the reads of K and V out of LDS by eight waves take about as many, at 2.08 GHz: the power that the products draw
-// holds the clock there (the same launch over zeros 1.76 ms, at 2.4 GHz).  A product of 8192 x 8192 x 8192 runs at 1.2 - 1.35 PFLOP/s on
+// Measured, bf16, 32 query heads of 128 channels: 4096 tokens over 32768 2.04 ms (median; from card to card and run to run 1.99 - 2.19), 1.0 PFLOP/s.
+// 4.45 million cycles, of which the matrix cores are busy for 44 % and the reads of K and V out of LDS by eight waves take about as many,
+// at 2.1 GHz: the power that the products draw holds the clock there (the same launch over zeros 1.76 ms, at 2.4 GHz).  A product of 8192 x 8192 x 8192 runs at 1.2 - 1.35 PFLOP/s on
 // such numbers, 1.8 on zeros.  First form, each read waited for: 2.71 ms.
 template <int S, int T, int DP, int NW, bool ONE>
 __global__ __launch_bounds__(NW * 64) void kv_tile_kernel(KvAttend a)
@@ -1108,7 +1113,7 @@ __global__ __launch_bounds__(NW * 64) void kv_tile_kernel(KvAttend a)
 }
 
 // The parts of a row joined, in order: 16 threads a row.  Parts have BR rows; a workgroup joins 16 of them.  BR 16: the parts of the kernel
-// for few rows, else of the one for many.  4 - 12 us, a launch and a chain of loads: 48 sequences of 8 heads in 13 parts 11 us.
+// for few rows, else of the one for many.  5 - 12 us, a launch and a chain of loads: 48 sequences of 8 heads in 13 parts 7 us.
 template <int T, int DP, int BR, bool SPARSE>
 __global__ __launch_bounds__(256) void kv_join_kernel(KvAttend a)
 {
@@ -1135,7 +1140,8 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttend a)
 }
 
 // Parts that the keys are cut into (`tiles` tiles of 64 at most): so many that there are `wgs` workgroups, each with `least` tiles at least;
-// more of them, up to `more_wgs`, where each has `much` tiles, as sequences' lengths differ.  Within the room for partial results.
+// more of them, up to `more_wgs`, where each has `much` tiles, as sequences' lengths differ.  Within the room for partial results.  A window does
+// not enter: parts that lie outside it end at once and are joined as parts without a key (one token, window 4096 of 131072: 25 us).
 void cut(KvAttend &a, int64_t items, int64_t tiles, int rows, int64_t wgs, int least, int64_t more_wgs, int much)
 {
     const int64_t room = a.part_floats / ((int64_t)rows * a.part_row) / std::max<int64_t>(items, 1);
@@ -1155,7 +1161,8 @@ hipError_t run(KvAttend a, hipStream_t s)
     // Most rows of queries of a sequence and head that are taken 16 at a time (above: 256 at a time).  Measured in us, 8 heads of 128 channels, 16
     // (256) at a time: bf16, 16 sequences of 64 rows over 8192 keys 182 (168), of 128 rows 309 (171), one of 64 rows over 32768 keys 54 (63), of
     // 128 rows 94 (65).  Codes of 8 bits cost the kernel for many more work for each tile, and half the reads here: int8, 16 sequences of 64 rows
-    // 115 (209), of 128 rows 214 (214), of 256 rows 382 (236); one of 128 rows over 32768 keys 65 (78), of 256 rows 112 (85).
+    // 115 (209), of 128 rows 214 (214), of 256 rows 382 (236); one of 128 rows over 32768 keys 65 (78), of 256 rows 112 (85).  (Other channels
+    // and heads go by the same numbers, unmeasured; so do the numbers of parts.)
     a.few_rows = SPARSE ? INT32_MAX : kv_coded<S> ? kKvFewRows : 64;
     a.part_row = DP;
     // sequences of few rows: unless all may have the same number of new tokens, and that is many.  (The host's numbers are bounds: sequences
@@ -1166,7 +1173,7 @@ hipError_t run(KvAttend a, hipStream_t s)
         const int64_t units = seqs * a.row_tiles, items = units * a.c.H;
         cut(a, items, tiles, 16, 2 * a.num_cu, 4, 16 * a.num_cu, 32);
         // The last part's workgroup joins them where all run at once: one token of 1025 keys 9.9 us, 7.1 + 3.8 with a launch of its own.  Where
-        // there are many its fences cost more than a launch: 48 sequences of up to 32768 keys 494 us, 240 + 12 with the launch.
+        // there are many its fences cost more than a launch: 48 sequences of up to 32768 keys 494 us, 235 + 7 with the launch.
         a.join_here = items * a.n_split <= a.num_cu && items <= kKvArrivals;
         const dim3 grid((unsigned)(items * a.n_split));
         const bool one = a.c.P >= kKvTile;
@@ -1182,8 +1189,10 @@ hipError_t run(KvAttend a, hipStream_t s)
     }
     if constexpr (!SPARSE) {
         if (rows > a.few_rows) {
-            // (a wave holds 32 x DP sums and the queries: of 256 channels these take all 512 registers, one wave a SIMD; of 64 channels 4 waves
-            // a workgroup were slower too: 16 ragged sequences 171 us, 143 with 8)
+            // (a wave holds 32 x DP sums and the queries: of 256 channels these take all 512 registers, one wave a SIMD, and more: 9 go to
+            // scratch at 16 bits, 66 over pages of fewer than 64 tokens, 13 and 24 of int8; 2048 tokens over 8192 708 us at bf16, 970 at int8.  Of
+            // 128 channels and 8 waves int8 has 11 in scratch.  Of 64 channels 4 waves a workgroup were slower: 16 ragged sequences 171 us, 143
+            // with 8)
             constexpr int NW = DP == 256 ? 4 : 8, BR = NW * 32;
             // row tiles of the sequences that have more rows than the others' kernel takes: at most
             const int64_t all = a.b.n_tokens * (int64_t)a.G, longs = std::min<int64_t>(a.b.n_seqs, all / (a.few_rows + 1));
