@@ -541,6 +541,76 @@ int pk_kv_select(pk_kv *kv, const pk_kv_batch *batch, const pk_rows *q, int32_t 
 int pk_kv_attend_blocks(pk_kv *kv, const pk_kv_batch *batch, const pk_rows *q, int32_t n_q_heads, float scale, const int32_t *blocks,
                         int32_t n_blocks, void *out, float *lse, void *stream);
 
+/*
+ * ---------------------------------------------------------------- pages of a key/value cache
+ *
+ * A pool counts for every page of a cache the table entries that hold it, and hands out those that nobody has.  Sequences may
+ * share pages: a fork takes no memory until one of the sharers writes.  All calls but create and free are asynchronous, allocate nothing
+ * and wait for nothing, and may be captured into a graph and replayed with other contents of the DEVICE arrays; calls on one pool (and its cache)
+ * come from one stream at a time.  Their results depend on counts and tables alone, not on what was called before: pages are handed out lowest first.
+ *
+ * Tables are the caller's: DEVICE int32 rows of n_cols entries, an entry outside [0, n_pages) is no page.  Rows that the
+ * pool is to know of come into being by pk_kv_pool_grant (into rows of -1) and pk_kv_pool_fork, or are made known by pk_kv_pool_adopt, and end by
+ * pk_kv_pool_release.  A page stands in a row once.
+ */
+typedef struct pk_kv_pool pk_kv_pool;
+
+typedef struct {
+    int32_t *data;   /* DEVICE                                                         */
+    int64_t stride;  /* entries from one row to the next                               */
+    int32_t n_rows, n_cols;
+} pk_kv_tables;
+
+/* Bytes of memory that the pool of such a cache needs; 0 for an invalid config. */
+size_t pk_kv_pool_bytes(const pk_kv_config *cfg);
+
+/* memory: DEVICE, 256-byte aligned, caller-owned, must stay allocated until pk_kv_pool_free.  All pages are free at first.  Synchronises the device. */
+int pk_kv_pool_create(pk_kv *kv, void *memory, size_t bytes, pk_kv_pool **out);
+
+/* The caller must have synchronised every stream that still uses the pool.  (The cache's handle may have been freed before.) */
+int pk_kv_pool_free(pk_kv_pool *pool);
+
+/* All pages are free again, whatever tables hold. */
+int pk_kv_pool_clear(pk_kv_pool *pool, void *stream);
+
+/* Counts every entry of the tables: for rows that were filled without the pool. */
+int pk_kv_pool_adopt(pk_kv_pool *pool, const pk_kv_tables *tables, void *stream);
+
+/*
+ * Makes every page that the batch's new tokens go into their sequence's own, before they are appended; batch->tables is written.
+ *   no page there          the lowest free one, in the order of sequences and positions
+ *   a page of others too   the same instead of it; what it holds is copied where tokens from before the call are in it.  If all that
+ *                          have the page write into it in this call, the last of them keeps it.
+ * Where none is left the entry becomes -1 (and what is appended there is left out); a page that is not there and would have to hold tokens from before the
+ * call stays away too.
+ *   missing  DEVICE [1] int32 or NULL: the number of such entries
+ */
+int pk_kv_pool_grant(pk_kv_pool *pool, const pk_kv_batch *batch, int32_t *missing, void *stream);
+
+/* Row to[i] becomes the pages of row from[i]'s first lens[from[i]] tokens, and -1, for i = 0 .. n - 1.  What the row held is not
+ * given up.  from, to DEVICE [n], no row twice in `to` and none in both; lens DEVICE [n_rows].  Rows that the tables have not are left out. */
+int pk_kv_pool_fork(pk_kv_pool *pool, const pk_kv_tables *tables, const int32_t *lens, const int32_t *from, const int32_t *to, int32_t n, void *stream);
+
+/* Row rows[i] keeps the pages of its first keep[i] tokens (keep NULL: none); the other entries become -1, and pages that nobody has any more
+ * are free.  rows, keep DEVICE [n].  Rows that the tables have not are left out. */
+int pk_kv_pool_release(pk_kv_pool *pool, const pk_kv_tables *tables, const int32_t *rows, const int32_t *keep, int32_t n, void *stream);
+
+/*
+ * Moves the pages in use into another cache of the same shape and storage (PK_ERR_DIM_MISMATCH else), of any number of pages, side by side and in
+ * their order: the i-th page in use becomes page i, its count with it.  Whatever the other cache and its pool held is lost; this one stays as it is.
+ *   out      tables of the same size, which may be the same ones: the pages' new numbers, -1 for entries that are no page in use
+ *   missing  DEVICE [1] int32 or NULL: pages that the other cache has no room for (their entries are -1)
+ */
+int pk_kv_pool_compact(pk_kv_pool *from, pk_kv_pool *to, const pk_kv_tables *tables, const pk_kv_tables *out, int32_t *missing, void *stream);
+
+/* Owners of every page: counts DEVICE [n_pages] int32, 0 for a free one. */
+int pk_kv_pool_counts(pk_kv_pool *pool, int32_t *counts, void *stream);
+
+/* Copies page from_pages[i] of one cache over page to_pages[i] of another (or the same) of the same shape and storage, with its scales and
+ * bounds.  DEVICE [n] int32; pairs with a number outside its cache are left out; no page twice in to_pages, nor in both where the cache is the same.
+ * Asynchronous. */
+int pk_kv_copy(pk_kv *to, pk_kv *from, const int32_t *to_pages, const int32_t *from_pages, int64_t n, void *stream);
+
 const char *pk_strerror(int status);
 
 #ifdef __cplusplus

@@ -26,7 +26,8 @@ PK_NOALLOC_WORKSPACE_BYTES = 64 << 20
 EXPORTS = ["pk_workspace_reserve", "pk_index_set_emit_cap", "pk_index_set_tile_cap", "pk_index_set_values_cap", "pk_search_noalloc", "pk_search_noalloc_bytes", "pk_search_levels", "pk_search_union", "pk_insert_multi", "pk_delete", "pk_index_split", "pk_index_centroids", "pk_list_ids", "pk_arena_bytes", "pk_index_build", "pk_index_add_arena", "pk_index_compact", "pk_kmeans", "pk_insert", "pk_insert_assigned", "pk_search",
            "pk_search_multi", "pk_coarse", "pk_scan_probes", "pk_index_stats", "pk_list_lengths", "pk_profile_begin",
            "pk_profile_end", "pk_index_free", "pk_kv_arena_bytes", "pk_kv_create", "pk_kv_free", "pk_kv_append", "pk_kv_read",
-           "pk_kv_bounds", "pk_kv_attend", "pk_kv_select", "pk_kv_attend_blocks", "pk_strerror"]
+           "pk_kv_bounds", "pk_kv_attend", "pk_kv_select", "pk_kv_attend_blocks", "pk_kv_pool_bytes", "pk_kv_pool_create", "pk_kv_pool_free", "pk_kv_pool_clear",
+           "pk_kv_pool_adopt", "pk_kv_pool_grant", "pk_kv_pool_fork", "pk_kv_pool_release", "pk_kv_pool_compact", "pk_kv_pool_counts", "pk_kv_copy", "pk_strerror"]
 
 
 class pk_config(C.Structure):
@@ -59,6 +60,10 @@ class pk_kv_batch(C.Structure):
 
 class pk_rows(C.Structure):
     _fields_ = [("data", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64), ("dtype", C.c_int32)]
+
+
+class pk_kv_tables(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("stride", C.c_int64), ("n_rows", C.c_int32), ("n_cols", C.c_int32)]
 
 
 class PancakeError(RuntimeError):
@@ -119,10 +124,23 @@ def lib():
         L.pk_kv_attend.argtypes = [vp, C.POINTER(pk_kv_batch), C.POINTER(pk_rows), i32, C.c_float, i32, vp, vp, vp]
         L.pk_kv_select.argtypes = [vp, C.POINTER(pk_kv_batch), C.POINTER(pk_rows), i32, i32, i32, i32, vp, vp]
         L.pk_kv_attend_blocks.argtypes = [vp, C.POINTER(pk_kv_batch), C.POINTER(pk_rows), i32, C.c_float, vp, i32, vp, vp, vp]
+        tables = C.POINTER(pk_kv_tables)
+        L.pk_kv_pool_bytes.restype = C.c_size_t
+        L.pk_kv_pool_bytes.argtypes = [C.POINTER(pk_kv_config)]
+        L.pk_kv_pool_create.argtypes = [vp, vp, C.c_size_t, C.POINTER(vp)]
+        L.pk_kv_pool_free.argtypes = [vp]
+        L.pk_kv_pool_clear.argtypes = [vp, vp]
+        L.pk_kv_pool_adopt.argtypes = [vp, tables, vp]
+        L.pk_kv_pool_grant.argtypes = [vp, C.POINTER(pk_kv_batch), vp, vp]
+        L.pk_kv_pool_fork.argtypes = [vp, tables, vp, vp, vp, i32, vp]
+        L.pk_kv_pool_release.argtypes = [vp, tables, vp, vp, i32, vp]
+        L.pk_kv_pool_compact.argtypes = [vp, vp, tables, tables, vp, vp]
+        L.pk_kv_pool_counts.argtypes = [vp, vp, vp]
+        L.pk_kv_copy.argtypes = [vp, vp, vp, vp, i64, vp]
         L.pk_strerror.restype = C.c_char_p
         L.pk_strerror.argtypes = [C.c_int]
         for name in EXPORTS:
-            if name not in ("pk_arena_bytes", "pk_strerror", "pk_search_noalloc_bytes", "pk_kv_arena_bytes"):
+            if name not in ("pk_arena_bytes", "pk_strerror", "pk_search_noalloc_bytes", "pk_kv_arena_bytes", "pk_kv_pool_bytes"):
                 getattr(L, name).restype = C.c_int
         _lib = L
     return _lib
@@ -516,6 +534,61 @@ def pk_kv_attend_blocks(handle: int, batch: pk_kv_batch, q, scale: float, blocks
                                      _dev(out, q.dtype, "out"), _dev(lse, torch.float32, "lse"), _stream_of(q.get_device())), "pk_kv_attend_blocks")
 
 
+def pk_kv_pool_bytes(cfg: pk_kv_config) -> int:
+    return int(lib().pk_kv_pool_bytes(C.byref(cfg)))
+
+
+def pk_kv_pool_create(kv: int, memory) -> int:
+    """Returns the handle (an integer).  `memory` is a uint8 CUDA tensor the caller keeps alive."""
+    h = C.c_void_p()
+    _check(lib().pk_kv_pool_create(kv, _dev(memory, torch.uint8, "memory"), memory.numel(), C.byref(h)), "pk_kv_pool_create")
+    return h.value
+
+
+def pk_kv_pool_free(pool: int):
+    _check(lib().pk_kv_pool_free(pool), "pk_kv_pool_free")
+
+
+def _tables(t, what="tables") -> pk_kv_tables:
+    if t.dim() != 2 or not t.is_cuda or t.dtype != torch.int32 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{what}: need an int32 CUDA tensor [sequence, page] with its rows' entries side by side")
+    return pk_kv_tables(t.data_ptr(), t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1]), t.shape[0], t.shape[1])
+
+
+def pk_kv_pool_clear(pool: int, device: int):
+    _check(lib().pk_kv_pool_clear(pool, _stream_of(device)), "pk_kv_pool_clear")
+
+
+def pk_kv_pool_adopt(pool: int, tables):
+    _check(lib().pk_kv_pool_adopt(pool, _tables(tables), _stream_of(tables.get_device())), "pk_kv_pool_adopt")
+
+
+def pk_kv_pool_grant(pool: int, batch: pk_kv_batch, missing, device: int):
+    _check(lib().pk_kv_pool_grant(pool, batch, _dev(missing, torch.int32, "missing"), _stream_of(device)), "pk_kv_pool_grant")
+
+
+def pk_kv_pool_fork(pool: int, tables, lens, sources, targets):
+    _check(lib().pk_kv_pool_fork(pool, _tables(tables), _dev(lens, torch.int32, "lens"), _dev(sources, torch.int32, "sources"), _dev(targets, torch.int32, "targets"), targets.shape[0],
+                                 _stream_of(tables.get_device())), "pk_kv_pool_fork")
+
+
+def pk_kv_pool_release(pool: int, tables, rows, keep=None):
+    _check(lib().pk_kv_pool_release(pool, _tables(tables), _dev(rows, torch.int32, "rows"), _dev(keep, torch.int32, "keep"), rows.shape[0], _stream_of(tables.get_device())),
+           "pk_kv_pool_release")
+
+
+def pk_kv_pool_compact(pool: int, into: int, tables, out, missing=None):
+    _check(lib().pk_kv_pool_compact(pool, into, _tables(tables), _tables(out, "out"), _dev(missing, torch.int32, "missing"), _stream_of(tables.get_device())), "pk_kv_pool_compact")
+
+
+def pk_kv_pool_counts(pool: int, counts):
+    _check(lib().pk_kv_pool_counts(pool, _dev(counts, torch.int32, "counts"), _stream_of(counts.get_device())), "pk_kv_pool_counts")
+
+
+def pk_kv_copy(to: int, source: int, to_pages, from_pages):
+    _check(lib().pk_kv_copy(to, source, _dev(to_pages, torch.int32, "to_pages"), _dev(from_pages, torch.int32, "from_pages"), to_pages.shape[0], _stream_of(to_pages.get_device())), "pk_kv_copy")
+
+
 class KVBatch:
     """One step of a batch of sequences: page tables, row offsets and lengths on the GPU (int32; tensors that are kept and may
     change from step to step), and their bounds on the host."""
@@ -577,6 +650,14 @@ class KVCache:
         pk_kv_bounds(self.handle, pages, hi, lo)
         return hi, lo
 
+    def copy_pages(self, pages, source, source_pages):
+        """Pages of another cache of the same shape and storage (or of this one), with their scales and bounds, over pages of this one."""
+        if pages.dim() != 1 or pages.shape != source_pages.shape:
+            raise ValueError(f"pages: need as many as there are source pages, got {list(pages.shape)} and {list(source_pages.shape)}")
+        if not (pages.get_device() == source_pages.get_device() == self.device == source.device):
+            raise ValueError(f"pages on {pages.device} and {source_pages.device}, caches on {self.arena.device} and {source.arena.device}")
+        pk_kv_copy(self.handle, source.handle, pages, source_pages)
+
     def _outputs(self, q, want_lse):
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
         return out, torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if want_lse else None
@@ -610,6 +691,87 @@ class KVCache:
             pk_kv_free(self.handle)
             self.handle = None
             self.arena = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class KVPool:
+    """The pages of a cache: who has them, and which are free (no arithmetic here).  Tables are int32 tensors [sequence, page] of the caller's, changed in place."""
+
+    def __init__(self, cache):
+        self.handle = None
+        self.cache, self.device = cache, cache.device
+        self.memory = torch.empty(pk_kv_pool_bytes(cache.cfg), dtype=torch.uint8, device=cache.arena.device)
+        with torch.cuda.device(cache.arena.device):
+            self.handle = pk_kv_pool_create(cache.handle, self.memory)
+
+    def _here(self, **tensors):
+        if self.cache.handle is None:
+            raise ValueError("the pool's cache is closed")
+        for what, t in tensors.items():
+            if t is not None and t.get_device() != self.device:
+                raise ValueError(f"{what} is on {t.device}, the pool on {self.memory.device}")
+
+    def clear(self):
+        """All pages are free."""
+        self._here()
+        pk_kv_pool_clear(self.handle, self.device)
+
+    def adopt(self, tables):
+        """Counts the pages of tables that were filled without the pool."""
+        self._here(tables=tables)
+        pk_kv_pool_adopt(self.handle, tables)
+
+    def grant(self, batch):
+        """Pages of their own for the batch's new tokens, shared ones copied first; batch.tables is changed.  Returns the number of entries that got none, an int32 tensor [1]."""
+        self._here()
+        if batch.device != self.device:
+            raise ValueError(f"the batch is on device {batch.device}, the pool on {self.memory.device}")
+        missing = torch.empty(1, dtype=torch.int32, device=self.memory.device)
+        pk_kv_pool_grant(self.handle, batch.c, missing, self.device)
+        return missing
+
+    def fork(self, tables, lens, sources, targets):
+        """Rows `targets` of the tables get the pages of rows `sources` (of lens tokens, by row of the tables)."""
+        self._here(tables=tables, lens=lens, sources=sources, targets=targets)
+        if lens.shape != (tables.shape[0],) or sources.dim() != 1 or sources.shape != targets.shape:
+            raise ValueError("a fork has lens for every row of the tables, and as many sources as targets")
+        pk_kv_pool_fork(self.handle, tables, lens, sources, targets)
+
+    def release(self, tables, rows, keep=None):
+        """Rows of the tables keep the pages of their first `keep` tokens (none where it is left out) and give up the others."""
+        self._here(tables=tables, rows=rows, keep=keep)
+        if rows.dim() != 1 or (keep is not None and keep.shape != rows.shape):
+            raise ValueError("a release has a list of rows, and as many numbers of tokens to keep")
+        pk_kv_pool_release(self.handle, tables, rows, keep)
+
+    def compact(self, into, tables):
+        """Moves the pages in use into the cache of another pool, side by side.  Returns the tables' new entries, and the number of pages that had no room, an int32 tensor [1]."""
+        self._here(tables=tables)
+        into._here()
+        if into.device != self.device:
+            raise ValueError(f"the other pool is on {into.memory.device}, this one on {self.memory.device}")
+        out, missing = torch.empty(tables.shape, dtype=torch.int32, device=tables.device), torch.empty(1, dtype=torch.int32, device=tables.device)
+        pk_kv_pool_compact(self.handle, into.handle, tables, out, missing)
+        return out, missing
+
+    def counts(self):
+        """Owners of every page, int32 [page]: 0 for a free one."""
+        self._here()
+        counts = torch.empty(self.cache.cfg.n_pages, dtype=torch.int32, device=self.memory.device)
+        pk_kv_pool_counts(self.handle, counts)
+        return counts
+
+    def close(self):
+        if self.handle:
+            torch.cuda.synchronize(self.memory.device)
+            pk_kv_pool_free(self.handle)
+            self.handle = None
+            self.memory = None
 
     def __del__(self):
         try:

@@ -19,7 +19,7 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libpancake.so")
 SOURCES = ["pk_api.hip", "pk_scan.hip", "pk_scan_rq.hip", "pk_select.hip", "pk_worklist.hip", "pk_index.hip", "pk_gemm.hip",
-           "pk_kmeans.hip", "pk_kv.hip", "pk_kv_attend.hip", "pk_kv_select.hip"]
+           "pk_kmeans.hip", "pk_kv.hip", "pk_kv_attend.hip", "pk_kv_select.hip", "pk_kv_pool.hip"]
 HEADERS = [os.path.join(CSRC, "pk_internal.h"), os.path.join(CSRC, "pk_worklist_dev.h"),
            os.path.join(CSRC, "pk_select_dev.h"), os.path.join(CSRC, "pk_kv.h"),
            os.path.join(ROOT, "include", "pancake.h")]

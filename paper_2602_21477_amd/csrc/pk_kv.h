@@ -1,6 +1,8 @@
 // Paged key/value cache: what its kernels and its host side share (gfx950 only).
 #pragma once
 
+#include <algorithm>
+
 #include "pk_internal.h"
 
 namespace pk {
@@ -237,11 +239,56 @@ hipError_t launch_kv_select(const KvDev &c, int dp, const KvBatch &b, const KvRo
 int64_t kv_select_workgroups(const KvDev &c, const KvBatch &b, int G); // of that launch, of 256 threads at least
 hipError_t launch_kv_attend(const KvAttend &a, int storage, int dp, int dtype, hipStream_t s);
 
+// ------------------------------------------------------------------ host side
+constexpr uint64_t kKvMagic = 0x70616e63616b7631ull;
+constexpr int64_t kKvMaxGroups = (1 << 24) - 1; // workgroups of 256 threads of a launch (of 512: half as many): a grid has 32 bits for its threads
+constexpr int kKvMaxTouched = 1 << 23;    // pages of one sequence that a call writes or reads: the same
+constexpr int64_t kKvMaxTokens = 1 << 30; // of a sequence: positions and what is added to them fit 32 bits
+
 constexpr int kKvTile = 64;          // keys of one step of the attention kernels
 constexpr int kKvFewRows = 128;      // rows of queries of a sequence and head that the kernel for few takes at most
 constexpr int64_t kKvPartFloats = 16 << 20; // partial results that a cache's workspace has room for: 512 workgroups' of 256 rows of 128 channels
 constexpr int kKvArrivals = 4096;
 constexpr int kKvMaxPage = 128;
 constexpr int kKvMaxSelect = 32768;  // blocks that one query chooses from: their keys lie in LDS
+
+// bytes of a token's key (or value) of one head, dp channels
+inline size_t kv_row_bytes(int storage, int dp) { return storage == PK_I8 || storage == PK_F8 ? (size_t)dp : (size_t)dp * 2; }
+
+// pages that one sequence's new tokens can touch
+inline int kv_touched(const KvDev &c, const KvBatch &b)
+{
+    const int64_t pages = ((int64_t)b.max_new + c.P - 2) / c.P + 1;
+    return (int)(pages < b.cols ? pages : b.cols);
+}
+
+} // namespace pk
+
+struct pk_kv {
+    uint64_t magic;
+    pk_kv_config cfg;
+    int dp;
+    pk::KvDev dev;
+    int num_cu;
+    char *ws; // partial results of split attention
+};
+
+namespace pk {
+
+inline bool kv_live(const pk_kv *kv) { return kv && kv->magic == kKvMagic; }
+
+// The batch as the kernels get it.  *none: there is nothing to do.
+inline int kv_take_batch(const pk_kv *kv, const pk_kv_batch *b, KvBatch *o, bool *none)
+{
+    if (!b || b->n_seqs < 0 || b->n_tokens < 0 || b->max_new < 0 || b->max_len < 0 || b->n_cols < 0) return PK_ERR_INVALID_ARG;
+    if (b->max_new > b->n_tokens) return PK_ERR_INVALID_ARG;
+    if (b->n_seqs > PK_KV_MAX_SEQS) return PK_ERR_UNSUPPORTED;
+    *none = b->n_seqs == 0 || b->n_tokens == 0 || b->max_new == 0;
+    if (*none) return b->n_tokens > 0 ? PK_ERR_INVALID_ARG : PK_OK; // tokens of no sequence
+    if (!b->tables || !b->offsets || !b->lens || b->n_cols < 1 || b->table_stride < b->n_cols || b->max_len < 1) return PK_ERR_INVALID_ARG;
+    if (std::min<int64_t>(b->max_len, (int64_t)b->n_cols * kv->cfg.page_tokens) > kKvMaxTokens) return PK_ERR_UNSUPPORTED;
+    *o = KvBatch{b->tables, b->offsets, b->lens, b->n_seqs, b->n_tokens, b->max_new, b->max_len, b->n_cols, b->table_stride};
+    return PK_OK;
+}
 
 } // namespace pk

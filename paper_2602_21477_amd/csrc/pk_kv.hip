@@ -344,12 +344,6 @@ __global__ __launch_bounds__(kThreads) void kv_bounds_kernel(KvDev c, int dp, co
     }
 }
 
-// pages that one sequence's new tokens can touch
-int touched(const KvDev &c, const KvBatch &b)
-{
-    return (int)std::min<int64_t>(((int64_t)b.max_new + c.P - 2) / c.P + 1, b.cols);
-}
-
 // A launch with LDS for a page's keys and values.
 template <typename K, typename... A>
 hipError_t with_image(K kernel, size_t lds, dim3 grid, hipStream_t s, A... args)
@@ -366,7 +360,7 @@ template <int S, int T>
 hipError_t append_dp(const KvDev &c, int dp, const KvBatch &b, const KvRows &k, const KvRows &v, hipStream_t s)
 {
     constexpr int ES = KvBytes<S>::v;
-    const dim3 grid(touched(c, b), c.H, b.n_seqs);
+    const dim3 grid(kv_touched(c, b), c.H, b.n_seqs);
     if (dp == 64) return with_image(kv_append_kernel<S, T, 64>, image_bytes<ES, 64>(c.P), grid, s, c, b, k, v);
     if (dp == 128) return with_image(kv_append_kernel<S, T, 128>, image_bytes<ES, 128>(c.P), grid, s, c, b, k, v);
     return with_image(kv_append_kernel<S, T, 256>, image_bytes<ES, 256>(c.P), grid, s, c, b, k, v);
@@ -384,7 +378,7 @@ template <int S, int T>
 hipError_t read_dp(const KvDev &c, int dp, const KvBatch &b, char *k, char *v, hipStream_t s)
 {
     constexpr int ES = KvBytes<S>::v;
-    const dim3 grid(touched(c, b), c.H, b.n_seqs);
+    const dim3 grid(kv_touched(c, b), c.H, b.n_seqs);
     if (dp == 64) return with_image(kv_read_kernel<S, T, 64>, image_bytes<ES, 64>(c.P), grid, s, c, b, k, v);
     if (dp == 128) return with_image(kv_read_kernel<S, T, 128>, image_bytes<ES, 128>(c.P), grid, s, c, b, k, v);
     return with_image(kv_read_kernel<S, T, 256>, image_bytes<ES, 256>(c.P), grid, s, c, b, k, v);
@@ -433,21 +427,8 @@ hipError_t launch_kv_bounds(const KvDev &c, int dp, const int32_t *pages, int64_
 
 using namespace pk;
 
-struct pk_kv {
-    uint64_t magic;
-    pk_kv_config cfg;
-    int dp;
-    KvDev dev;
-    int num_cu;
-    char *ws; // partial results of split attention
-};
-
 namespace {
 
-constexpr uint64_t kKvMagic = 0x70616e63616b7631ull;
-constexpr int64_t kMaxGroups = (1 << 24) - 1; // workgroups of 256 threads of a launch (of 512: half as many): a grid has 32 bits for its threads
-constexpr int kMaxTouched = 1 << 23;   // pages of one sequence that a call writes or reads: the same
-constexpr int64_t kMaxTokens = 1 << 30; // of a sequence: positions and what is added to them fit 32 bits
 constexpr int kMaxHeads = 1024; // key/value heads of a cache, and query heads of one of them
 
 size_t up256(size_t v) { return (v + 255) / 256 * 256; }
@@ -465,17 +446,18 @@ bool valid(const pk_kv_config *g)
 size_t lay_out(const pk_kv_config &g, char *base, KvDev *c)
 {
     const int dp = padded(g.head_dim);
-    const size_t es = g.storage == PK_I8 || g.storage == PK_F8 ? 1 : 2, ph = (size_t)g.n_pages * g.n_heads;
+    const size_t row = kv_row_bytes(g.storage, dp), ph = (size_t)g.n_pages * g.n_heads;
     size_t off = 0;
     auto take = [&](size_t n) {
         char *p = base ? base + off : nullptr;
         off = up256(off + n);
         return p;
     };
-    c->k = take(ph * g.page_tokens * dp * es);
-    c->v = take(ph * g.page_tokens * dp * es);
-    const size_t scales = es == 1 ? ph * g.page_tokens * sizeof(float) : 0;
-    c->ks = reinterpret_cast<float *>(take(scales));
+    c->k = take(ph * g.page_tokens * row);
+    c->v = take(ph * g.page_tokens * row);
+    const bool coded = g.storage == PK_I8 || g.storage == PK_F8;
+    const size_t scales = coded ? ph * g.page_tokens * sizeof(float) : 0;
+    c->ks = reinterpret_cast<float *>(take(scales)); // (of a 16-bit storage: nothing lies there)
     c->vs = reinterpret_cast<float *>(take(scales));
     c->bc = reinterpret_cast<int8_t *>(take(ph * 2 * dp));
     c->bs = reinterpret_cast<float *>(take(ph * sizeof(float)));
@@ -487,23 +469,7 @@ size_t lay_out(const pk_kv_config &g, char *base, KvDev *c)
     return off;
 }
 
-bool live(const pk_kv *kv) { return kv && kv->magic == kKvMagic; }
-
 bool row_type(int32_t t) { return t == PK_F32 || t == PK_F16 || t == PK_BF16; }
-
-// The batch as the kernels get it.  *none: there is nothing to do.
-int take_batch(const pk_kv *kv, const pk_kv_batch *b, KvBatch *o, bool *none)
-{
-    if (!b || b->n_seqs < 0 || b->n_tokens < 0 || b->max_new < 0 || b->max_len < 0 || b->n_cols < 0) return PK_ERR_INVALID_ARG;
-    if (b->max_new > b->n_tokens) return PK_ERR_INVALID_ARG;
-    if (b->n_seqs > PK_KV_MAX_SEQS) return PK_ERR_UNSUPPORTED;
-    *none = b->n_seqs == 0 || b->n_tokens == 0 || b->max_new == 0;
-    if (*none) return b->n_tokens > 0 ? PK_ERR_INVALID_ARG : PK_OK; // tokens of no sequence
-    if (!b->tables || !b->offsets || !b->lens || b->n_cols < 1 || b->table_stride < b->n_cols || b->max_len < 1) return PK_ERR_INVALID_ARG;
-    if (std::min<int64_t>(b->max_len, (int64_t)b->n_cols * kv->cfg.page_tokens) > kMaxTokens) return PK_ERR_UNSUPPORTED;
-    *o = KvBatch{b->tables, b->offsets, b->lens, b->n_seqs, b->n_tokens, b->max_new, b->max_len, b->n_cols, b->table_stride};
-    return PK_OK;
-}
 
 int take_rows(const pk_rows *r, KvRows *o)
 {
@@ -528,10 +494,10 @@ int take_queries(const pk_kv *kv, const pk_rows *q, int32_t n_q_heads, KvRows *o
 int attend(pk_kv *kv, const pk_kv_batch *batch, const pk_rows *q, int32_t n_q_heads, float scale, int32_t window, const int32_t *blocks,
            int32_t n_blocks, void *out, float *lse, hipStream_t s)
 {
-    if (!live(kv)) return PK_ERR_BAD_HANDLE;
+    if (!kv_live(kv)) return PK_ERR_BAD_HANDLE;
     KvAttend a{};
     bool none;
-    int rc = take_batch(kv, batch, &a.b, &none);
+    int rc = kv_take_batch(kv, batch, &a.b, &none);
     if (rc != PK_OK) return rc;
     if (window < 0 || !std::isfinite(scale)) return PK_ERR_INVALID_ARG;
     if (none) return PK_OK;
@@ -540,7 +506,7 @@ int attend(pk_kv *kv, const pk_kv_batch *batch, const pk_rows *q, int32_t n_q_he
     if (!out || reinterpret_cast<uintptr_t>(out) % 16) return PK_ERR_INVALID_ARG;
     a.c = kv->dev;
     a.scale = scale;
-    a.window = (int32_t)std::min<int64_t>(window, kMaxTokens); // (a position before the first one less the window fits 32 bits too)
+    a.window = (int32_t)std::min<int64_t>(window, kKvMaxTokens); // (a position before the first one less the window fits 32 bits too)
     a.blocks = blocks;
     a.n_blocks = n_blocks;
     a.out = static_cast<char *>(out);
@@ -549,7 +515,7 @@ int attend(pk_kv *kv, const pk_kv_batch *batch, const pk_rows *q, int32_t n_q_he
     const int64_t H = kv->cfg.n_heads, rows = (int64_t)a.b.n_tokens * a.G;
     const int64_t few = blocks ? (int64_t)a.b.n_tokens * ((a.G + 15) / 16) : a.b.n_seqs * std::min<int64_t>(((int64_t)a.b.max_new * a.G + 15) / 16, kKvFewRows / 16);
     const int64_t many = blocks ? 0 : rows / 128 + a.b.n_seqs;
-    if (few * H > kMaxGroups || many * H > kMaxGroups / 2) return PK_ERR_UNSUPPORTED;
+    if (few * H > kKvMaxGroups || many * H > kKvMaxGroups / 2) return PK_ERR_UNSUPPORTED;
     a.part = reinterpret_cast<float *>(kv->ws);
     a.part_floats = kKvPartFloats;
     a.part_ml = a.part + kKvPartFloats;
@@ -607,7 +573,7 @@ int pk_kv_create(const pk_kv_config *cfg, void *arena, size_t arena_bytes, pk_kv
 
 int pk_kv_free(pk_kv *kv)
 {
-    if (!live(kv)) return PK_ERR_BAD_HANDLE;
+    if (!kv_live(kv)) return PK_ERR_BAD_HANDLE;
     kv->magic = 0;
     const bool ok = hipFree(kv->ws) == hipSuccess;
     delete kv;
@@ -616,35 +582,35 @@ int pk_kv_free(pk_kv *kv)
 
 int pk_kv_append(pk_kv *kv, const pk_kv_batch *batch, const pk_rows *k, const pk_rows *v, void *stream)
 {
-    if (!live(kv)) return PK_ERR_BAD_HANDLE;
+    if (!kv_live(kv)) return PK_ERR_BAD_HANDLE;
     KvBatch b;
     bool none;
-    int rc = take_batch(kv, batch, &b, &none);
+    int rc = kv_take_batch(kv, batch, &b, &none);
     if (rc != PK_OK || none) return rc;
     KvRows kr, vr;
     rc = take_rows(k, &kr);
     if (rc == PK_OK) rc = take_rows(v, &vr);
     if (rc != PK_OK) return rc;
     if (k->dtype != v->dtype) return PK_ERR_INVALID_ARG;
-    if (touched(kv->dev, b) > kMaxTouched) return PK_ERR_UNSUPPORTED;
+    if (kv_touched(kv->dev, b) > kKvMaxTouched) return PK_ERR_UNSUPPORTED;
     return launch_kv_append(kv->dev, kv->cfg.storage, kv->dp, b, kr, vr, k->dtype, static_cast<hipStream_t>(stream)) == hipSuccess ? PK_OK : PK_ERR_HIP;
 }
 
 int pk_kv_read(pk_kv *kv, const pk_kv_batch *batch, void *k_out, void *v_out, int32_t dtype, void *stream)
 {
-    if (!live(kv)) return PK_ERR_BAD_HANDLE;
+    if (!kv_live(kv)) return PK_ERR_BAD_HANDLE;
     KvBatch b;
     bool none;
-    const int rc = take_batch(kv, batch, &b, &none);
+    const int rc = kv_take_batch(kv, batch, &b, &none);
     if (rc != PK_OK || none) return rc;
     if (!k_out || !v_out || !row_type(dtype) || ((reinterpret_cast<uintptr_t>(k_out) | reinterpret_cast<uintptr_t>(v_out)) & 15)) return PK_ERR_INVALID_ARG;
-    if (touched(kv->dev, b) > kMaxTouched) return PK_ERR_UNSUPPORTED;
+    if (kv_touched(kv->dev, b) > kKvMaxTouched) return PK_ERR_UNSUPPORTED;
     return launch_kv_read(kv->dev, kv->cfg.storage, kv->dp, b, k_out, v_out, dtype, static_cast<hipStream_t>(stream)) == hipSuccess ? PK_OK : PK_ERR_HIP;
 }
 
 int pk_kv_bounds(pk_kv *kv, const int32_t *pages, int64_t n, float *hi, float *lo, void *stream)
 {
-    if (!live(kv)) return PK_ERR_BAD_HANDLE;
+    if (!kv_live(kv)) return PK_ERR_BAD_HANDLE;
     if (n < 0 || n > 0x7fffffff) return PK_ERR_INVALID_ARG;
     if (n == 0) return PK_OK;
     if (!pages || !hi || !lo || ((reinterpret_cast<uintptr_t>(hi) | reinterpret_cast<uintptr_t>(lo)) & 15)) return PK_ERR_INVALID_ARG;
@@ -660,7 +626,7 @@ int pk_kv_attend(pk_kv *kv, const pk_kv_batch *batch, const pk_rows *q, int32_t 
 int pk_kv_attend_blocks(pk_kv *kv, const pk_kv_batch *batch, const pk_rows *q, int32_t n_q_heads, float scale, const int32_t *blocks,
                         int32_t n_blocks, void *out, float *lse, void *stream)
 {
-    if (!live(kv)) return PK_ERR_BAD_HANDLE;
+    if (!kv_live(kv)) return PK_ERR_BAD_HANDLE;
     if (n_blocks < 1 || n_blocks > kKvMaxSelect) return PK_ERR_INVALID_ARG;
     if (!blocks && batch && batch->n_tokens > 0) return PK_ERR_INVALID_ARG;
     static const int32_t nothing = 0;
@@ -670,10 +636,10 @@ int pk_kv_attend_blocks(pk_kv *kv, const pk_kv_batch *batch, const pk_rows *q, i
 int pk_kv_select(pk_kv *kv, const pk_kv_batch *batch, const pk_rows *q, int32_t n_q_heads, int32_t n_blocks, int32_t sink, int32_t local,
                  int32_t *out_blocks, void *stream)
 {
-    if (!live(kv)) return PK_ERR_BAD_HANDLE;
+    if (!kv_live(kv)) return PK_ERR_BAD_HANDLE;
     KvBatch b;
     bool none;
-    int rc = take_batch(kv, batch, &b, &none);
+    int rc = kv_take_batch(kv, batch, &b, &none);
     if (rc != PK_OK) return rc;
     if (n_blocks < 1 || sink < 0 || local < 1 || (int64_t)sink + local > n_blocks) return PK_ERR_INVALID_ARG;
     if (n_blocks > kKvMaxSelect || (!none && (std::min<int64_t>(b.max_len, (int64_t)b.cols * kv->cfg.page_tokens) + kv->cfg.page_tokens - 1) / kv->cfg.page_tokens > kKvMaxSelect))
@@ -684,7 +650,7 @@ int pk_kv_select(pk_kv *kv, const pk_kv_batch *batch, const pk_rows *q, int32_t 
     rc = take_queries(kv, q, n_q_heads, &qr, &G);
     if (rc != PK_OK) return rc;
     if (!out_blocks) return PK_ERR_INVALID_ARG;
-    if (kv_select_workgroups(kv->dev, b, G) > kMaxGroups) return PK_ERR_UNSUPPORTED;
+    if (kv_select_workgroups(kv->dev, b, G) > kKvMaxGroups) return PK_ERR_UNSUPPORTED;
     return launch_kv_select(kv->dev, kv->dp, b, qr, q->dtype, G, n_blocks, sink, local, kv->num_cu, out_blocks, static_cast<hipStream_t>(stream)) == hipSuccess
                ? PK_OK
                : PK_ERR_HIP;

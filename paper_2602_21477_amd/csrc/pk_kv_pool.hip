@@ -1,0 +1,577 @@
+// Pages of a key/value cache: who has them, which are free, giving them to sequences, sharing, copying and moving them.
+// See include/pancake.h for the contract.  Integer work on tables and counts; pages themselves move at the rate of a copy.
+// Every result is a function of the inputs alone: counts are sums, pages are handed out by rank (the lowest free ones in the order
+// of sequences and positions), and no order of atomics decides anything.
+#include <algorithm>
+#include <new>
+
+#include "pk_kv.h"
+
+namespace pk {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kGrantThreads = 1024; // of the one workgroup that hands out pages
+constexpr int64_t kMaxPageGroups = 1 << 20; // workgroups that copy pages of a list or a cache, in turns where there are more pages
+
+struct KvPool {
+    uint32_t n_pages, n_words;
+    int32_t *refs;          // [n_pages] table entries that hold the page
+    int32_t *users, *last;  // [n_pages] of a call: sequences that write into a shared page, and the last one plus 1; zeros between calls
+    int32_t *list;          // [n_pages] free pages that a call hands out
+    uint32_t *bits;         // [n_words] free pages, 32 a word (beyond n_pages: 0)
+    int32_t *rank;          // [n_words] of a call: pages in use before a word's
+    int32_t *base, *copy_to, *copy_from; // [PK_KV_MAX_SEQS] of a call: pages that the sequences before need; the page copied for a sequence, or -1
+};
+
+// The regions of an arena, bytes of a page each.
+constexpr int kRegions = 7;
+struct KvMove {
+    char *to[kRegions];
+    const char *from[kRegions];
+    uint32_t bytes[kRegions];
+    uint32_t to_pages, from_pages;
+};
+
+// One page of every region, by `pieces` workgroups.  Reads are asked for four at a time.
+__device__ __forceinline__ void copy_page(const KvMove &m, uint32_t dst, uint32_t src, int piece, int pieces)
+{
+#pragma unroll 1
+    for (int r = 0; r < kRegions; ++r) {
+        const uint32_t bytes = m.bytes[r];
+        char *to = m.to[r] + (size_t)dst * bytes;
+        const char *from = m.from[r] + (size_t)src * bytes;
+        if (bytes % 16 == 0) {
+            const uint32_t n = bytes / 16, step = pieces * kThreads;
+            for (uint32_t i = piece * kThreads + threadIdx.x; i < n; i += 4 * step) {
+                u32x4 w[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (i + k * step < n) w[k] = *reinterpret_cast<const u32x4 *>(from + (size_t)(i + k * step) * 16);
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (i + k * step < n) *reinterpret_cast<u32x4 *>(to + (size_t)(i + k * step) * 16) = w[k];
+            }
+        } else {
+            for (uint32_t i = piece * kThreads + threadIdx.x; i < bytes / 4; i += pieces * kThreads)
+                *reinterpret_cast<uint32_t *>(to + (size_t)i * 4) = *reinterpret_cast<const uint32_t *>(from + (size_t)i * 4);
+        }
+    }
+}
+
+__global__ __launch_bounds__(kThreads) void kv_copy_kernel(KvMove m, const int32_t *dst, const int32_t *src, int64_t n)
+{
+    for (int64_t i = blockIdx.x; i < n; i += gridDim.x) {
+        const uint32_t d = (uint32_t)dst[i], s = (uint32_t)src[i];
+        if (d < m.to_pages && s < m.from_pages) copy_page(m, d, s, blockIdx.y, gridDim.y);
+    }
+}
+
+// One more owner of a page (whose count may have been zero).
+__device__ __forceinline__ void take_page(const KvPool &p, uint32_t page)
+{
+    if (atomicAdd(&p.refs[page], 1) == 0) atomicAnd(&p.bits[page >> 5], ~(1u << (page & 31)));
+}
+// One owner less; a page that nobody had stays so.
+__device__ __forceinline__ void drop_page(const KvPool &p, uint32_t page)
+{
+    const int was = atomicSub(&p.refs[page], 1);
+    if (was == 1) atomicOr(&p.bits[page >> 5], 1u << (page & 31));
+    else if (was <= 0) atomicAdd(&p.refs[page], 1);
+}
+
+__global__ __launch_bounds__(kThreads) void kv_clear_kernel(KvPool p)
+{
+    const size_t step = (size_t)gridDim.x * kThreads;
+    for (size_t i = (size_t)blockIdx.x * kThreads + threadIdx.x; i < p.n_pages; i += step) {
+        p.refs[i] = p.users[i] = p.last[i] = 0;
+        if (i < p.n_words) p.bits[i] = (i + 1) * 32 <= p.n_pages ? ~0u : (1u << (p.n_pages & 31)) - 1;
+    }
+}
+
+__global__ __launch_bounds__(kThreads) void kv_adopt_kernel(KvPool p, pk_kv_tables t)
+{
+    for (int64_t row = blockIdx.x; row < t.n_rows; row += gridDim.x)
+        for (int j = threadIdx.x; j < t.n_cols; j += kThreads) {
+            const uint32_t page = (uint32_t)t.data[row * t.stride + j];
+            if (page < p.n_pages) take_page(p, page);
+        }
+}
+
+__global__ __launch_bounds__(kThreads) void kv_fork_kernel(KvPool p, pk_kv_tables t, const int32_t *lens, const int32_t *from, const int32_t *to, int logP, int P)
+{
+    const int f = from[blockIdx.x], d = to[blockIdx.x];
+    if ((uint32_t)f >= (uint32_t)t.n_rows || (uint32_t)d >= (uint32_t)t.n_rows) return;
+    const int pages = (int)(((int64_t)max(lens[f], 0) + P - 1) >> logP);
+    for (int j = threadIdx.x; j < t.n_cols; j += kThreads) {
+        const uint32_t page = j < pages ? (uint32_t)t.data[f * t.stride + j] : ~0u;
+        if (page < p.n_pages) take_page(p, page);
+        t.data[d * t.stride + j] = page < p.n_pages ? (int32_t)page : -1;
+    }
+}
+
+__global__ __launch_bounds__(kThreads) void kv_release_kernel(KvPool p, pk_kv_tables t, const int32_t *rows, const int32_t *keep, int logP, int P)
+{
+    const int row = rows[blockIdx.x];
+    if ((uint32_t)row >= (uint32_t)t.n_rows) return;
+    const int64_t kept = keep ? ((int64_t)max(keep[blockIdx.x], 0) + P - 1) >> logP : 0;
+    for (int64_t j = kept + threadIdx.x; j < t.n_cols; j += kThreads) {
+        // (exchanged: an entry of a row that is listed twice is given up once)
+        const uint32_t page = (uint32_t)atomicExch(&t.data[row * t.stride + j], -1);
+        if (page < p.n_pages) drop_page(p, page);
+    }
+}
+
+__global__ __launch_bounds__(kThreads) void kv_counts_kernel(KvPool p, int32_t *out)
+{
+    const size_t step = (size_t)gridDim.x * kThreads;
+    for (size_t i = (size_t)blockIdx.x * kThreads + threadIdx.x; i < p.n_pages; i += step) out[i] = p.refs[i];
+}
+
+// Sum over the threads before this one, and over all; sums: one for each wave.
+__device__ __forceinline__ int scan(int v, int *sums, int &total)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int upto = v;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const int x = __shfl_up(upto, d);
+        if (lane >= d) upto += x;
+    }
+    __syncthreads(); // (sums may still be read from before)
+    if (lane == 63) sums[wave] = upto;
+    __syncthreads();
+    int before = 0;
+    total = 0;
+    for (int w = 0; w < (int)blockDim.x / 64; ++w) {
+        before += w < wave ? sums[w] : 0;
+        total += sums[w];
+    }
+    return before + upto - v;
+}
+
+// Pages for a batch's new tokens, by one workgroup; a sequence has W lanes, a lane an entry of its table at a time.
+//   1  entries that hold a page of several owners are counted, and the last sequence with each is noted
+//   2  what an entry needs is decided and written in its place (-1: a page; -2 - page: a page instead of that one), needs are summed over the sequences
+//   3  the lowest free pages, as many as are needed
+//   4  entries get theirs by rank; counts, and the list of pages to be copied, which the next launch does
+// Everything fits registers and the caches: the time is that of four chains of dependent loads.
+__global__ __launch_bounds__(kGrantThreads) void kv_grant_kernel(KvPool p, KvBatch b, int P, int logP, int W, int32_t *missing)
+{
+    __shared__ int sums[kGrantThreads / 64];
+    __shared__ int lost; // pages that are not there and would have to hold older tokens
+    const int tid = threadIdx.x, groups = kGrantThreads / W, in = tid & (W - 1), group = tid / W;
+    const int shift = (tid & 63) & ~(W - 1);
+    const unsigned long long mine = (W == 64 ? ~0ull : (1ull << W) - 1) << shift, below = mine & ((1ull << (tid & 63)) - 1);
+    int32_t *tables = const_cast<int32_t *>(b.tables);
+    if (tid == 0) lost = 0;
+    __syncthreads();
+
+    // entries lp0 .. lp1 of a sequence are those that the call's tokens go into; `begin`: the first new position
+    struct Part {
+        int32_t *row;
+        int begin, lp0, lp1;
+    };
+    auto part = [&](int s) __attribute__((always_inline)) {
+        Part r{nullptr, 0, 0, -1};
+        if (s >= b.n_seqs) return r;
+        const KvSeq q = kv_seq(b, s, P);
+        r.row = tables + (size_t)s * b.table_stride;
+        r.begin = max(q.len - q.m, 0);
+        if (q.m > 0 && q.len > 0) r.lp0 = r.begin >> logP, r.lp1 = (q.len - 1) >> logP;
+        return r;
+    };
+
+    for (int s = group; s < b.n_seqs; s += groups) {
+        const Part r = part(s);
+        for (int j = r.lp0 + in; j <= r.lp1; j += W) {
+            const uint32_t page = (uint32_t)r.row[j];
+            if (page < p.n_pages && p.refs[page] > 1) {
+                atomicAdd(&p.users[page], 1);
+                atomicMax(&p.last[page], s + 1);
+            }
+        }
+    }
+    __threadfence();
+    __syncthreads();
+
+    int need = 0;
+    for (int s0 = 0; s0 < b.n_seqs; s0 += groups) {
+        const int s = s0 + group;
+        const Part r = part(s);
+        int n = 0;
+        for (int j = r.lp0 + in; j - in <= r.lp1; j += W) { // (all lanes of a group in step)
+            bool wants = false;
+            if (j <= r.lp1) {
+                const uint32_t page = (uint32_t)r.row[j];
+                const bool there = page < p.n_pages;
+                if (there) {
+                    // (written by other waves: read where their atomics wrote)
+                    const int refs = p.refs[page], users = __hip_atomic_load(&p.users[page], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT),
+                              last = __hip_atomic_load(&p.last[page], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                    wants = refs > 1 && (users < refs || last != s + 1);
+                    if (wants) r.row[j] = -2 - (int32_t)page;
+                } else {
+                    wants = r.begin <= j << logP;
+                    if (!wants) atomicAdd(&lost, 1);
+                    r.row[j] = -1;
+                }
+            }
+            n += __popcll(__ballot(wants) & mine);
+        }
+        int total;
+        const int before = scan(in == 0 ? n : 0, sums, total);
+        if (in == 0 && s < b.n_seqs) p.base[s] = need + before;
+        need += total;
+    }
+
+    int have = 0;
+    for (uint32_t w0 = 0; w0 < p.n_words && have < need; w0 += kGrantThreads * 4) {
+        uint32_t word[4];
+        int n = 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            word[k] = w0 + tid * 4 + k < p.n_words ? p.bits[w0 + tid * 4 + k] : 0;
+            n += __popc(word[k]);
+        }
+        int total, at = have + scan(n, sums, total);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            for (uint32_t w = word[k]; w && at < need; w &= w - 1) p.list[at++] = (int32_t)((w0 + tid * 4 + k) * 32 + __ffs(w) - 1);
+        have += total;
+    }
+    __threadfence();
+    __syncthreads();
+
+    for (int s = group; s < b.n_seqs; s += groups) {
+        const Part r = part(s);
+        int at = p.base[s];
+        if (in == 0) p.copy_to[s] = -1;
+        for (int j = r.lp0 + in; j - in <= r.lp1; j += W) {
+            const bool inside = j <= r.lp1;
+            const int32_t entry = inside ? r.row[j] : 0;
+            const bool older = r.begin > j << logP; // the page has tokens from before the call
+            const bool wants = inside && (entry < -1 || (entry == -1 && !older));
+            const unsigned long long all = __ballot(wants) & mine;
+            const int rank = at + __popcll(all & below);
+            at += __popcll(all);
+            if (!inside) continue;
+            const int32_t old = entry < -1 ? -2 - entry : entry;
+            if (old >= 0) p.users[old] = p.last[old] = 0;
+            if (!wants) continue;
+            const int32_t page = rank < have ? p.list[rank] : -1;
+            r.row[j] = page;
+            if (entry < -1) atomicSub(&p.refs[old], 1); // (it keeps one owner at least)
+            if (page < 0) continue;
+            p.refs[page] = 1;
+            atomicAnd(&p.bits[page >> 5], ~(1u << (page & 31)));
+            if (entry < -1 && older) {
+                p.copy_from[s] = old;
+                p.copy_to[s] = page;
+            }
+        }
+    }
+    if (tid == 0 && missing) *missing = max(need - have, 0) + lost;
+}
+
+__global__ __launch_bounds__(kThreads) void kv_granted_copy_kernel(KvPool p, KvMove m)
+{
+    const int32_t to = p.copy_to[blockIdx.x];
+    if (to >= 0) copy_page(m, (uint32_t)to, (uint32_t)p.copy_from[blockIdx.x], blockIdx.y, gridDim.y);
+}
+
+__device__ __forceinline__ uint32_t in_use(const KvPool &p, uint32_t word)
+{
+    const uint32_t there = (word + 1) * 32ull <= p.n_pages ? ~0u : (1u << (p.n_pages & 31)) - 1;
+    return ~p.bits[word] & there;
+}
+
+// Pages in use before each word's, by one workgroup: 32768 words, a million pages, a step.
+__global__ __launch_bounds__(kGrantThreads) void kv_rank_kernel(KvPool from, KvPool to, int32_t *missing)
+{
+    __shared__ int sums[kGrantThreads / 64];
+    constexpr int EACH = 32;
+    int upto = 0;
+    for (uint32_t w0 = 0; w0 < from.n_words; w0 += kGrantThreads * EACH) {
+        const uint32_t first = w0 + threadIdx.x * EACH;
+        int n = 0;
+        for (uint32_t w = first; w < min(first + EACH, from.n_words); ++w) n += __popc(in_use(from, w));
+        int total, at = upto + scan(n, sums, total);
+        for (uint32_t w = first; w < min(first + EACH, from.n_words); ++w) {
+            from.rank[w] = at;
+            at += __popc(in_use(from, w));
+        }
+        upto += total;
+    }
+    if (threadIdx.x == 0) {
+        from.base[0] = upto;
+        if (missing) *missing = max(upto - (int)min(to.n_pages, 0x7fffffffu), 0);
+    }
+}
+
+// The number among the pages in use; -1 for a page that is not.
+__device__ __forceinline__ int32_t rank_of(const KvPool &p, uint32_t page)
+{
+    if (page >= p.n_pages) return -1;
+    const uint32_t w = in_use(p, page >> 5), bit = 1u << (page & 31);
+    return w & bit ? p.rank[page >> 5] + __popc(w & (bit - 1)) : -1;
+}
+
+__global__ __launch_bounds__(kThreads) void kv_rename_kernel(KvPool from, KvPool to, pk_kv_tables in, pk_kv_tables out)
+{
+    const size_t step = (size_t)gridDim.x * kThreads, me = (size_t)blockIdx.x * kThreads + threadIdx.x;
+    for (size_t i = me; i < (size_t)in.n_rows * in.n_cols; i += step) {
+        const size_t row = i / in.n_cols, col = i % in.n_cols;
+        const int32_t name = rank_of(from, (uint32_t)in.data[row * in.stride + col]);
+        out.data[row * out.stride + col] = (uint32_t)name < to.n_pages ? name : -1;
+    }
+    const uint32_t used = min((uint32_t)from.base[0], to.n_pages);
+    for (size_t i = me; i < to.n_pages; i += step) {
+        if (i >= used) to.refs[i] = 0;
+        to.users[i] = to.last[i] = 0;
+        if (i < to.n_words) {
+            const uint32_t there = (i + 1) * 32 <= to.n_pages ? ~0u : (1u << (to.n_pages & 31)) - 1;
+            to.bits[i] = there & (i * 32 >= used ? ~0u : used - i * 32 >= 32 ? 0u : ~((1u << (used & 31)) - 1));
+        }
+    }
+}
+
+__global__ __launch_bounds__(kThreads) void kv_move_kernel(KvPool from, KvPool to, KvMove m)
+{
+    for (uint32_t page = blockIdx.x; page < from.n_pages; page += gridDim.x) {
+        const int32_t name = rank_of(from, page);
+        if ((uint32_t)name >= to.n_pages) continue;
+        copy_page(m, (uint32_t)name, page, blockIdx.y, gridDim.y);
+        if (threadIdx.x == 0 && blockIdx.y == 0) to.refs[name] = from.refs[page];
+    }
+}
+
+} // namespace
+} // namespace pk
+
+// ------------------------------------------------------------------ host side
+
+using namespace pk;
+
+struct pk_kv_pool {
+    uint64_t magic;
+    pk_kv kv; // (the cache's numbers as they are; its handle may go first)
+    KvPool dev;
+};
+
+namespace {
+
+constexpr uint64_t kPoolMagic = 0x70616e63706f6f6cull;
+
+bool live(const pk_kv_pool *p) { return p && p->magic == kPoolMagic; }
+
+// Regions of the pool's memory; base may be null (sizes only).
+size_t lay_out(int64_t n_pages, char *base, KvPool *p)
+{
+    const size_t n = (size_t)n_pages, words = (n + 31) / 32;
+    size_t off = 0;
+    auto take = [&](size_t count) {
+        char *at = base ? base + off : nullptr;
+        off += (count * 4 + 255) / 256 * 256;
+        return reinterpret_cast<int32_t *>(at);
+    };
+    p->n_pages = (uint32_t)n;
+    p->n_words = (uint32_t)words;
+    p->refs = take(n);
+    p->users = take(n);
+    p->last = take(n);
+    p->list = take(n);
+    p->bits = reinterpret_cast<uint32_t *>(take(words));
+    p->rank = take(words);
+    p->base = take(PK_KV_MAX_SEQS);
+    p->copy_to = take(PK_KV_MAX_SEQS);
+    p->copy_from = take(PK_KV_MAX_SEQS);
+    return off;
+}
+
+KvMove move_between(const pk_kv &to, const pk_kv &from)
+{
+    const size_t H = from.cfg.n_heads, P = from.cfg.page_tokens, dp = from.dp, row = kv_row_bytes(from.cfg.storage, from.dp);
+    const size_t scales = row < 2 * dp ? H * P * sizeof(float) : 0;
+    const size_t bytes[kRegions] = {H * P * row, H * P * row, scales, scales, 0, H * 2 * dp, H * sizeof(float)};
+    auto regions = [](const KvDev &c, char *(&r)[kRegions]) {
+        char *all[kRegions] = {c.k, c.v, reinterpret_cast<char *>(c.ks), reinterpret_cast<char *>(c.vs), nullptr, reinterpret_cast<char *>(c.bc), reinterpret_cast<char *>(c.bs)};
+        std::copy(all, all + kRegions, r);
+    };
+    KvMove m{};
+    char *source[kRegions];
+    regions(to.dev, m.to);
+    regions(from.dev, source);
+    for (int i = 0; i < kRegions; ++i) m.from[i] = source[i], m.bytes[i] = (uint32_t)bytes[i];
+    m.to_pages = to.dev.n_pages;
+    m.from_pages = from.dev.n_pages;
+    return m;
+}
+
+// Caches whose pages are alike.
+bool alike(const pk_kv_config &a, const pk_kv_config &b)
+{
+    return a.n_heads == b.n_heads && a.head_dim == b.head_dim && a.page_tokens == b.page_tokens && a.storage == b.storage;
+}
+
+// Workgroups that share a page, so that a few pages have the chip: of about 16 KB of it each where there are many pages.
+int pieces_of(const KvMove &m, int64_t pages, int num_cu)
+{
+    size_t bytes = 0;
+    for (uint32_t x : m.bytes) bytes += x;
+    const int64_t most = std::max<int64_t>((int64_t)(bytes / (8 << 10)), 1), wanted = std::max<int64_t>(8 * (int64_t)num_cu / std::max<int64_t>(pages, 1), 1);
+    return (int)std::min(most, wanted);
+}
+
+bool valid(const pk_kv_tables *t, bool *none)
+{
+    if (!t || t->n_rows < 0 || t->n_cols < 0) return false;
+    *none = t->n_rows == 0 || t->n_cols == 0;
+    return *none || (t->data && t->stride >= t->n_cols);
+}
+
+int done() { return hipGetLastError() == hipSuccess ? PK_OK : PK_ERR_HIP; }
+
+unsigned threads_for(size_t n, int num_cu) { return (unsigned)std::max<size_t>(std::min<size_t>((n + kThreads - 1) / kThreads, (size_t)num_cu * 8), 1); }
+
+void clear(const pk_kv_pool *pool, hipStream_t s)
+{
+    kv_clear_kernel<<<threads_for(pool->dev.n_pages, pool->kv.num_cu), kThreads, 0, s>>>(pool->dev);
+}
+
+} // namespace
+
+extern "C" {
+
+size_t pk_kv_pool_bytes(const pk_kv_config *cfg)
+{
+    KvPool p;
+    return pk_kv_arena_bytes(cfg) ? lay_out(cfg->n_pages, nullptr, &p) : 0;
+}
+
+int pk_kv_pool_create(pk_kv *kv, void *memory, size_t bytes, pk_kv_pool **out)
+{
+    if (!out) return PK_ERR_INVALID_ARG;
+    *out = nullptr;
+    if (!kv_live(kv)) return PK_ERR_BAD_HANDLE;
+    if (!memory || (reinterpret_cast<uintptr_t>(memory) & 255)) return PK_ERR_INVALID_ARG;
+    if (bytes < pk_kv_pool_bytes(&kv->cfg)) return PK_ERR_NOMEM;
+    pk_kv_pool *pool = new (std::nothrow) pk_kv_pool();
+    if (!pool) return PK_ERR_NOMEM;
+    pool->kv = *kv;
+    lay_out(kv->cfg.n_pages, static_cast<char *>(memory), &pool->dev);
+    clear(pool, nullptr);
+    if (done() != PK_OK || hipDeviceSynchronize() != hipSuccess) {
+        (void)hipGetLastError();
+        delete pool;
+        return PK_ERR_HIP;
+    }
+    pool->magic = kPoolMagic;
+    *out = pool;
+    return PK_OK;
+}
+
+int pk_kv_pool_free(pk_kv_pool *pool)
+{
+    if (!live(pool)) return PK_ERR_BAD_HANDLE;
+    pool->magic = 0;
+    delete pool;
+    return PK_OK;
+}
+
+int pk_kv_pool_clear(pk_kv_pool *pool, void *stream)
+{
+    if (!live(pool)) return PK_ERR_BAD_HANDLE;
+    clear(pool, static_cast<hipStream_t>(stream));
+    return done();
+}
+
+int pk_kv_pool_adopt(pk_kv_pool *pool, const pk_kv_tables *tables, void *stream)
+{
+    if (!live(pool)) return PK_ERR_BAD_HANDLE;
+    bool none;
+    if (!valid(tables, &none)) return PK_ERR_INVALID_ARG;
+    if (none) return PK_OK;
+    kv_adopt_kernel<<<(unsigned)std::min<int64_t>(tables->n_rows, kMaxPageGroups), kThreads, 0, static_cast<hipStream_t>(stream)>>>(pool->dev, *tables);
+    return done();
+}
+
+int pk_kv_pool_grant(pk_kv_pool *pool, const pk_kv_batch *batch, int32_t *missing, void *stream)
+{
+    if (!live(pool)) return PK_ERR_BAD_HANDLE;
+    KvBatch b{};
+    bool none;
+    const int rc = kv_take_batch(&pool->kv, batch, &b, &none);
+    if (rc != PK_OK) return rc;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    if (none) b.n_seqs = 0; // (the number of missing pages is written all the same)
+    int W = 1;
+    while (!none && W < 64 && W < kv_touched(pool->kv.dev, b)) W *= 2;
+    kv_grant_kernel<<<1, kGrantThreads, 0, s>>>(pool->dev, b, pool->kv.dev.P, pool->kv.dev.logP, W, missing);
+    if (!none) {
+        const KvMove m = move_between(pool->kv, pool->kv);
+        kv_granted_copy_kernel<<<dim3(b.n_seqs, pieces_of(m, b.n_seqs, pool->kv.num_cu)), kThreads, 0, s>>>(pool->dev, m);
+    }
+    return done();
+}
+
+int pk_kv_pool_fork(pk_kv_pool *pool, const pk_kv_tables *tables, const int32_t *lens, const int32_t *from, const int32_t *to, int32_t n, void *stream)
+{
+    if (!live(pool)) return PK_ERR_BAD_HANDLE;
+    bool none;
+    if (!valid(tables, &none) || n < 0 || (n > 0 && (!lens || !from || !to))) return PK_ERR_INVALID_ARG;
+    if (n > kKvMaxGroups) return PK_ERR_UNSUPPORTED;
+    if (none || n == 0) return PK_OK;
+    kv_fork_kernel<<<n, kThreads, 0, static_cast<hipStream_t>(stream)>>>(pool->dev, *tables, lens, from, to, pool->kv.dev.logP, pool->kv.dev.P);
+    return done();
+}
+
+int pk_kv_pool_release(pk_kv_pool *pool, const pk_kv_tables *tables, const int32_t *rows, const int32_t *keep, int32_t n, void *stream)
+{
+    if (!live(pool)) return PK_ERR_BAD_HANDLE;
+    bool none;
+    if (!valid(tables, &none) || n < 0 || (n > 0 && !rows)) return PK_ERR_INVALID_ARG;
+    if (n > kKvMaxGroups) return PK_ERR_UNSUPPORTED;
+    if (none || n == 0) return PK_OK;
+    kv_release_kernel<<<n, kThreads, 0, static_cast<hipStream_t>(stream)>>>(pool->dev, *tables, rows, keep, pool->kv.dev.logP, pool->kv.dev.P);
+    return done();
+}
+
+int pk_kv_pool_compact(pk_kv_pool *from, pk_kv_pool *to, const pk_kv_tables *tables, const pk_kv_tables *out, int32_t *missing, void *stream)
+{
+    if (!live(from) || !live(to)) return PK_ERR_BAD_HANDLE;
+    bool none, out_none;
+    if (from == to || !valid(tables, &none) || !valid(out, &out_none)) return PK_ERR_INVALID_ARG;
+    if (tables->n_rows != out->n_rows || tables->n_cols != out->n_cols || from->kv.dev.k == to->kv.dev.k) return PK_ERR_INVALID_ARG;
+    if (!alike(from->kv.cfg, to->kv.cfg)) return PK_ERR_DIM_MISMATCH;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    const int cu = from->kv.num_cu;
+    kv_rank_kernel<<<1, kGrantThreads, 0, s>>>(from->dev, to->dev, missing);
+    const size_t entries = (size_t)tables->n_rows * tables->n_cols;
+    kv_rename_kernel<<<threads_for(std::max<size_t>(entries, to->dev.n_pages), cu), kThreads, 0, s>>>(from->dev, to->dev, *tables, *out);
+    const KvMove m = move_between(to->kv, from->kv);
+    const int64_t pages = from->dev.n_pages;
+    kv_move_kernel<<<dim3((unsigned)std::min(pages, kMaxPageGroups), pieces_of(m, pages, cu)), kThreads, 0, s>>>(from->dev, to->dev, m);
+    return done();
+}
+
+int pk_kv_pool_counts(pk_kv_pool *pool, int32_t *counts, void *stream)
+{
+    if (!live(pool)) return PK_ERR_BAD_HANDLE;
+    if (!counts) return PK_ERR_INVALID_ARG;
+    kv_counts_kernel<<<threads_for(pool->dev.n_pages, pool->kv.num_cu), kThreads, 0, static_cast<hipStream_t>(stream)>>>(pool->dev, counts);
+    return done();
+}
+
+int pk_kv_copy(pk_kv *to, pk_kv *from, const int32_t *to_pages, const int32_t *from_pages, int64_t n, void *stream)
+{
+    if (!kv_live(to) || !kv_live(from)) return PK_ERR_BAD_HANDLE;
+    if (n < 0 || n > 0x7fffffff || (n > 0 && (!to_pages || !from_pages))) return PK_ERR_INVALID_ARG;
+    if (!alike(to->cfg, from->cfg)) return PK_ERR_DIM_MISMATCH;
+    if (n == 0) return PK_OK;
+    const KvMove m = move_between(*to, *from);
+    kv_copy_kernel<<<dim3((unsigned)std::min(n, kMaxPageGroups), pieces_of(m, n, from->num_cu)), kThreads, 0, static_cast<hipStream_t>(stream)>>>(m, to_pages, from_pages, n);
+    return done();
+}
+
+} // extern "C"
