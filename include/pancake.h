@@ -75,7 +75,8 @@ typedef enum {
     PK_F16 = 1,  /* these two: storage types of list vectors                           */
     PK_BF16 = 2, /* rows of a key/value cache's callers, and its storage types: the     */
     PK_I8 = 3,   /* 16-bit ones, and codes of 8 bits with a scale for each row          */
-    PK_F8 = 4    /* (e4m3)                                                              */
+    PK_F8 = 4,   /* (e4m3)                                                              */
+    PK_F4 = 6    /* or of 4 (e2m1)                                                      */
 } pk_dtype;
 
 typedef enum {
@@ -424,13 +425,16 @@ int pk_index_free(pk_index *index);
  *
  * What a search finds is put before a model, which keeps the context that it has read as keys and values, a row of each
  * for every token, layer and head.  These calls hold them for one layer of many agents' sequences in pages (as the lists' delta pages are held: a
- * table for each sequence, tokens appended at its end), in 16 or 8 bits, and attend over them: over everything, or, as a search does
+ * table for each sequence, tokens appended at its end), in 16, 8 or 4 bits, and attend over them: over everything, or, as a search does
  * with its lists, over the blocks that a cheap score of bounds promises the most of.
  *
  * A token's key (or value) of one head is a row of head_dim elements.  Storage of a row x:
  *   PK_F16, PK_BF16  rounded once to nearest even
  *   PK_I8            scale = max|x| * (1/127), codes rint(x * (127 / max|x|)); a row of zeros has scale 0
  *   PK_F8            scale = max|x| * (1/448), codes x * (448 / max|x|) rounded to nearest even e4m3
+ *   PK_F4            scale = max|x| * (1/6), codes x * (6 / max|x|) rounded to nearest even e2m1 (0, 1/2, 1, 3/2, 2, 3, 4, 6); of a key
+ *                    each 32 channels are first multiplied by 2^e and their codes stand for 2^-e of themselves: e the whole number by which
+ *                    the exponent of their largest magnitude, its fraction with it, is below that of the row's, 15 at most
  * all in 32 bits, so that a row's stored value depends on the row alone.  The bounds of a page (and head) are for every channel the
  * largest and the smallest stored value of the keys in it, as int8 codes hi = ceil(max * 127 / a - 2^-10),
  * lo = floor(min * 127 / a + 2^-10) with a = the largest magnitude among them, and the scale a * (1/127).
@@ -453,7 +457,7 @@ typedef struct {
     int32_t n_heads;     /* key/value heads, 1 .. 1024                                 */
     int32_t head_dim;    /* multiple of 8 in [8, PK_KV_MAX_DIM]                        */
     int32_t page_tokens; /* 16, 32, 64 or 128: also the block of pk_kv_select          */
-    int32_t storage;     /* PK_F16, PK_BF16, PK_I8 or PK_F8                            */
+    int32_t storage;     /* PK_F16, PK_BF16, PK_I8, PK_F8 or PK_F4                     */
 } pk_kv_config;
 
 /*

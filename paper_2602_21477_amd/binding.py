@@ -16,7 +16,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libpancake.so")
 
 PK_METRIC_IP, PK_METRIC_L2 = 0, 1
-PK_F32, PK_F16, PK_BF16, PK_I8, PK_F8 = 0, 1, 2, 3, 4
+PK_F32, PK_F16, PK_BF16, PK_I8, PK_F8, PK_F4 = 0, 1, 2, 3, 4, 6
 PK_OK = 0
 PK_ERR_INVALID_ARG, PK_ERR_BAD_HANDLE, PK_ERR_DIM_MISMATCH, PK_ERR_NOMEM, PK_ERR_HIP, PK_ERR_UNSUPPORTED = (
     -1, -2, -3, -4, -5, -6)

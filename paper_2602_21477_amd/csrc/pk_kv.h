@@ -15,28 +15,38 @@ namespace pk {
 //                    attention of 1024 tokens to 32 blocks each of int8: 1.0 of 1.1 million cycles).
 //                    Keys: groups of four tokens, their rows' 16-byte pieces side by side [4][DP * bytes / 16][4 tokens][16 bytes].
 //                    Values: 16 bytes of one channel, 16 or 8 tokens, the channels side by side [1 or 2][DP][16 bytes].
-//   ks, vs [P]       scales of keys and values (8-bit storages)
+//                    4 bits: a key's piece is 32 channels, the even one of two in the lower half of a byte; values: 16 tokens of channel
+//                    32 q + c, then the same of 32 q + 16 + c, [DP / 32 q][16 c][2][8 bytes], the even token in the lower half.
+//   ks, vs [P]       scales of keys and values (coded storages)
+//   ke  [P / 16]     4 bits: 127 - e of every token and 32 channels of its key, whose codes stand for 2^-e of what they else would:
+//                    [DP / 32][4 t][4 i] for token 4 i + t of the 16, so that a lane has its four tokens' side by side
 //   bc  [2][DP]      bounds of the keys (largest, smallest value of each channel) in int8, zero padded
 //   bs  [1]          their scale
 struct KvDev {
     char *k, *v;
     float *ks, *vs;
+    uint8_t *ke;
     int8_t *bc;
     float *bs;
     uint32_t n_pages;
     int32_t H, D, P, logP;
 };
 
-// Where byte `at` of a token's key lies in its page and head, and a token's value of channel d.
-template <int ES, int DP>
+template <int S> constexpr bool kv_coded = S == PK_I8 || S == PK_F8 || S == PK_F4;
+template <int S> constexpr float kv_largest = S == PK_F8 ? 448.f : S == PK_F4 ? 6.f : 127.f;
+template <int S> constexpr int kv_bits = S == PK_F4 ? 4 : S == PK_I8 || S == PK_F8 ? 8 : 16;
+
+// Where byte `at` of a token's key lies in its page and head, of RB bytes a row.
+template <int RB>
 __device__ __forceinline__ int k_place(int tok, int at)
 {
-    return (tok >> 2) * (DP * ES * 4) + (at >> 4) * 64 + (tok & 3) * 16 + (at & 15);
+    return (tok >> 2) * (RB * 4) + (at >> 4) * 64 + (tok & 3) * 16 + (at & 15);
 }
-template <int ES, int DP>
-__device__ __forceinline__ int v_place(int tok, int d)
+// Where the power of two of a token's key lies, for channels 32 group and on.
+template <int DP>
+__device__ __forceinline__ int e_place(int tok, int group)
 {
-    return (tok * ES >> 4) * (DP * 16) + d * 16 + (tok * ES & 15);
+    return ((tok >> 4) * (DP / 32) + group) * 16 + (tok & 3) * 4 + (tok >> 2 & 3);
 }
 
 // One call's batch, as the kernels get it.
@@ -94,11 +104,6 @@ typedef _Float16 half4v __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-
-template <int S> struct KvBytes { static constexpr int v = S == PK_I8 || S == PK_F8 ? 1 : 2; };
-template <int S> constexpr bool kv_coded = S == PK_I8 || S == PK_F8;
-template <int S> constexpr float kv_largest = S == PK_F8 ? 448.f : 127.f;
-
 
 // Rows of the caller's may begin at any element.
 struct __attribute__((packed, aligned(2))) AnyEight16 {
@@ -176,11 +181,28 @@ __device__ __forceinline__ void codes_to(uint32_t w, uint32_t &lo, uint32_t &hi)
     }
 }
 
+// Eight e2m1 codes of 4 bits as elements of type T, times `scale`, a power of two: exact, as a code has two bits and both types have
+// 2^-15 of the smallest.
+template <int T>
+__device__ __forceinline__ u32x4 eight_of_4(uint32_t w, float scale)
+{
+    if constexpr (T == PK_F16)
+        return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 0)), __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 1)),
+                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 2)), __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 3))};
+    else
+        return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0)), __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1)),
+                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2)), __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3))};
+}
+
+// 2^-e of a byte 127 - e.
+__device__ __forceinline__ float power_of(uint32_t byte) { return __uint_as_float(byte << 23); }
+
 // One code of a key, or of a value, as the number that it stands for (before its scale).
 template <int S, bool VALUES>
 __device__ __forceinline__ float code_value(uint8_t c)
 {
-    if constexpr (S == PK_I8 && VALUES) return (float)(c & 0x80 ? -(int)(c & 0x7f) : (int)c);
+    if constexpr (S == PK_F4) return __builtin_amdgcn_cvt_scalef32_pk_f32_fp4((uint32_t)c, 1.f, 0)[0];
+    else if constexpr (S == PK_I8 && VALUES) return (float)(c & 0x80 ? -(int)(c & 0x7f) : (int)c);
     else if constexpr (S == PK_I8) return (float)((int)c - 128);
     else {
         const half2v h = __builtin_bit_cast(half2v, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((uint32_t)c, 1.f, false));
@@ -203,6 +225,7 @@ __device__ __forceinline__ uint8_t to_code(float x, float up)
         const int code = (int)rintf(y);
         return (uint8_t)(!VALUES ? code + 128 : code < 0 ? 0x80 - code : code);
     }
+    if constexpr (S == PK_F4) return (uint8_t)(__builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, y, y, 1.f, 0) & 15u);
     return (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(y, y, 0, false);
 }
 
@@ -253,7 +276,8 @@ constexpr int kKvMaxPage = 128;
 constexpr int kKvMaxSelect = 32768;  // blocks that one query chooses from: their keys lie in LDS
 
 // bytes of a token's key (or value) of one head, dp channels
-inline size_t kv_row_bytes(int storage, int dp) { return storage == PK_I8 || storage == PK_F8 ? (size_t)dp : (size_t)dp * 2; }
+inline size_t kv_row_bytes(int storage, int dp) { return (size_t)dp * (storage == PK_F4 ? 4 : storage == PK_I8 || storage == PK_F8 ? 8 : 16) / 8; }
+inline bool kv_is_coded(int storage) { return storage == PK_I8 || storage == PK_F8 || storage == PK_F4; }
 
 // pages that one sequence's new tokens can touch
 inline int kv_touched(const KvDev &c, const KvBatch &b)

@@ -48,16 +48,36 @@ __device__ __forceinline__ void load_row(float (&x)[E], const char *row, int at,
 }
 
 // A page's keys (or values) as they lie in memory, in LDS: values with 16 bytes more for every 8 channels, so that lanes that share
-// a row write to banks of their own.
+// a row write to banks of their own; values of 4 bits as a byte each.
 template <int ES, int DP>
 __device__ __forceinline__ int v_image(int tok, int d)
 {
     return (tok * ES >> 4) * (DP * 18) + d * 16 + (d >> 3) * 16 + (tok * ES & 15);
 }
-template <int ES, int DP>
+template <int S> constexpr int kv_value_bytes = kv_bits<S> == 16 ? 2 : 1; // of an element there
+template <int S, int DP>
 constexpr size_t image_bytes(int P)
 {
-    return (size_t)P * DP * ES + (size_t)P * ES / 16 * DP * 18;
+    return (size_t)P * DP * kv_bits<S> / 8 + (size_t)P * kv_value_bytes<S> / 16 * DP * 18;
+}
+
+// Sixteen tokens of 4 bits of a channel as bytes, and back.
+__device__ __forceinline__ u32x4 unpack_run(uint32_t a, uint32_t b)
+{
+    u32x4 r;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const uint32_t w = i ? b : a, even = w & 0x0f0f0f0fu, odd = w >> 4 & 0x0f0f0f0fu;
+        r[2 * i] = __builtin_amdgcn_perm(odd, even, 0x05010400u);
+        r[2 * i + 1] = __builtin_amdgcn_perm(odd, even, 0x07030602u);
+    }
+    return r;
+}
+__device__ __forceinline__ uint32_t pack_run(uint32_t a, uint32_t b) // eight of them
+{
+    a &= 0x0f0f0f0fu, b &= 0x0f0f0f0fu; // (what has not been written may be anything)
+    a |= a >> 4, b |= b >> 4;           // bytes 0 and 2 hold two codes each
+    return __builtin_amdgcn_perm(b, a, 0x06040200u);
 }
 
 // What a workgroup does: one page that the batch touches, one head.
@@ -80,11 +100,35 @@ __device__ __forceinline__ bool kv_page_of(const KvDev &c, const KvBatch &b, KvP
     return true;
 }
 
-// E consecutive elements of a row as they are stored: codes with a scale, or 16 bits.
+// Bytes of a lane's E elements of a row: of values in 4 bits, a byte for each.
+template <int S, int E, bool VALUES> constexpr int kv_part = S == PK_F4 && VALUES ? E : E * kv_bits<S> / 8;
+
+// E consecutive elements of a row as they are stored: codes with a scale (keys in 4 bits: and the byte of their power of two), or 16 bits.
 template <int S, int E, bool VALUES>
-__device__ __forceinline__ float encode(const float (&x)[E], char (&codes)[E * KvBytes<S>::v])
+__device__ __forceinline__ float encode(const float (&x)[E], char (&codes)[kv_part<S, E, VALUES>], uint32_t &power)
 {
-    if constexpr (kv_coded<S>) {
+    if constexpr (S == PK_F4) {
+        float most = 0.f;
+#pragma unroll
+        for (int i = 0; i < E; ++i) most = fmaxf(most, fabsf(x[i]));
+        float group = most; // of 32 channels: 32 / E lanes
+#pragma unroll
+        for (int d = 1; d < 32 / E; d *= 2) group = fmaxf(group, __shfl_xor(group, d));
+        most = quarter_max(most);
+        const float up = code_factor(most, kv_largest<S>);
+        float shift = 1.f;
+        if constexpr (!VALUES) {
+            const uint32_t e = min((__float_as_uint(most) - __float_as_uint(group)) >> 23, 15u);
+            power = 127u - e;
+            shift = __uint_as_float((127u + e) << 23);
+        }
+        uint8_t c[E];
+#pragma unroll
+        for (int i = 0; i < E; ++i) c[i] = to_code<S, VALUES>(x[i] * shift, up);
+#pragma unroll
+        for (int i = 0; i < kv_part<S, E, VALUES>; ++i) codes[i] = (char)(VALUES ? c[i] : c[2 * i] | c[2 * i + 1] << 4);
+        return most * (1.f / kv_largest<S>);
+    } else if constexpr (kv_coded<S>) {
         float most = 0.f;
 #pragma unroll
         for (int i = 0; i < E; ++i) most = fmaxf(most, fabsf(x[i]));
@@ -105,7 +149,8 @@ __device__ __forceinline__ float encode(const float (&x)[E], char (&codes)[E * K
 template <int S, bool VALUES>
 __device__ __forceinline__ float decode(const char *codes, int i)
 {
-    if constexpr (kv_coded<S>) return code_value<S, VALUES>((uint8_t)codes[i]);
+    if constexpr (S == PK_F4 && !VALUES) return code_value<S, VALUES>((uint8_t)codes[i >> 1] >> 4 * (i & 1) & 15);
+    else if constexpr (kv_coded<S>) return code_value<S, VALUES>((uint8_t)codes[i]);
     else {
         uint16_t w;
         __builtin_memcpy(&w, codes + 2 * i, 2);
@@ -126,18 +171,21 @@ __device__ __forceinline__ float decode(const char *codes, int i)
 template <int S, int T, int DP>
 __global__ __launch_bounds__(kThreads) void kv_append_kernel(KvDev c, KvBatch b, KvRows kin, KvRows vin)
 {
-    constexpr int ES = KvBytes<S>::v;
+    constexpr int RB = DP * kv_bits<S> / 8, ES = kv_value_bytes<S>;
     constexpr int E = DP / kRowLanes; // elements of a lane
+    constexpr int KB = kv_part<S, E, false>, N = KB < 16 ? KB : 16; // its bytes of a key, which lie in pieces of 16, or in one
+    constexpr bool FOUR = S == PK_F4;
     extern __shared__ __align__(16) char image[];
     __shared__ float red[4][2][DP];
     const int h = blockIdx.y, tid = threadIdx.x;
     KvPage g;
     if (!kv_page_of(c, b, g) || g.page >= c.n_pages) return;
     const int p0 = g.p0, p1 = g.p1;
-    char *kimg = image, *vimg = image + c.P * DP * ES;
+    char *kimg = image, *vimg = image + c.P * RB;
     const size_t ph = (size_t)g.page * c.H + h;
-    char *kp = c.k + ph * c.P * DP * ES;
-    char *vp = c.v + ph * c.P * DP * ES;
+    char *kp = c.k + ph * c.P * RB;
+    char *vp = c.v + ph * c.P * RB;
+    uint8_t *ke = FOUR ? c.ke + ph * c.P * (DP / 32) : nullptr;
     const int sub = tid & (kRowLanes - 1), at = sub * E;
 
     float hi[E], lo[E];
@@ -146,55 +194,62 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(KvDev c, KvBatch b,
         hi[i] = -INFINITY;
         lo[i] = INFINITY;
     }
-    auto bound = [&](const char *codes, float scale) __attribute__((always_inline)) {
+    auto bound = [&](const char *codes, float scale, uint32_t power) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < E; ++i) {
-            const float z = kv_coded<S> ? decode<S, false>(codes, i) * scale : decode<S, false>(codes, i);
+            float z = decode<S, false>(codes, i);
+            if constexpr (FOUR) z *= power_of(power);
+            if constexpr (kv_coded<S>) z *= scale;
             hi[i] = fmaxf(hi[i], z);
             lo[i] = fminf(lo[i], z);
         }
     };
-    constexpr int N = E * ES < 16 ? E * ES : 16; // (a lane's bytes of a row lie in pieces of 16, or in one)
     // rows that were there, several asked for at once
     constexpr int AHEAD = 4;
     for (int r0 = 0; r0 < p0; r0 += AHEAD * kRowsAtOnce) {
-        char codes[AHEAD][E * ES];
+        char codes[AHEAD][KB];
         float scale[AHEAD];
+        uint32_t power[AHEAD];
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k) {
             const int r = min(r0 + k * kRowsAtOnce + tid / kRowLanes, p0 - 1); // (a row twice is no other bound)
 #pragma unroll
-            for (int i = 0; i < E * ES; i += N) __builtin_memcpy(codes[k] + i, kp + k_place<ES, DP>(r, at * ES + i), N);
+            for (int i = 0; i < KB; i += N) __builtin_memcpy(codes[k] + i, kp + k_place<RB>(r, sub * KB + i), N);
             scale[k] = kv_coded<S> ? c.ks[ph * c.P + r] : 1.f;
+            power[k] = FOUR ? ke[e_place<DP>(r, at / 32)] : 0;
         }
 #pragma unroll
-        for (int k = 0; k < AHEAD; ++k) bound(codes[k], scale[k]);
+        for (int k = 0; k < AHEAD; ++k) bound(codes[k], scale[k], power[k]);
     }
     // new rows
     for (int r0 = p0 / kRowsAtOnce * kRowsAtOnce; r0 < p1; r0 += kRowsAtOnce) {
         const int r = r0 + tid / kRowLanes;
         if (r < p0 || r >= p1) continue;
         const int t = g.q.first + (g.base + r - (g.q.len - g.q.m));
-        char codes[E * ES];
+        char codes[KB], vcodes[kv_part<S, E, true>];
+        uint32_t power = 0;
         float x[E], y[E];
         load_row<T, E>(x, kin.data + ((size_t)t * kin.token_stride + (size_t)h * kin.head_stride) * (T == PK_F32 ? 4 : 2), at, c.D);
         load_row<T, E>(y, vin.data + ((size_t)t * vin.token_stride + (size_t)h * vin.head_stride) * (T == PK_F32 ? 4 : 2), at, c.D);
-        const float vscale = encode<S, E, true>(y, codes);
+        const float vscale = encode<S, E, true>(y, vcodes, power);
 #pragma unroll
         for (int i = 0; i < E; ++i) {
-            if constexpr (ES == 1) vimg[v_image<ES, DP>(r, at + i)] = codes[i];
-            else __builtin_memcpy(vimg + v_image<ES, DP>(r, at + i), codes + 2 * i, 2);
+            if constexpr (ES == 1) vimg[v_image<ES, DP>(r, at + i)] = vcodes[i];
+            else __builtin_memcpy(vimg + v_image<ES, DP>(r, at + i), vcodes + 2 * i, 2);
         }
-        const float scale = encode<S, E, false>(x, codes);
+        const float scale = encode<S, E, false>(x, codes, power);
 #pragma unroll
-        for (int i = 0; i < E * ES; i += N) __builtin_memcpy(kimg + k_place<ES, DP>(r, at * ES + i), codes + i, N);
+        for (int i = 0; i < KB; i += N) __builtin_memcpy(kimg + k_place<RB>(r, sub * KB + i), codes + i, N);
+        if constexpr (FOUR) {
+            if (at % 32 == 0) ke[e_place<DP>(r, at / 32)] = (uint8_t)power;
+        }
         if constexpr (kv_coded<S>) {
             if (sub == 0) {
                 c.ks[ph * c.P + r] = scale;
                 c.vs[ph * c.P + r] = vscale;
             }
         }
-        bound(codes, scale);
+        bound(codes, scale, power);
     }
 #pragma unroll
     for (int i = 0; i < E; ++i) {
@@ -234,10 +289,34 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(KvDev c, KvBatch b,
         if (tid == 0) c.bs[ph] = most * (1.f / 127.f);
     }
     // keys: a piece is part of one token; values: 16 or 8 tokens of a channel, one by one where not all of them are new
-    constexpr int VN = 16 / ES, PIECES = DP * ES / 16;
+    constexpr int VN = 16 / ES, PIECES = RB / 16;
     for (int i = (p0 >> 2) * 4 * PIECES + tid; i < ((p1 + 3) >> 2) * 4 * PIECES; i += kThreads) {
         const int tok = i / (4 * PIECES) * 4 + (i & 3);
         if (tok >= p0 && tok < p1) *reinterpret_cast<u32x4 *>(kp + (size_t)i * 16) = *reinterpret_cast<const u32x4 *>(kimg + i * 16);
+    }
+    if constexpr (FOUR) { // 16 tokens of two channels a piece; what is not new is kept
+        for (int i = (p0 >> 4) * (DP / 2) + tid; i < ((p1 + 15) >> 4) * (DP / 2); i += kThreads) {
+            const int tok = i / (DP / 2) * 16, d = i % (DP / 2) / 16 * 32 + i % 16;
+            if (d >= c.D) continue;
+            u32x4 w;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const char *from = vimg + v_image<1, DP>(tok + (j & 1) * 8, d + (j >> 1) * 16);
+                w[j] = pack_run(reinterpret_cast<const uint32_t *>(from)[0], reinterpret_cast<const uint32_t *>(from)[1]);
+            }
+            u32x4 *to = reinterpret_cast<u32x4 *>(vp + (size_t)i * 16);
+            if (tok < p0 || tok + 16 > p1) {
+                const u32x4 old = *to;
+                const unsigned long long upto = p1 - tok >= 16 ? ~0ull : (1ull << 4 * (p1 - tok)) - 1, fresh = upto & (~0ull << 4 * max(p0 - tok, 0));
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t keep = ~(uint32_t)(fresh >> 32 * (j & 1));
+                    w[j] = (w[j] & ~keep) | (old[j] & keep);
+                }
+            }
+            *to = w;
+        }
+        return;
     }
     for (int i = p0 / VN * DP + tid; i < (p1 + VN - 1) / VN * DP; i += kThreads) {
         const int tok = i / DP * VN, d = i % DP;
@@ -260,18 +339,27 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(KvDev c, KvBatch b,
 template <int S, int T, int DP>
 __global__ __launch_bounds__(kThreads) void kv_read_kernel(KvDev c, KvBatch b, char *kout, char *vout)
 {
-    constexpr int ES = KvBytes<S>::v, TS = T == PK_F32 ? 4 : 2, E = DP / kRowLanes;
+    constexpr int RB = DP * kv_bits<S> / 8, ES = kv_value_bytes<S>, TS = T == PK_F32 ? 4 : 2, E = DP / kRowLanes, KB = kv_part<S, E, false>;
+    constexpr bool FOUR = S == PK_F4;
     extern __shared__ __align__(16) char image[];
     const int h = blockIdx.y, tid = threadIdx.x;
     KvPage g;
     if (!kv_page_of(c, b, g)) return;
     const bool there = g.page < c.n_pages;
-    char *kimg = image, *vimg = image + c.P * DP * ES;
+    char *kimg = image, *vimg = image + c.P * RB;
     const size_t ph = (size_t)(there ? g.page : 0) * c.H + h;
-    const char *kp = c.k + ph * c.P * DP * ES, *vp = c.v + ph * c.P * DP * ES;
-    constexpr int N = 16 / ES, PIECES = DP * ES / 16;
+    const char *kp = c.k + ph * c.P * RB, *vp = c.v + ph * c.P * RB;
+    constexpr int N = 16 / ES, PIECES = RB / 16;
     for (int i = (g.p0 >> 2) * 4 * PIECES + tid; i < ((g.p1 + 3) >> 2) * 4 * PIECES; i += kThreads)
         *reinterpret_cast<u32x4 *>(kimg + i * 16) = *reinterpret_cast<const u32x4 *>(kp + (size_t)i * 16);
+    if constexpr (FOUR) {
+        for (int i = (g.p0 >> 4) * (DP / 2) + tid; i < ((g.p1 + 15) >> 4) * (DP / 2); i += kThreads) {
+            const u32x4 w = *reinterpret_cast<const u32x4 *>(vp + (size_t)i * 16);
+            char *to = vimg + v_image<1, DP>(i / (DP / 2) * 16, i % (DP / 2) / 16 * 32 + i % 16);
+            *reinterpret_cast<u32x4 *>(to) = unpack_run(w[0], w[1]);
+            *reinterpret_cast<u32x4 *>(to + v_image<1, DP>(0, 16)) = unpack_run(w[2], w[3]);
+        }
+    } else
     for (int i = g.p0 / N * DP + tid; i < (g.p1 + N - 1) / N * DP; i += kThreads)
         *reinterpret_cast<u32x4 *>(vimg + v_image<ES, DP>(i / DP * N, i % DP)) = *reinterpret_cast<const u32x4 *>(vp + (size_t)i * 16);
     __syncthreads();
@@ -285,15 +373,18 @@ __global__ __launch_bounds__(kThreads) void kv_read_kernel(KvDev c, KvBatch b, c
         }
         const size_t t = (size_t)(g.q.first + (g.base + r - (g.q.len - g.q.m)));
         const size_t o = ((t * c.H + h) * c.D + at) * TS;
-        char codes[E * ES];
-        constexpr int M = E * ES < 16 ? E * ES : 16;
+        char codes[KB];
+        constexpr int M = KB < 16 ? KB : 16;
 #pragma unroll
-        for (int i = 0; i < E * ES; i += M) __builtin_memcpy(codes + i, kimg + k_place<ES, DP>(r, at * ES + i), M);
+        for (int i = 0; i < KB; i += M) __builtin_memcpy(codes + i, kimg + k_place<RB>(r, sub * KB + i), M);
+        float power = 1.f;
+        if constexpr (FOUR) power = !there ? 1.f : power_of(c.ke[ph * c.P * (DP / 32) + e_place<DP>(r, at / 32)]);
         float x[E], y[E];
 #pragma unroll
         for (int i = 0; i < E; ++i) {
             x[i] = there ? decode<S, false>(codes, i) : 0.f;
             y[i] = there ? decode<S, true>(vimg + v_image<ES, DP>(r, at + i), 0) : 0.f;
+            if constexpr (FOUR) x[i] *= power;
             if constexpr (kv_coded<S>) {
                 x[i] *= ks;
                 y[i] *= vs;
@@ -359,11 +450,10 @@ hipError_t with_image(K kernel, size_t lds, dim3 grid, hipStream_t s, A... args)
 template <int S, int T>
 hipError_t append_dp(const KvDev &c, int dp, const KvBatch &b, const KvRows &k, const KvRows &v, hipStream_t s)
 {
-    constexpr int ES = KvBytes<S>::v;
     const dim3 grid(kv_touched(c, b), c.H, b.n_seqs);
-    if (dp == 64) return with_image(kv_append_kernel<S, T, 64>, image_bytes<ES, 64>(c.P), grid, s, c, b, k, v);
-    if (dp == 128) return with_image(kv_append_kernel<S, T, 128>, image_bytes<ES, 128>(c.P), grid, s, c, b, k, v);
-    return with_image(kv_append_kernel<S, T, 256>, image_bytes<ES, 256>(c.P), grid, s, c, b, k, v);
+    if (dp == 64) return with_image(kv_append_kernel<S, T, 64>, image_bytes<S, 64>(c.P), grid, s, c, b, k, v);
+    if (dp == 128) return with_image(kv_append_kernel<S, T, 128>, image_bytes<S, 128>(c.P), grid, s, c, b, k, v);
+    return with_image(kv_append_kernel<S, T, 256>, image_bytes<S, 256>(c.P), grid, s, c, b, k, v);
 }
 
 template <int S>
@@ -377,11 +467,10 @@ hipError_t append_s(const KvDev &c, int dp, const KvBatch &b, const KvRows &k, c
 template <int S, int T>
 hipError_t read_dp(const KvDev &c, int dp, const KvBatch &b, char *k, char *v, hipStream_t s)
 {
-    constexpr int ES = KvBytes<S>::v;
     const dim3 grid(kv_touched(c, b), c.H, b.n_seqs);
-    if (dp == 64) return with_image(kv_read_kernel<S, T, 64>, image_bytes<ES, 64>(c.P), grid, s, c, b, k, v);
-    if (dp == 128) return with_image(kv_read_kernel<S, T, 128>, image_bytes<ES, 128>(c.P), grid, s, c, b, k, v);
-    return with_image(kv_read_kernel<S, T, 256>, image_bytes<ES, 256>(c.P), grid, s, c, b, k, v);
+    if (dp == 64) return with_image(kv_read_kernel<S, T, 64>, image_bytes<S, 64>(c.P), grid, s, c, b, k, v);
+    if (dp == 128) return with_image(kv_read_kernel<S, T, 128>, image_bytes<S, 128>(c.P), grid, s, c, b, k, v);
+    return with_image(kv_read_kernel<S, T, 256>, image_bytes<S, 256>(c.P), grid, s, c, b, k, v);
 }
 
 template <int S>
@@ -399,6 +488,7 @@ hipError_t launch_kv_append(const KvDev &c, int storage, int dp, const KvBatch &
     switch (storage) {
     case PK_I8: return append_s<PK_I8>(c, dp, b, k, v, dtype, s);
     case PK_F8: return append_s<PK_F8>(c, dp, b, k, v, dtype, s);
+    case PK_F4: return append_s<PK_F4>(c, dp, b, k, v, dtype, s);
     case PK_F16: return append_s<PK_F16>(c, dp, b, k, v, dtype, s);
     default: return append_s<PK_BF16>(c, dp, b, k, v, dtype, s);
     }
@@ -410,6 +500,7 @@ hipError_t launch_kv_read(const KvDev &c, int storage, int dp, const KvBatch &b,
     switch (storage) {
     case PK_I8: return read_s<PK_I8>(c, dp, b, ko, vo, dtype, s);
     case PK_F8: return read_s<PK_F8>(c, dp, b, ko, vo, dtype, s);
+    case PK_F4: return read_s<PK_F4>(c, dp, b, ko, vo, dtype, s);
     case PK_F16: return read_s<PK_F16>(c, dp, b, ko, vo, dtype, s);
     default: return read_s<PK_BF16>(c, dp, b, ko, vo, dtype, s);
     }
@@ -439,7 +530,7 @@ bool valid(const pk_kv_config *g)
 {
     return g && g->n_pages >= 1 && g->n_pages <= 0x7fffffff && g->n_heads >= 1 && g->n_heads <= kMaxHeads && g->head_dim >= 8 &&
            g->head_dim <= PK_KV_MAX_DIM && g->head_dim % 8 == 0 && g->page_tokens >= 16 && g->page_tokens <= kKvMaxPage &&
-           (g->page_tokens & (g->page_tokens - 1)) == 0 && g->storage >= PK_F16 && g->storage <= PK_F8;
+           (g->page_tokens & (g->page_tokens - 1)) == 0 && (kv_is_coded(g->storage) || g->storage == PK_F16 || g->storage == PK_BF16);
 }
 
 // Regions of the arena; base may be null (sizes only).
@@ -455,10 +546,10 @@ size_t lay_out(const pk_kv_config &g, char *base, KvDev *c)
     };
     c->k = take(ph * g.page_tokens * row);
     c->v = take(ph * g.page_tokens * row);
-    const bool coded = g.storage == PK_I8 || g.storage == PK_F8;
-    const size_t scales = coded ? ph * g.page_tokens * sizeof(float) : 0;
-    c->ks = reinterpret_cast<float *>(take(scales)); // (of a 16-bit storage: nothing lies there)
+    const size_t scales = kv_is_coded(g.storage) ? ph * g.page_tokens * sizeof(float) : 0;
+    c->ks = reinterpret_cast<float *>(take(scales));
     c->vs = reinterpret_cast<float *>(take(scales));
+    c->ke = reinterpret_cast<uint8_t *>(take(g.storage == PK_F4 ? ph * g.page_tokens * (dp / 32) : 0));
     c->bc = reinterpret_cast<int8_t *>(take(ph * 2 * dp));
     c->bs = reinterpret_cast<float *>(take(ph * sizeof(float)));
     c->n_pages = (uint32_t)g.n_pages;

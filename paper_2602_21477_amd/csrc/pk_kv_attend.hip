@@ -9,20 +9,21 @@ namespace {
 
 
 // How the second product's operands are scaled.  The largest weight is 2^top: in half precision that type has the more of its range
-// below it (2^-39 of it is the smallest), in bfloat16 it keeps the products with denormal codes where 32 bits are normal.  Both times a
+// below it (2^-39 of it is the smallest), in bfloat16 it keeps the products with denormal codes where 32 bits are normal, and small weights that
+// alone make a channel which all heavy keys' 4 bits have as zero.  Each time a
 // value's scale goes into the weight in units of the largest seen, so that no size of them overflows.
 // One rounding of a weight is of the size of the result's own: against 64 bits a result is off by 2.1e-3, with weights of 32 bits by 1.6e-3
 // (one bfloat16 token), by 2.9e-4 and 2.1e-4 (half precision over e4m3).  A second part would be the second product once more: only where
-// bfloat16 has fewer bits than the codes are worth.
+// bfloat16 has fewer bits than the codes are worth, which those of 4 bits are not.
 template <int S, int T>
 struct KvScaling {
     static constexpr bool CODED = kv_coded<S>, HALF = T == PK_F16;
-    static constexpr bool TWICE = CODED && !HALF;             // a weight is the sum of two numbers
-    static constexpr bool UNITS = CODED && (HALF || S == PK_I8);
-    static constexpr float top = HALF ? 15.f : S == PK_I8 ? 127.f : 0.f;
+    static constexpr bool TWICE = CODED && !HALF && S != PK_F4; // a weight is the sum of two numbers
+    static constexpr bool UNITS = CODED && (HALF || S != PK_F8);
+    static constexpr float top = HALF ? 15.f : S == PK_I8 ? 127.f : S == PK_F4 ? 16.f : 0.f;
     static constexpr float l_unit = !HALF && S == PK_I8 ? 0x1p-27f : 1.f; // of the sum of weights: it does not overflow
-    // sums of weights, and of products (before the unit), in the end: both as if the largest weight were 1
-    static constexpr float l_back = HALF ? 0x1p-15f : S == PK_I8 ? 0x1p-100f : 1.f;
+    // sums of weights, and of products (before the unit, of 2^-100 at least), in the end: both as if the largest weight were 1
+    static constexpr float l_back = HALF ? 0x1p-15f : S == PK_I8 ? 0x1p-100f : S == PK_F4 ? 0x1p-16f : 1.f;
     static constexpr float o_back = S != PK_I8 ? l_back : HALF ? 0x1p9f : 0x1p6f;
 };
 
@@ -56,23 +57,57 @@ __device__ __forceinline__ f32x4 mma(u32x4 a, u32x4 b, f32x4 acc)
     else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf8, a), __builtin_bit_cast(bf8, b), acc, 0, 0, 0);
 }
 
-// Sixteen bytes of a row as operands of a product: one of 8 elements, or two of 8 codes each.
-template <int S, int T, bool VALUES>
-__device__ __forceinline__ void operands(u32x4 w, u32x4 &first, u32x4 &second)
+// Sixteen bytes of a row as operands of a product: one of 8 elements, two of 8 codes each, or (keys) four of 8 codes in 4 bits.
+template <int S> constexpr int kv_operands = 16 / kv_bits<S>;
+template <int S, int T, bool VALUES, int N>
+__device__ __forceinline__ void operands(u32x4 w, float power, u32x4 (&to)[N])
 {
-    if constexpr (kv_coded<S>) {
-        uint32_t lo, hi;
-        codes_to<S, T, VALUES>(w[0], lo, hi);
-        first[0] = lo, first[1] = hi;
-        codes_to<S, T, VALUES>(w[1], lo, hi);
-        first[2] = lo, first[3] = hi;
-        codes_to<S, T, VALUES>(w[2], lo, hi);
-        second[0] = lo, second[1] = hi;
-        codes_to<S, T, VALUES>(w[3], lo, hi);
-        second[2] = lo, second[3] = hi;
+    if constexpr (S == PK_F4) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) to[i] = eight_of_4<T>(w[i], power);
+    } else if constexpr (kv_coded<S>) {
+        static_assert(N == 2, "");
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            uint32_t lo, hi;
+            codes_to<S, T, VALUES>(w[2 * i], lo, hi);
+            to[i][0] = lo, to[i][1] = hi;
+            codes_to<S, T, VALUES>(w[2 * i + 1], lo, hi);
+            to[i][2] = lo, to[i][3] = hi;
+        }
     } else {
-        first = w;
+        to[0] = w;
     }
+}
+
+// What a run of 16 tokens of channel tile d is in a lane's 16-byte loads of values: in 16 bits two loads, of which each is an operand; in 8 one; in
+// 4 bits half a load, words of 8 tokens.
+template <int S> constexpr int kv_value_loads = kv_bits<S> == 16 ? 2 : 1;
+template <int S, int DT> constexpr int kv_value_words = S == PK_F4 ? DT / 2 : DT * kv_value_loads<S>;
+template <int S, int T, int N>
+__device__ __forceinline__ void value_operands(const u32x4 (&w)[N], int d, u32x4 &first, u32x4 &second)
+{
+    if constexpr (S == PK_F4) {
+        first = eight_of_4<T>(w[d / 2][(d & 1) * 2], 1.f);
+        second = eight_of_4<T>(w[d / 2][(d & 1) * 2 + 1], 1.f);
+    } else if constexpr (kv_coded<S>) {
+        u32x4 f[2];
+        operands<S, T, true>(w[d], 1.f, f);
+        first = f[0], second = f[1];
+    } else {
+        first = w[2 * d], second = w[2 * d + 1];
+    }
+}
+// The bits of word i of such a load whose tokens, of the lane's 16, come before `held`.
+template <int S>
+__device__ __forceinline__ uint32_t held_bits(int word, int load, int held)
+{
+    constexpr int B = kv_bits<S>, EACH = 32 / B;
+    const int first = (S == PK_F4 ? (word & 1) : kv_bits<S> == 8 ? word : load * 4 + word) * EACH;
+    uint32_t keep = 0;
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) keep |= first + e < held ? ((1u << B) - 1) << (B * e) : 0u;
+    return keep;
 }
 
 __device__ __forceinline__ float over_quarters_max(float x)
@@ -183,16 +218,16 @@ __device__ __forceinline__ void kv_join_parts(const KvAttend &a, size_t first, i
 // caches and is bound by the vector units (1024 tokens, 32 blocks each of int8: 4 query heads a group, R 1 403 us, R 4 352 - 362; 2, R 1 412,
 // R 4 373; 8, R 1 423, R 2 393).
 template <int S, int T, int DP, bool SPARSE, bool ONE, int R>
-__global__ __launch_bounds__(256, DP * KvBytes<S>::v > 128 ? 1 : 2) void kv_rows_kernel(KvAttend a)
+__global__ __launch_bounds__(256, DP * kv_bits<S> / 8 > 128 ? 1 : 2) void kv_rows_kernel(KvAttend a)
 {
-    constexpr int ES = KvBytes<S>::v;
     using Sc = KvScaling<S, T>;
-    constexpr bool CODED = Sc::CODED, HALF = Sc::HALF, TWICE = Sc::TWICE;
-    constexpr int EL = 16 / ES;               // elements of a 16-byte load
-    constexpr int KC = DP / (4 * EL);         // such loads of a lane for one row of K
+    constexpr bool CODED = Sc::CODED, HALF = Sc::HALF, TWICE = Sc::TWICE, FOUR = S == PK_F4;
+    constexpr int RB = DP * kv_bits<S> / 8;   // bytes of a row
+    constexpr int KB = RB / 4 < 16 ? RB / 4 : 16, KC = RB / (4 * KB); // a lane's loads for one row of K: bytes of each, their number
+    constexpr int EL = KB * 8 / kv_bits<S>, OPS = EL / 8; // elements of such a load, operands of a product of them
     constexpr int KS = DP / 32;               // products over the channels
     constexpr int DT = DP / 16;               // tiles of 16 channels of the output
-    constexpr int VC = CODED ? 1 : 2;         // loads of a lane for 16 tokens of a channel
+    constexpr int VN = kv_value_words<S, DT>; // loads of a lane for 16 tokens of all channels
     constexpr int RT = 16 / R, NI = 4 / R;    // queries of a tile; of a lane's four groups of four keys, those that its column weighs
     __shared__ __align__(16) float join_o[4][16][DP + 4];
     __shared__ float join_m[4][16], join_l[4][16], join_q[16];
@@ -271,13 +306,26 @@ __global__ __launch_bounds__(256, DP * KvBytes<S>::v > 128 ? 1 : 2) void kv_rows
         return r;
     };
     u32x4 kw[4][KC];
+    uint32_t kpow[KC]; // (4 bits) powers of two of the lane's four keys
     auto ask_k = [&](const KvRun &r) __attribute__((always_inline)) {
         const size_t ph = (size_t)(r.page < c.n_pages ? r.page : 0) * c.H + h;
-        const char *kr = c.k + (ph * P + (r.base >= 0 ? r.base & (P - 1) : 0)) * DP * ES + (uint32_t)((ONE ? col >> 2 : 0) * 16 * DP * ES + g * 64 + (col & 3) * 16);
+        const int off = r.base >= 0 ? r.base & (P - 1) : 0, run = ONE ? col >> 2 : 0;
+        const char *kr = c.k + (ph * P + off) * RB + (uint32_t)(run * 16 * RB + (KB == 16 ? g * 64 : (g >> 1) * 64 + (g & 1) * 8) + (col & 3) * 16);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int k = 0; k < KC; ++k) kw[i][k] = *reinterpret_cast<const u32x4 *>(kr + i * DP * ES * 4 + k * 256);
+            for (int k = 0; k < KC; ++k) {
+                if constexpr (KB == 16) kw[i][k] = *reinterpret_cast<const u32x4 *>(kr + i * RB * 4 + k * 256);
+                else {
+                    const u32x2 w = *reinterpret_cast<const u32x2 *>(kr + i * RB * 4);
+                    kw[i][k] = u32x4{w[0], w[1], 0u, 0u};
+                }
+            }
+        if constexpr (FOUR) {
+            const uint8_t *e = c.ke + (ph * P + off) * (DP / 32) + (uint32_t)(run * (DP / 2) + (KB == 16 ? g : g >> 1) * 16 + (col & 3) * 4);
+#pragma unroll
+            for (int k = 0; k < KC; ++k) kpow[k] = *reinterpret_cast<const uint32_t *>(e + k * 64);
+        }
     };
     const int tw = t0 + wave;
     int kblock = 0, vblock = 0; // (sparse) of the round after the next
@@ -302,7 +350,7 @@ __global__ __launch_bounds__(256, DP * KvBytes<S>::v > 128 ? 1 : 2) void kv_rows
         float x[KS][8], most = 0.f, sum = 0.f;
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
-            const int at = CODED ? (k >> 1) * 64 + g * 16 + (k & 1) * 8 : k * 32 + g * 8;
+            const int at = (k / OPS * 4 + g) * EL + k % OPS * 8;
 #pragma unroll
             for (int i = 0; i < 8; ++i) x[k][i] = 0.f;
             if (valid && at < c.D) load_eight<T>(x[k], qrow, at);
@@ -334,7 +382,7 @@ __global__ __launch_bounds__(256, DP * KvBytes<S>::v > 128 ? 1 : 2) void kv_rows
         const bool there = vr.page < c.n_pages;
         const int vb = ONE ? (vr.base >= 0 ? vr.base + g * 16 : -1) : vr.base; // the lane's first token
         f32x4 ksc[NI], vsc[NI];
-        u32x4 vw[DT][VC];
+        u32x4 vw[VN];
         {
             const size_t vph = (size_t)(there ? vr.page : 0) * c.H + h;
             const int voff = vr.base >= 0 ? vr.base & (P - 1) : 0, vrun = ONE ? g * 16 : 0;
@@ -346,11 +394,9 @@ __global__ __launch_bounds__(256, DP * KvBytes<S>::v > 128 ? 1 : 2) void kv_rows
                     vsc[i] = *reinterpret_cast<const f32x4 *>(vs + 4 * i);
                 }
             }
-            const char *v = c.v + (vph * P + voff) * DP * ES + (uint32_t)(vrun * DP * ES + col * 16);
+            const char *v = c.v + (vph * P + voff) * RB + (uint32_t)(vrun * RB + col * 16);
 #pragma unroll
-            for (int d = 0; d < DT; ++d)
-#pragma unroll
-                for (int k = 0; k < VC; ++k) vw[d][k] = *reinterpret_cast<const u32x4 *>(v + d * 256 + k * DP * 16);
+            for (int d = 0; d < VN; ++d) vw[d] = *reinterpret_cast<const u32x4 *>(v + (kv_bits<S> == 16 ? d / 2 * 256 + d % 2 * DP * 16 : d * 256));
         }
         __builtin_amdgcn_sched_barrier(0);
 
@@ -360,14 +406,10 @@ __global__ __launch_bounds__(256, DP * KvBytes<S>::v > 128 ? 1 : 2) void kv_rows
             xa[i] = f32x4{x0, x0, x0, x0};
 #pragma unroll
             for (int k = 0; k < KC; ++k) {
-                u32x4 f0, f1;
-                operands<S, T, false>(kw[i][k], f0, f1);
-                if constexpr (CODED) {
-                    xa[i] = mma<HALF>(f0, qf[2 * k], xa[i]);
-                    xa[i] = mma<HALF>(f1, qf[2 * k + 1], xa[i]);
-                } else {
-                    xa[i] = mma<HALF>(f0, qf[k], xa[i]);
-                }
+                u32x4 f[OPS];
+                operands<S, T, false>(kw[i][k], FOUR ? power_of(kpow[k] >> 8 * i & 0xffu) : 1.f, f);
+#pragma unroll
+                for (int e = 0; e < OPS; ++e) xa[i] = mma<HALF>(f[e], qf[OPS * k + e], xa[i]);
             }
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -406,17 +448,9 @@ __global__ __launch_bounds__(256, DP * KvBytes<S>::v > 128 ? 1 : 2) void kv_rows
                     if constexpr (CODED) vsc[i][j] = key < held ? vsc[i][j] : 0.f;
                 }
 #pragma unroll
-            for (int d = 0; d < DT; ++d)
+            for (int d = 0; d < VN; ++d)
 #pragma unroll
-                for (int k = 0; k < VC; ++k)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int w = (k * 4 + i) * (4 / ES); // first token of the word
-                        uint32_t keep = 0;
-#pragma unroll
-                        for (int e = 0; e < 4 / ES; ++e) keep |= w + e < held ? (ES == 1 ? 0xffu : 0xffffu) << (8 * ES * e) : 0u;
-                        vw[d][k][i] &= keep;
-                    }
+                for (int i = 0; i < 4; ++i) vw[d][i] &= held_bits<S>(i, kv_bits<S> == 16 ? d & 1 : 0, held);
         }
         float most = -INFINITY;
 #pragma unroll
@@ -485,8 +519,7 @@ __global__ __launch_bounds__(256, DP * KvBytes<S>::v > 128 ? 1 : 2) void kv_rows
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
             u32x4 f0, f1;
-            operands<S, T, true>(vw[d][0], f0, f1);
-            if constexpr (!CODED) f1 = vw[d][VC - 1];
+            value_operands<S, T>(vw, d, f0, f1);
             o[d] = mma<HALF>(f0, pf[0], o[d]);
             o[d] = mma<HALF>(f1, pf[1], o[d]);
             if constexpr (TWICE) {
@@ -657,16 +690,16 @@ __device__ __forceinline__ float over_wave_max(float v)
 // Tiles on their way into LDS: their pages, then pieces of K(j) and V(j - 1) in registers, then LDS.
 template <int S, int T, int DP, int NW, bool ONE>
 struct KvTiles {
-    static constexpr int ES = KvBytes<S>::v, NT = NW * 64, CH = DP / 8;
-    static constexpr bool CODED = kv_coded<S>, UNITS = KvScaling<S, T>::UNITS;
-    static constexpr int PIECES = kKvTile * DP * ES / 16; // 16-byte pieces of a tile of K, and of one of V
+    static constexpr int RB = DP * kv_bits<S> / 8, NT = NW * 64, CH = DP / 8; // bytes of a row
+    static constexpr bool CODED = kv_coded<S>, FOUR = S == PK_F4, UNITS = KvScaling<S, T>::UNITS;
+    static constexpr int PIECES = kKvTile * RB / 16; // 16-byte pieces of a tile of K, and of one of V
     static constexpr int KP = (PIECES + NT - 1) / NT;     // of a thread
-    static constexpr int KR = DP * ES / 16;               // pieces of a row of K
-    // piece p of a tile in memory: of K piece k_piece of token k_tok; of V channel v_row, tokens from v_tok on
+    static constexpr int KR = RB / 16;                    // pieces of a row of K
+    // piece p of a tile in memory: of K piece k_piece of token k_tok; of V channel v_row (4 bits: and the one 16 beyond), tokens from v_tok on
     static __device__ __forceinline__ int k_tok(int p) { return p / (4 * KR) * 4 + (p & 3); }
     static __device__ __forceinline__ int k_piece(int p) { return p / 4 % KR; }
-    static __device__ __forceinline__ int v_row(int p) { return p % DP; }
-    static __device__ __forceinline__ int v_tok(int p) { return p / DP * (16 / ES); }
+    static __device__ __forceinline__ int v_row(int p) { return FOUR ? p % RB / 16 * 32 + p % 16 : p % DP; }
+    static __device__ __forceinline__ int v_tok(int p) { return FOUR ? p / RB * 16 : p / DP * (128 / kv_bits<S>); }
     static constexpr int PG = ONE ? 1 : KP;
     static_assert(PIECES % NT == 0 || PIECES < NT, "");
     struct Lds {
@@ -678,11 +711,13 @@ struct KvTiles {
 
     const char *k, *v;
     const float *ks, *vs;
+    const uint8_t *ke;
     const int32_t *table;
     uint32_t n_pages;
     int H, h, P, logP, len;
     uint32_t kpage[PG], vpage[PG], spage; // of K(j), of V(j - 1); of the lane's token of K(j)
     u32x4 kw[KP], vw[KP];
+    uint32_t kpow[FOUR ? KP : 1]; // powers of two of the pieces of K
     float ksw, vsw;
     float unit, fade; // (of the wave that brings them) largest scale of a value so far, and the one before it in units of it
     uint32_t v_in;    // which of the thread's pieces of V(j - 1) lie in pages that the table has
@@ -691,7 +726,7 @@ struct KvTiles {
 
     __device__ __forceinline__ void begin(const KvDev &c, const int32_t *t, int head, int tokens)
     {
-        k = c.k, v = c.v, ks = c.ks, vs = c.vs, table = t;
+        k = c.k, v = c.v, ks = c.ks, vs = c.vs, ke = c.ke, table = t;
         n_pages = c.n_pages, H = c.H, h = head, P = c.P, logP = c.logP, len = tokens;
         spage = 0, ksw = 0.f, vsw = 0.f, in_next = 0, v_in = 0, v_there = true, unit = 1e-30f, fade = 1.f;
     }
@@ -724,7 +759,7 @@ struct KvTiles {
             // (taken here, not where they were asked for: that would be a wait for all that is on its way)
             asm volatile("" : "+v"(kpage[0]), "+v"(vpage[0]));
             const uint32_t kp = (uint32_t)same((int)kpage[0]), vp = (uint32_t)same((int)vpage[0]);
-            const char *kr = k + (place(kp) * P + (kb & (P - 1))) * DP * ES, *vr = v + (place(vp) * P + (vb & (P - 1))) * DP * ES;
+            const char *kr = k + (place(kp) * P + (kb & (P - 1))) * RB, *vr = v + (place(vp) * P + (vb & (P - 1))) * RB;
             in_next = kp < n_pages ? 15u : 0u;
             if constexpr (CODED) { // (first: loads come back in their order, and the scales are wanted before the rest)
                 const size_t at = place(kp) * P + (kb & (P - 1));
@@ -740,6 +775,7 @@ struct KvTiles {
                     const int p = tid + i * NT;
                     kw[i] = *reinterpret_cast<const u32x4 *>(kr + (uint32_t)(p * 16));
                     vw[i] = *reinterpret_cast<const u32x4 *>(vr + (uint32_t)(p * 16));
+                    if constexpr (FOUR) kpow[i] = ke[(place(kp) * P + (kb & (P - 1))) * (DP / 32) + (uint32_t)e_place<DP>(k_tok(p), k_piece(p))];
                 }
             }
             v_there = vp < n_pages;
@@ -754,9 +790,11 @@ struct KvTiles {
                 const int p = tid + i * NT;
                 if (mine) {
                     // (a run of 16 tokens lies in one page)
-                    constexpr int RUN = 16 * DP * ES / 16; // pieces of a run
-                    kw[i] = *reinterpret_cast<const u32x4 *>(k + (place(kpage[i]) * P + ((kb + p / RUN * 16) & (P - 1))) * DP * ES + (p % RUN) * 16);
-                    vw[i] = *reinterpret_cast<const u32x4 *>(v + (place(vpage[i]) * P + ((vb + p / RUN * 16) & (P - 1))) * DP * ES + (p % RUN) * 16);
+                    constexpr int RUN = RB; // pieces of a run
+                    const size_t krun = place(kpage[i]) * P + ((kb + p / RUN * 16) & (P - 1)), vrun = place(vpage[i]) * P + ((vb + p / RUN * 16) & (P - 1));
+                    kw[i] = *reinterpret_cast<const u32x4 *>(k + krun * RB + (p % RUN) * 16);
+                    vw[i] = *reinterpret_cast<const u32x4 *>(v + vrun * RB + (p % RUN) * 16);
+                    if constexpr (FOUR) kpow[i] = ke[krun * (DP / 32) + (uint32_t)e_place<DP>(k_tok(p) & 15, k_piece(p))];
                 }
                 v_in |= (vpage[i] < n_pages ? 1u : 0u) << i;
             }
@@ -794,12 +832,7 @@ struct KvTiles {
         for (int i = 0; i < KP; ++i) {
             const int p = threadIdx.x + i * NT, held = vb >= 0 && (v_in >> i & 1) ? len - (vb + v_tok(p)) : 0;
 #pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                uint32_t keep = 0;
-#pragma unroll
-                for (int e = 0; e < 4 / ES; ++e) keep |= w * (4 / ES) + e < held ? (ES == 1 ? 0xffu : 0xffffu) << (8 * ES * e) : 0u;
-                vw[i][w] &= keep;
-            }
+            for (int w = 0; w < 4; ++w) vw[i][w] &= held_bits<S>(w, 0, held);
         }
     }
 
@@ -811,14 +844,22 @@ struct KvTiles {
             for (int i = 0; i < KP; ++i) {
                 const int p = tid + i * NT;
                 const int row = k_tok(p), piece = k_piece(p), vrow = v_row(p), vpiece = v_tok(p) / 8;
-                if constexpr (CODED) {
-                    u32x4 f0, f1;
-                    operands<S, T, false>(kw[i], f0, f1);
-                    lds.k[kb][lds_piece<CH>(row, piece * 2)] = f0;
-                    lds.k[kb][lds_piece<CH>(row, piece * 2 + 1)] = f1;
-                    operands<S, T, true>(vw[i], f0, f1);
-                    lds.v[vb][lds_piece<8>(vrow, vpiece)] = f0;
-                    lds.v[vb][lds_piece<8>(vrow, vpiece + 1)] = f1;
+                if constexpr (FOUR) {
+                    u32x4 f[4];
+                    operands<S, T, false>(kw[i], power_of(kpow[i]), f);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) lds.k[kb][lds_piece<CH>(row, piece * 4 + e)] = f[e];
+                    operands<S, T, true>(vw[i], 1.f, f);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) lds.v[vb][lds_piece<8>(vrow + (e >> 1) * 16, vpiece + (e & 1))] = f[e];
+                } else if constexpr (CODED) {
+                    u32x4 f[2];
+                    operands<S, T, false>(kw[i], 1.f, f);
+                    lds.k[kb][lds_piece<CH>(row, piece * 2)] = f[0];
+                    lds.k[kb][lds_piece<CH>(row, piece * 2 + 1)] = f[1];
+                    operands<S, T, true>(vw[i], 1.f, f);
+                    lds.v[vb][lds_piece<8>(vrow, vpiece)] = f[0];
+                    lds.v[vb][lds_piece<8>(vrow, vpiece + 1)] = f[1];
                 } else {
                     lds.k[kb][lds_piece<CH>(row, piece)] = kw[i];
                     lds.v[vb][lds_piece<8>(vrow, vpiece)] = vw[i];
@@ -1222,6 +1263,7 @@ hipError_t launch_kv_attend(const KvAttend &a, int storage, int dp, int dtype, h
     switch (storage) {
     case PK_I8: return dtype == PK_F16 ? run_dp<PK_I8, PK_F16>(a, dp, s) : run_dp<PK_I8, PK_BF16>(a, dp, s);
     case PK_F8: return dtype == PK_F16 ? run_dp<PK_F8, PK_F16>(a, dp, s) : run_dp<PK_F8, PK_BF16>(a, dp, s);
+    case PK_F4: return dtype == PK_F16 ? run_dp<PK_F4, PK_F16>(a, dp, s) : run_dp<PK_F4, PK_BF16>(a, dp, s);
     case PK_F16: return run_dp<PK_F16, PK_F16>(a, dp, s);
     default: return run_dp<PK_BF16, PK_BF16>(a, dp, s);
     }

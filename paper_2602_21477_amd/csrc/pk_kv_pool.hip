@@ -392,10 +392,10 @@ size_t lay_out(int64_t n_pages, char *base, KvPool *p)
 KvMove move_between(const pk_kv &to, const pk_kv &from)
 {
     const size_t H = from.cfg.n_heads, P = from.cfg.page_tokens, dp = from.dp, row = kv_row_bytes(from.cfg.storage, from.dp);
-    const size_t scales = row < 2 * dp ? H * P * sizeof(float) : 0;
-    const size_t bytes[kRegions] = {H * P * row, H * P * row, scales, scales, 0, H * 2 * dp, H * sizeof(float)};
+    const size_t scales = kv_is_coded(from.cfg.storage) ? H * P * sizeof(float) : 0, powers = from.cfg.storage == PK_F4 ? H * P * (dp / 32) : 0;
+    const size_t bytes[kRegions] = {H * P * row, H * P * row, scales, scales, powers, H * 2 * dp, H * sizeof(float)};
     auto regions = [](const KvDev &c, char *(&r)[kRegions]) {
-        char *all[kRegions] = {c.k, c.v, reinterpret_cast<char *>(c.ks), reinterpret_cast<char *>(c.vs), nullptr, reinterpret_cast<char *>(c.bc), reinterpret_cast<char *>(c.bs)};
+        char *all[kRegions] = {c.k, c.v, reinterpret_cast<char *>(c.ks), reinterpret_cast<char *>(c.vs), reinterpret_cast<char *>(c.ke), reinterpret_cast<char *>(c.bc), reinterpret_cast<char *>(c.bs)};
         std::copy(all, all + kRegions, r);
     };
     KvMove m{};
