@@ -523,6 +523,22 @@ int pk_kv_attend(pk_kv *kv, const pk_kv_batch *batch, const pk_rows *q, int32_t 
                  float *lse, void *stream);
 
 /*
+ * As pk_kv_attend, with scores and masks of other kinds: the query of position p sees the key of position j if
+ *   j < prefix, or start <= j <= p (window > 0: and j > p - window),  j in the sequence,
+ * and its score is
+ *   cap tanh(scale q.k / cap) - slope |p - j|
+ * A prefix is seen by queries before its end too.  start: of the query's token, the first position of its document; negative ones are 0.
+ */
+typedef struct {
+    float cap;             /* > 0, finite; 0: scores are not capped                      */
+    const float *slopes;   /* DEVICE [n_q_heads], finite, or NULL                        */
+    const int32_t *starts; /* DEVICE [n_tokens] or NULL                                  */
+    const int32_t *prefix; /* DEVICE [n_seqs] tokens of a sequence or NULL               */
+} pk_kv_scores;
+int pk_kv_attend_scored(pk_kv *kv, const pk_kv_batch *batch, const pk_rows *q, int32_t n_q_heads, float scale, int32_t window,
+                        const pk_kv_scores *scores, void *out, float *lse, void *stream);
+
+/*
  * The blocks (pages) that each new token attends to, one choice for each key/value head: the first `sink` blocks, the last
  * `local` ones up to its own, and of those between the ones with the best scores, n_blocks in all (all that there are, if fewer).
  *   q in int8 by head (code and scale as PK_I8 storage);  U = sum_c max(q_c hi_c, q_c lo_c) over the codes, a whole number

@@ -26,7 +26,7 @@ PK_NOALLOC_WORKSPACE_BYTES = 64 << 20
 EXPORTS = ["pk_workspace_reserve", "pk_index_set_emit_cap", "pk_index_set_tile_cap", "pk_index_set_values_cap", "pk_search_noalloc", "pk_search_noalloc_bytes", "pk_search_levels", "pk_search_union", "pk_insert_multi", "pk_delete", "pk_index_split", "pk_index_centroids", "pk_list_ids", "pk_arena_bytes", "pk_index_build", "pk_index_add_arena", "pk_index_compact", "pk_kmeans", "pk_insert", "pk_insert_assigned", "pk_search",
            "pk_search_multi", "pk_coarse", "pk_scan_probes", "pk_index_stats", "pk_list_lengths", "pk_profile_begin",
            "pk_profile_end", "pk_index_free", "pk_kv_arena_bytes", "pk_kv_create", "pk_kv_free", "pk_kv_append", "pk_kv_read",
-           "pk_kv_bounds", "pk_kv_attend", "pk_kv_select", "pk_kv_attend_blocks", "pk_kv_pool_bytes", "pk_kv_pool_create", "pk_kv_pool_free", "pk_kv_pool_clear",
+           "pk_kv_bounds", "pk_kv_attend", "pk_kv_attend_scored", "pk_kv_select", "pk_kv_attend_blocks", "pk_kv_pool_bytes", "pk_kv_pool_create", "pk_kv_pool_free", "pk_kv_pool_clear",
            "pk_kv_pool_adopt", "pk_kv_pool_grant", "pk_kv_pool_fork", "pk_kv_pool_release", "pk_kv_pool_compact", "pk_kv_pool_counts", "pk_kv_copy", "pk_strerror"]
 
 
@@ -60,6 +60,10 @@ class pk_kv_batch(C.Structure):
 
 class pk_rows(C.Structure):
     _fields_ = [("data", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64), ("dtype", C.c_int32)]
+
+
+class pk_kv_scores(C.Structure):
+    _fields_ = [("cap", C.c_float), ("slopes", C.c_void_p), ("starts", C.c_void_p), ("prefix", C.c_void_p)]
 
 
 class pk_kv_tables(C.Structure):
@@ -122,6 +126,7 @@ def lib():
         L.pk_kv_read.argtypes = [vp, C.POINTER(pk_kv_batch), vp, vp, i32, vp]
         L.pk_kv_bounds.argtypes = [vp, vp, i64, vp, vp, vp]
         L.pk_kv_attend.argtypes = [vp, C.POINTER(pk_kv_batch), C.POINTER(pk_rows), i32, C.c_float, i32, vp, vp, vp]
+        L.pk_kv_attend_scored.argtypes = [vp, C.POINTER(pk_kv_batch), C.POINTER(pk_rows), i32, C.c_float, i32, C.POINTER(pk_kv_scores), vp, vp, vp]
         L.pk_kv_select.argtypes = [vp, C.POINTER(pk_kv_batch), C.POINTER(pk_rows), i32, i32, i32, i32, vp, vp]
         L.pk_kv_attend_blocks.argtypes = [vp, C.POINTER(pk_kv_batch), C.POINTER(pk_rows), i32, C.c_float, vp, i32, vp, vp, vp]
         tables = C.POINTER(pk_kv_tables)
@@ -524,6 +529,12 @@ def pk_kv_attend(handle: int, batch: pk_kv_batch, q, scale: float, window: int, 
                               _stream_of(q.get_device())), "pk_kv_attend")
 
 
+def pk_kv_attend_scored(handle: int, batch: pk_kv_batch, q, scale: float, window: int, cap: float, slopes, starts, prefix, out, lse=None):
+    scores = pk_kv_scores(cap, _dev(slopes, torch.float32, "slopes"), _dev(starts, torch.int32, "starts"), _dev(prefix, torch.int32, "prefix"))
+    _check(lib().pk_kv_attend_scored(handle, batch, _rows(q, "q"), q.shape[1], scale, window, scores, _dev(out, q.dtype, "out"), _dev(lse, torch.float32, "lse"),
+                                     _stream_of(q.get_device())), "pk_kv_attend_scored")
+
+
 def pk_kv_select(handle: int, batch: pk_kv_batch, q, n_blocks: int, sink: int, local: int, out_blocks):
     _check(lib().pk_kv_select(handle, batch, _rows(q, "q"), q.shape[1], n_blocks, sink, local, _dev(out_blocks, torch.int32, "out_blocks"), _stream_of(q.get_device())),
            "pk_kv_select")
@@ -662,11 +673,18 @@ class KVCache:
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
         return out, torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if want_lse else None
 
-    def attend(self, q, batch, scale, window=0, want_lse=False):
-        """Attention of the new tokens over their sequences: out, or (out, lse)."""
+    def attend(self, q, batch, scale, window=0, want_lse=False, cap=0.0, slopes=None, starts=None, prefix=None):
+        """Attention of the new tokens over their sequences: out, or (out, lse).  Scores are capped (cap tanh(score / cap)) where cap is not 0, and
+        lessened by slopes [query head] times the distance; starts [token]: the first position that a token sees; prefix [sequence]: tokens that all see."""
         self._shape(q, batch, 0, "q")
         out, lse = self._outputs(q, want_lse)
-        pk_kv_attend(self.handle, batch.c, q, scale, window, out, lse)
+        if cap == 0.0 and slopes is None and starts is None and prefix is None:
+            pk_kv_attend(self.handle, batch.c, q, scale, window, out, lse)
+        else:
+            for what, t, n in (("slopes", slopes, q.shape[1]), ("starts", starts, batch.n_tokens), ("prefix", prefix, batch.lens.shape[0])):
+                if t is not None and (t.shape != (n,) or t.get_device() != self.device):
+                    raise ValueError(f"{what}: need [{n}] on {self.arena.device}, got {list(t.shape)} on {t.device}")
+            pk_kv_attend_scored(self.handle, batch.c, q, scale, window, cap, slopes, starts, prefix, out, lse)
         return (out, lse) if want_lse else out
 
     def select(self, q, batch, n_blocks, sink=1, local=2):

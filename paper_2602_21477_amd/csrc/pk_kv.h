@@ -239,6 +239,11 @@ struct KvAttend {
     int32_t window;       // 0: none
     const int32_t *blocks; // sparse: [n_tokens][H][n_blocks], else null
     int32_t n_blocks;
+    int32_t scored;       // the next four are looked at
+    float cap;            // 0: none
+    const float *slopes;  // [H * G] or null
+    const int32_t *starts; // [n_tokens] or null
+    const int32_t *prefix; // [n_seqs] or null
     char *out;            // [n_tokens][H * G][D]
     float *lse;           // [n_tokens][H * G] or null
     float *part, *part_ml, *part_q; // room for partial results: part_floats of O, two floats for each row of them (maximum and sum), one for

@@ -583,7 +583,7 @@ int take_queries(const pk_kv *kv, const pk_rows *q, int32_t n_q_heads, KvRows *o
 }
 
 int attend(pk_kv *kv, const pk_kv_batch *batch, const pk_rows *q, int32_t n_q_heads, float scale, int32_t window, const int32_t *blocks,
-           int32_t n_blocks, void *out, float *lse, hipStream_t s)
+           int32_t n_blocks, const pk_kv_scores *scores, void *out, float *lse, hipStream_t s)
 {
     if (!kv_live(kv)) return PK_ERR_BAD_HANDLE;
     KvAttend a{};
@@ -591,6 +591,7 @@ int attend(pk_kv *kv, const pk_kv_batch *batch, const pk_rows *q, int32_t n_q_he
     int rc = kv_take_batch(kv, batch, &a.b, &none);
     if (rc != PK_OK) return rc;
     if (window < 0 || !std::isfinite(scale)) return PK_ERR_INVALID_ARG;
+    if (scores && !(scores->cap >= 0.f && std::isfinite(scores->cap))) return PK_ERR_INVALID_ARG;
     if (none) return PK_OK;
     rc = take_queries(kv, q, n_q_heads, &a.q, &a.G);
     if (rc != PK_OK) return rc;
@@ -600,6 +601,13 @@ int attend(pk_kv *kv, const pk_kv_batch *batch, const pk_rows *q, int32_t n_q_he
     a.window = (int32_t)std::min<int64_t>(window, kKvMaxTokens); // (a position before the first one less the window fits 32 bits too)
     a.blocks = blocks;
     a.n_blocks = n_blocks;
+    if (scores && (scores->cap > 0.f || scores->slopes || scores->starts || scores->prefix)) {
+        a.scored = 1;
+        a.cap = scores->cap;
+        a.slopes = scores->slopes;
+        a.starts = scores->starts;
+        a.prefix = scores->prefix;
+    }
     a.out = static_cast<char *>(out);
     a.lse = lse;
     a.num_cu = kv->num_cu;
@@ -711,7 +719,15 @@ int pk_kv_bounds(pk_kv *kv, const int32_t *pages, int64_t n, float *hi, float *l
 int pk_kv_attend(pk_kv *kv, const pk_kv_batch *batch, const pk_rows *q, int32_t n_q_heads, float scale, int32_t window, void *out, float *lse,
                  void *stream)
 {
-    return attend(kv, batch, q, n_q_heads, scale, window, nullptr, 0, out, lse, static_cast<hipStream_t>(stream));
+    return attend(kv, batch, q, n_q_heads, scale, window, nullptr, 0, nullptr, out, lse, static_cast<hipStream_t>(stream));
+}
+
+int pk_kv_attend_scored(pk_kv *kv, const pk_kv_batch *batch, const pk_rows *q, int32_t n_q_heads, float scale, int32_t window,
+                        const pk_kv_scores *scores, void *out, float *lse, void *stream)
+{
+    if (!kv_live(kv)) return PK_ERR_BAD_HANDLE;
+    if (!scores) return PK_ERR_INVALID_ARG;
+    return attend(kv, batch, q, n_q_heads, scale, window, nullptr, 0, scores, out, lse, static_cast<hipStream_t>(stream));
 }
 
 int pk_kv_attend_blocks(pk_kv *kv, const pk_kv_batch *batch, const pk_rows *q, int32_t n_q_heads, float scale, const int32_t *blocks,
@@ -721,7 +737,7 @@ int pk_kv_attend_blocks(pk_kv *kv, const pk_kv_batch *batch, const pk_rows *q, i
     if (n_blocks < 1 || n_blocks > kKvMaxSelect) return PK_ERR_INVALID_ARG;
     if (!blocks && batch && batch->n_tokens > 0) return PK_ERR_INVALID_ARG;
     static const int32_t nothing = 0;
-    return attend(kv, batch, q, n_q_heads, scale, 0, blocks ? blocks : &nothing, n_blocks, out, lse, static_cast<hipStream_t>(stream));
+    return attend(kv, batch, q, n_q_heads, scale, 0, blocks ? blocks : &nothing, n_blocks, nullptr, out, lse, static_cast<hipStream_t>(stream));
 }
 
 int pk_kv_select(pk_kv *kv, const pk_kv_batch *batch, const pk_rows *q, int32_t n_q_heads, int32_t n_blocks, int32_t sink, int32_t local,

@@ -1,0 +1,6 @@
+// Attention over a cache held in int8.
+#include "pk_kv_attend_dev.h"
+
+namespace pk {
+hipError_t launch_kv_attend_i8(const KvAttend &a, int dp, int dtype, hipStream_t s) { return run_storage<PK_I8>(a, dp, dtype, s); }
+} // namespace pk
