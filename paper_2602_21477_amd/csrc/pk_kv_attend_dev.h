@@ -142,46 +142,67 @@ struct KvRun {
 };
 
 // ------------------------------------------------------------------ scores that are capped or biased, masks of documents and a prefix
-// y = cap tanh(x / cap) - slope |distance|, in powers of two (the logarithm's factor is part of cap and slope).
+// y = cap tanh(x / cap) - slope |distance|.  Capped scores are powers of two (the logarithm's factor is part of cap and slope), and what they are scaled by later is
+// 1; others stay products, which are scaled later, and the bias is made one of them: a slope then costs an instruction a score, a mask none.
 struct KvScoring {
-    float z, cap;   // capped: products times z are x / cap; cap 0: z makes powers of two of them
+    float z, twice, cap; // products times z are x / cap, times twice 2 x / cap as a power of two
     float slope;
     bool capped, biased;
-    __device__ __forceinline__ void begin(const KvAttend &a, int query_head, float qscale)
+    // qscale: what products are scaled by, then what y is
+    __device__ __forceinline__ void begin(const KvAttend &a, int query_head, float &qscale)
     {
         capped = a.cap > 0.f, biased = a.slopes != nullptr;
         cap = a.cap * kLog2e;
-        z = capped ? qscale / cap : qscale;
+        z = qscale / cap;
+        twice = z * (2.f * kLog2e);
         slope = biased ? a.slopes[query_head] * kLog2e : 0.f;
+        if (capped) qscale = 1.f;
+        else slope /= qscale;
     }
-    // N products of a lane, in place, by all lanes of a wave together.  Where no |x / cap| of the wave's is beyond 1/2, the rule in practice, tanh is z times
-    // a polynomial in z^2 (fitted to tanh(z) / z, off by 2^-26 of it); else 1 - 2 / (1 + e^2z), whose error, 2^-23 of the cap, is as small beside
-    // the scores that are there then.  7 full-rate instructions a score, or 3 and two of a quarter of the rate.
+    // z times a polynomial in z^2 that was fitted to tanh(z) / z up to 1/2 (off by 2^-26 of it), times the cap.
+    __device__ __forceinline__ float near(float x) const
+    {
+        const float t = x * x;
+        float r = __builtin_fmaf(t, 0.017135003577794676f, -0.05298607376020325f);
+        r = __builtin_fmaf(r, t, 0.1332477929361659f);
+        r = __builtin_fmaf(r, t, -0.33333069392817194f);
+        r = __builtin_fmaf(r, t, 0.9999999868717396f);
+        return x * r * cap;
+    }
+    __device__ __forceinline__ float by_power(float power) const
+    {
+        const float e = __builtin_amdgcn_exp2f(power);
+        return __builtin_fmaf(-2.f * cap, __builtin_amdgcn_rcpf(1.f + e), cap);
+    }
+    // N products of a lane, in place, by all lanes of a wave together.  1 - 2 / (1 + e^2z) is off by 2^-23 of the cap: as little as a score of a few units is
+    // itself by for caps up to kPlainCap.  Beyond, that is for scores beyond half the cap, and below them the polynomial: each score
+    // by itself, so that it does not depend on what others there are.  A wave that has none beyond does without the power.
+    static constexpr float kPlainCap = 64.f;
     template <int N>
     __device__ __forceinline__ void cap_all(float (&x)[N]) const
     {
+        constexpr int EACH = 8; // scores that are on their way together (all of them at once did not fit the registers)
+        if (cap <= kPlainCap * kLog2e) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                x[i] = by_power(x[i] * twice);
+                if (i % EACH == EACH - 1) __builtin_amdgcn_sched_barrier(0);
+            }
+            return;
+        }
         float most = 0.f;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             x[i] *= z;
             most = fmaxf(most, fabsf(x[i]));
         }
-        if (__any(most > 0.5f)) {
+        const bool all_near = !__any(most > 0.5f);
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const float e = __builtin_amdgcn_exp2f(x[i] * (2.f * kLog2e));
-                x[i] = __builtin_fmaf(-2.f * cap, __builtin_amdgcn_rcpf(1.f + e), cap);
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const float t = x[i] * x[i];
-                float r = __builtin_fmaf(t, 0.017135003577794676f * cap, -0.05298607376020325f * cap);
-                r = __builtin_fmaf(r, t, 0.1332477929361659f * cap);
-                r = __builtin_fmaf(r, t, -0.33333069392817194f * cap);
-                r = __builtin_fmaf(r, t, 0.9999999868717396f * cap);
-                x[i] *= r;
-            }
+        for (int i = 0; i < N; ++i) {
+            const float y = near(x[i]);
+            if (all_near) x[i] = y;
+            else x[i] = fabsf(x[i]) > 0.5f ? by_power(x[i] * (2.f * kLog2e)) : y;
+            if (i % EACH == EACH - 1) __builtin_amdgcn_sched_barrier(0);
         }
     }
 };
@@ -448,10 +469,7 @@ __global__ __launch_bounds__(256, DP * kv_bits<S> / 8 > 128 ? 1 : 2) void kv_row
         qscale *= qs.back;
     }
     KvScoring scoring;
-    if constexpr (SCORED) {
-        scoring.begin(a, h * G + member, qscale);
-        qscale = 1.f; // (scores are powers of two from the start)
-    }
+    if constexpr (SCORED) scoring.begin(a, h * G + member, qscale);
 
     f32x4 o[DT];
 #pragma unroll
@@ -520,10 +538,6 @@ __global__ __launch_bounds__(256, DP * kv_bits<S> / 8 > 128 ? 1 : 2) void kv_row
 #pragma unroll
             for (int i = 0; i < 16; ++i) y[i] = x[i >> 2][i & 3];
             if (scoring.capped) scoring.cap_all(y);
-            else {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) y[i] *= scoring.z;
-            }
             if (scoring.biased) {
                 const float far = (float)(pos - vb);
 #pragma unroll
@@ -531,6 +545,8 @@ __global__ __launch_bounds__(256, DP * kv_bits<S> / 8 > 128 ? 1 : 2) void kv_row
             }
 #pragma unroll
             for (int i = 0; i < 16; ++i) x[i >> 2][i & 3] = y[i];
+#pragma unroll
+            for (int i = 0; i < NI; ++i) asm volatile("" : "+v"(x[i])); // (what follows is the same code for all kinds: without it 4 - 9 registers go to scratch)
         }
         // keys that a query does not see; the values of tokens that no query sees are taken as zeros, whatever lies there
         const int seen = (there ? min(pos, sq.len - 1) : -1) - vb; // of the lane's 16 keys: 0 .. seen
@@ -1008,7 +1024,7 @@ __global__ __launch_bounds__(NW * 64) void kv_tile_kernel(KvAttend a)
     using Sc = KvScaling<S, T>;
     constexpr bool CODED = Sc::CODED, HALF = Sc::HALF, TWICE = Sc::TWICE;
     constexpr int KS = DP / 16, DT = DP / 32, CH = DP / 8;
-    constexpr bool ALWAYS = DP == 256 || SCORED; // the maximum is taken off in every tile
+    constexpr bool ALWAYS = DP == 256; // the maximum is taken off in every tile
     __shared__ __align__(16) typename KvTiles<S, T, DP, NW, ONE, SCORED>::Lds lds;
     const int tid = threadIdx.x, wave = same(tid >> 6), lane = tid & 63, col = lane & 31, hf = lane >> 5;
     const int late = NW > 4 ? wave >> 2 : 0;
@@ -1097,10 +1113,7 @@ __global__ __launch_bounds__(NW * 64) void kv_tile_kernel(KvAttend a)
     float m = -INFINITY, l = 0.f;
 
     KvScoring scoring;
-    if constexpr (SCORED) {
-        scoring.begin(a, h * G + member, qscale);
-        qscale = 1.f; // (scores are powers of two from the start)
-    }
+    if constexpr (SCORED) scoring.begin(a, h * G + member, qscale);
 
     // ---- the two phases
     u32x4 pf[4], pr[4];
@@ -1157,21 +1170,19 @@ __global__ __launch_bounds__(NW * 64) void kv_tile_kernel(KvAttend a)
                 for (int j = 0; j < 8; ++j) s[u >> 1][8 * (u & 1) + j] *= ks[u * 16 + hf * 8 + j];
         }
         if constexpr (SCORED) {
-            float y[32];
+            if (scoring.capped || scoring.biased) {
+                float y[32];
 #pragma unroll
-            for (int i = 0; i < 32; ++i) y[i] = s[i >> 4][i & 15];
-            if (scoring.capped) scoring.cap_all(y);
-            else {
+                for (int i = 0; i < 32; ++i) y[i] = s[i >> 4][i & 15];
+                if (scoring.capped) scoring.cap_all(y);
+                if (scoring.biased) {
+                    const float away = (float)(pos - base - hf * 8);
 #pragma unroll
-                for (int i = 0; i < 32; ++i) y[i] *= scoring.z;
+                    for (int i = 0; i < 32; ++i) y[i] = __builtin_fmaf(-scoring.slope, fabsf(away - (float)(i / 8 * 16 + i % 8)), y[i]);
+                }
+#pragma unroll
+                for (int i = 0; i < 32; ++i) s[i >> 4][i & 15] = y[i];
             }
-            if (scoring.biased) {
-                const float away = (float)(pos - base - hf * 8);
-#pragma unroll
-                for (int i = 0; i < 32; ++i) y[i] = __builtin_fmaf(-scoring.slope, fabsf(away - (float)(i / 8 * 16 + i % 8)), y[i]);
-            }
-#pragma unroll
-            for (int i = 0; i < 32; ++i) s[i >> 4][i & 15] = y[i];
         }
         float above = m; // what a score has to exceed to be a new maximum
         if (far || held != 15u || (!(SCORED && base + kKvTile <= prefix) && __any(base + kKvTile - 1 > pos || base < from))) {

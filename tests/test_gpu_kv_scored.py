@@ -3,7 +3,7 @@
 Tolerances are those of test_gpu_kv, with e, the relative error of a weight, from these errors of a score (twice their sum, a score's and the largest
 one's, and 2^-20 for the exponential, the sums and the scale):
   (D + 8) 2^-24 sum|q k| scale   the product
-  2^-21 min(cap, 2 largest |x|)  the cap: where some score x of a wave is beyond cap / 2, tanh = 1 - 2 / (1 + e^2z), in which the quotient is
+  2^-21 min(cap, 2 largest |x|)  the cap: where a score x is beyond cap / 2, tanh = 1 - 2 / (1 + e^2z), in which the quotient is
                                  off by 2^-23, the sum below it by 2^-24 and the power by 2^-21 of itself (at z < 3, later it is none of
                                  the result's): 2 (2^-23 + 2^-24) / (1 + e) + 2^-21 / 2 of the cap, less than 2^-21; else a polynomial, off by
                                  2^-26 and six roundings, 2^-21 of the score
@@ -47,7 +47,6 @@ class Setup(base.Setup):
         u_out, u_w = U[self.kind], 2 * U[torch.float16] if self.storage in ("i8", "f8") else U[self.kind]
         out, lse, q, cap = out.cpu().double(), lse.cpu().double(), self.q.double(), how["cap"]
         slopes = how["slopes"].double() if "slopes" in how else torch.zeros(self.H * self.G, dtype=torch.float64)
-        most = max([float(((q[row, h * self.G:(h + 1) * self.G] @ ks[i][:, h].T) * scale).abs().max()) for row, i, _ in self.tokens() for h in range(self.H) if self.lens[i]] + [0.0])
         for row, i, pos in self.tokens():
             key = torch.arange(self.lens[i])
             mask = key <= pos
@@ -67,6 +66,7 @@ class Setup(base.Setup):
                     continue
                 x = (q[row, rows] @ k.T) * scale
                 size = ((q[row, rows].abs() @ k.abs().T) * abs(scale)).amax(1, keepdim=True)
+                most = x.abs().amax(1, keepdim=True)
                 if cap:
                     x = cap * torch.tanh(x / cap)
                 bias = slopes[rows, None] * far
@@ -74,7 +74,7 @@ class Setup(base.Setup):
                 w = torch.softmax(x, 1)
                 # (a key that is far below the largest has no weight, and its error none either)
                 near = x > x.amax(1, keepdim=True) - 60
-                off_score = (self.D + 8) * 2.0 ** -24 * size + (2.0 ** -21 * min(cap, 2 * most) if cap else 0.0)
+                off_score = (self.D + 8) * 2.0 ** -24 * size + (2.0 ** -21 * (2 * most).clamp(max=cap) if cap else 0.0)
                 off_score = off_score + ((2.0 ** -22 * bias.abs() + 2.0 ** -23 * x.abs()) * near).amax(1, keepdim=True)
                 e = 2 * off_score + 2.0 ** -20
                 ref, a = w @ v, w @ v.abs()
@@ -178,6 +178,19 @@ def test_fewer_tokens_than_the_host_says(gpu_device, storage, dtype, P, D, news)
     B.pk_kv_attend_scored(s.cache.handle, batch.c, q, 0.1, 0, 9.0, h["slopes"].cuda(), starts, h["prefix"].cuda(), out, lse)
     s.check(out[:sum(news)], lse[:sum(news)], 0.1, h)
     assert torch.all(out[sum(news):].isnan()) and torch.all(lse[sum(news):].isnan())
+
+
+@pytest.mark.parametrize("storage,dtype", [("bf16", "bf16"), ("i8", "f16"), ("f4", "bf16")])
+def test_what_no_query_sees_changes_no_bit(gpu_device, storage, dtype):
+    """Rows behind a sequence's end, other sequences' scores beside the cap, other contents of pages that are free."""
+    got = []
+    for garbage, size in ((0xff, 1.0), (0x00, 1.0), (0x7b, 40.0)):
+        s = Setup(storage, dtype, 2, 4, 64, 64, [1, 40, 1], [75, 100, 300], seed=61, garbage=garbage)
+        s.q[0] *= size  # (another sequence's queries)
+        out, lse = s.run(0.125, s.how(cap=1000.0, slopes=0.01))
+        got.append((out[1:], lse[1:]))
+    for out, lse in got[1:]:
+        assert torch.equal(out, got[0][0]) and torch.equal(lse, got[0][1])
 
 
 def test_calls_in_a_graph_follow_the_arrays(gpu_device):
