@@ -225,7 +225,6 @@ __device__ __forceinline__ uint8_t to_code(float x, float up)
         const int code = (int)rintf(y);
         return (uint8_t)(!VALUES ? code + 128 : code < 0 ? 0x80 - code : code);
     }
-    if constexpr (S == PK_F4) return (uint8_t)(__builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, y, y, 1.f, 0) & 15u);
     return (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(y, y, 0, false);
 }
 

@@ -13,13 +13,18 @@ constexpr int kThreads = 256;
 constexpr int kRowLanes = 16; // lanes that share a row: a quarter of a wave
 constexpr int kRowsAtOnce = kThreads / kRowLanes;
 
-// largest of 16 neighbouring lanes, in all of them
-__device__ __forceinline__ float quarter_max(float x)
+// largest of 2, 4, 8 or 16 neighbouring lanes, in all of them, by lane moves (no LDS)
+template <int N>
+__device__ __forceinline__ float lanes_max(float x)
 {
-#pragma unroll
-    for (int d = 1; d < kRowLanes; d *= 2) x = fmaxf(x, __shfl_xor(x, d));
+    auto with = [](float v, int moved) __attribute__((always_inline)) { return fmaxf(v, __int_as_float(moved)); };
+    x = with(x, __builtin_amdgcn_update_dpp(0, __float_as_int(x), 0xb1, 0xf, 0xf, true));                         // lanes 1 0 3 2
+    if constexpr (N >= 4) x = with(x, __builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x4e, 0xf, 0xf, true));   // 2 3 0 1
+    if constexpr (N >= 8) x = with(x, __builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x141, 0xf, 0xf, true));  // 7 6 .. 0
+    if constexpr (N >= 16) x = with(x, __builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x140, 0xf, 0xf, true)); // 15 14 .. 0
     return x;
 }
+__device__ __forceinline__ float quarter_max(float x) { return lanes_max<kRowLanes>(x); }
 
 // E consecutive elements of a caller's row, zeros past its D.
 template <int T, int E>
@@ -83,15 +88,24 @@ __device__ __forceinline__ uint32_t pack_run(uint32_t a, uint32_t b) // eight of
 // What a workgroup does: one page that the batch touches, one head.
 struct KvPage {
     KvSeq q;
-    int lp, base, p0, p1; // its number in the sequence, its first position, the rows of the batch's new tokens in it
+    int h, lp, base, p0, p1; // the head; the page's number in the sequence, its first position, the rows of the batch's new tokens in it
     uint32_t page;
 };
+// Heads of a page one after the other, where a grid has that many: rows of a token, heads side by side, are then read (and written) at about
+// the same time.
+dim3 page_grid(const KvDev &c, const KvBatch &b)
+{
+    const int64_t pages = kv_touched(c, b);
+    return pages * c.H <= kKvMaxGroups ? dim3((unsigned)(pages * c.H), 1, b.n_seqs) : dim3((unsigned)pages, c.H, b.n_seqs);
+}
 __device__ __forceinline__ bool kv_page_of(const KvDev &c, const KvBatch &b, KvPage &g)
 {
     const int s = blockIdx.z;
     g.q = kv_seq(b, s, c.P);
     const int begin = max(g.q.len - g.q.m, 0);
-    g.lp = (begin >> c.logP) + (int)blockIdx.x;
+    const bool flat = gridDim.y == 1;
+    g.h = flat ? blockIdx.x % c.H : blockIdx.y;
+    g.lp = (begin >> c.logP) + (int)(flat ? blockIdx.x / c.H : blockIdx.x);
     if (g.q.m == 0 || ((long long)g.lp << c.logP) >= g.q.len) return false;
     g.page = (uint32_t)b.tables[(size_t)s * b.table_stride + g.lp];
     g.base = g.lp << c.logP;
@@ -111,22 +125,31 @@ __device__ __forceinline__ float encode(const float (&x)[E], char (&codes)[kv_pa
         float most = 0.f;
 #pragma unroll
         for (int i = 0; i < E; ++i) most = fmaxf(most, fabsf(x[i]));
-        float group = most; // of 32 channels: 32 / E lanes
-#pragma unroll
-        for (int d = 1; d < 32 / E; d *= 2) group = fmaxf(group, __shfl_xor(group, d));
+        const float group = lanes_max<32 / E>(most); // of 32 channels
         most = quarter_max(most);
         const float up = code_factor(most, kv_largest<S>);
-        float shift = 1.f;
-        if constexpr (!VALUES) {
-            const uint32_t e = min((__float_as_uint(most) - __float_as_uint(group)) >> 23, 15u);
-            power = 127u - e;
-            shift = __uint_as_float((127u + e) << 23);
+        // (the conversion divides by a power of two before it rounds, and gives 6 for what is beyond: no more than a rounding of the product)
+        if constexpr (VALUES) {
+#pragma unroll
+            for (int i = 0; i < E; i += 4) {
+                uint32_t w = 0;
+                w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[i] * up, 0.f, 1.f, 0);
+                w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[i + 1] * up, 0.f, 1.f, 1);
+                w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[i + 2] * up, 0.f, 1.f, 2);
+                w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[i + 3] * up, 0.f, 1.f, 3);
+                __builtin_memcpy(codes + i, &w, 4);
+            }
+        } else {
+            power = 127u - min((__float_as_uint(most) - __float_as_uint(group)) >> 23, 15u);
+            const float unit = power_of(power);
+#pragma unroll
+            for (int i = 0; i < E; i += 4) {
+                uint32_t w = 0;
+                w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[i] * up, x[i + 1] * up, unit, 0);
+                w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[i + 2] * up, x[i + 3] * up, unit, 1);
+                __builtin_memcpy(codes + i / 2, &w, 2);
+            }
         }
-        uint8_t c[E];
-#pragma unroll
-        for (int i = 0; i < E; ++i) c[i] = to_code<S, VALUES>(x[i] * shift, up);
-#pragma unroll
-        for (int i = 0; i < kv_part<S, E, VALUES>; ++i) codes[i] = (char)(VALUES ? c[i] : c[2 * i] | c[2 * i + 1] << 4);
         return most * (1.f / kv_largest<S>);
     } else if constexpr (kv_coded<S>) {
         float most = 0.f;
@@ -177,10 +200,10 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(KvDev c, KvBatch b,
     constexpr bool FOUR = S == PK_F4;
     extern __shared__ __align__(16) char image[];
     __shared__ float red[4][2][DP];
-    const int h = blockIdx.y, tid = threadIdx.x;
+    const int tid = threadIdx.x;
     KvPage g;
     if (!kv_page_of(c, b, g) || g.page >= c.n_pages) return;
-    const int p0 = g.p0, p1 = g.p1;
+    const int h = g.h, p0 = g.p0, p1 = g.p1;
     char *kimg = image, *vimg = image + c.P * RB;
     const size_t ph = (size_t)g.page * c.H + h;
     char *kp = c.k + ph * c.P * RB;
@@ -197,8 +220,13 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(KvDev c, KvBatch b,
     auto bound = [&](const char *codes, float scale, uint32_t power) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < E; ++i) {
-            float z = decode<S, false>(codes, i);
-            if constexpr (FOUR) z *= power_of(power);
+            float z;
+            if constexpr (FOUR) {
+                const f32x2 both = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4((uint32_t)(uint8_t)codes[i / 2], power_of(power), 0);
+                z = both[i & 1];
+            } else {
+                z = decode<S, false>(codes, i);
+            }
             if constexpr (kv_coded<S>) z *= scale;
             hi[i] = fmaxf(hi[i], z);
             lo[i] = fminf(lo[i], z);
@@ -342,9 +370,10 @@ __global__ __launch_bounds__(kThreads) void kv_read_kernel(KvDev c, KvBatch b, c
     constexpr int RB = DP * kv_bits<S> / 8, ES = kv_value_bytes<S>, TS = T == PK_F32 ? 4 : 2, E = DP / kRowLanes, KB = kv_part<S, E, false>;
     constexpr bool FOUR = S == PK_F4;
     extern __shared__ __align__(16) char image[];
-    const int h = blockIdx.y, tid = threadIdx.x;
+    const int tid = threadIdx.x;
     KvPage g;
     if (!kv_page_of(c, b, g)) return;
+    const int h = g.h;
     const bool there = g.page < c.n_pages;
     char *kimg = image, *vimg = image + c.P * RB;
     const size_t ph = (size_t)(there ? g.page : 0) * c.H + h;
@@ -450,7 +479,7 @@ hipError_t with_image(K kernel, size_t lds, dim3 grid, hipStream_t s, A... args)
 template <int S, int T>
 hipError_t append_dp(const KvDev &c, int dp, const KvBatch &b, const KvRows &k, const KvRows &v, hipStream_t s)
 {
-    const dim3 grid(kv_touched(c, b), c.H, b.n_seqs);
+    const dim3 grid = page_grid(c, b);
     if (dp == 64) return with_image(kv_append_kernel<S, T, 64>, image_bytes<S, 64>(c.P), grid, s, c, b, k, v);
     if (dp == 128) return with_image(kv_append_kernel<S, T, 128>, image_bytes<S, 128>(c.P), grid, s, c, b, k, v);
     return with_image(kv_append_kernel<S, T, 256>, image_bytes<S, 256>(c.P), grid, s, c, b, k, v);
@@ -467,7 +496,7 @@ hipError_t append_s(const KvDev &c, int dp, const KvBatch &b, const KvRows &k, c
 template <int S, int T>
 hipError_t read_dp(const KvDev &c, int dp, const KvBatch &b, char *k, char *v, hipStream_t s)
 {
-    const dim3 grid(kv_touched(c, b), c.H, b.n_seqs);
+    const dim3 grid = page_grid(c, b);
     if (dp == 64) return with_image(kv_read_kernel<S, T, 64>, image_bytes<S, 64>(c.P), grid, s, c, b, k, v);
     if (dp == 128) return with_image(kv_read_kernel<S, T, 128>, image_bytes<S, 128>(c.P), grid, s, c, b, k, v);
     return with_image(kv_read_kernel<S, T, 256>, image_bytes<S, 256>(c.P), grid, s, c, b, k, v);

@@ -293,13 +293,15 @@ __device__ __forceinline__ void kv_join_parts(const KvAttend &a, size_t first, i
 // Measured (medians), 8 heads of 128, 4 query heads each: one token of each of 48 sequences of up to 32768 tokens, int8, 1.22 GB in 235 us,
 // 5.2 TB/s (without what is asked for ahead 446); one token of 1025, bf16, 9.2 us, a chain of lengths, pages, keys and the join.
 // Of 256 channels at 16 bits K and V do not fit the 512 registers of one wave a SIMD: 70 - 96 of them go to scratch, 268 - 376 bytes a lane (48
-// sequences of 8192 bf16 tokens, a token each, 787 us, 4.1 TB/s; int8, with no scratch, 296 us, 5.5 TB/s).
+// sequences of 8192 bf16 tokens, a token each, 787 us, 4.1 TB/s; int8, with no scratch, 296 us, 5.5 TB/s; 4 bits 172 us, 250 where two waves of a SIMD have 256 registers each).
+// 4 bits: one token of each of 48 sequences of up to 65536 tokens, 128 channels, 1.11 GB in 228 us, 4.9 TB/s: three waves a SIMD with half the bytes of 8 bits on
+// their way, vector units 38 % busy.
 // R: where there are 16 / R queries at most, each of them has R columns, and a column weighs that part of a lane's keys that is its own: a
 // column is a softmax of its own, joined with the others in the end as the waves' are.  For the sparse form, which reads from the
 // caches and is bound by the vector units (1024 tokens, 32 blocks each of int8: 4 query heads a group, R 1 403 us, R 4 352 - 362; 2, R 1 412,
 // R 4 373; 8, R 1 423, R 2 393).
 template <int S, int T, int DP, bool SPARSE, bool ONE, int R, bool SCORED>
-__global__ __launch_bounds__(256, DP * kv_bits<S> / 8 > 128 ? 1 : 2) void kv_rows_kernel(KvAttend a)
+__global__ __launch_bounds__(256, DP * kv_bits<S> / 8 > 128 || (S == PK_F4 && DP == 256) ? 1 : 2) void kv_rows_kernel(KvAttend a)
 {
     using Sc = KvScaling<S, T>;
     constexpr bool CODED = Sc::CODED, HALF = Sc::HALF, TWICE = Sc::TWICE, FOUR = S == PK_F4;
@@ -1358,7 +1360,8 @@ hipError_t run(KvAttend a, hipStream_t s)
     // Most rows of queries of a sequence and head that are taken 16 at a time (above: 256 at a time).  Measured in us, 8 heads of 128 channels, 16
     // (256) at a time: bf16, 16 sequences of 64 rows over 8192 keys 182 (168), of 128 rows 309 (171), one of 64 rows over 32768 keys 54 (63), of
     // 128 rows 94 (65).  Codes of 8 bits cost the kernel for many more work for each tile, and half the reads here: int8, 16 sequences of 64 rows
-    // 115 (209), of 128 rows 214 (214), of 256 rows 382 (236); one of 128 rows over 32768 keys 65 (78), of 256 rows 112 (85).  (Other channels
+    // 115 (209), of 128 rows 214 (214), of 256 rows 382 (236); one of 128 rows over 32768 keys 65 (78), of 256 rows 112 (85); 4 bits, 16 sequences of 64 rows
+    // 81 (81), of 128 rows 147 (183), of 256 rows 201 (195), one of 128 rows over 32768 keys 45 (62).  (Other channels
     // and heads go by the same numbers, unmeasured; so do the numbers of parts.)
     a.few_rows = SPARSE ? INT32_MAX : kv_coded<S> ? kKvFewRows : 64;
     a.part_row = DP;
