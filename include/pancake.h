@@ -528,6 +528,7 @@ int pk_kv_attend(pk_kv *kv, const pk_kv_batch *batch, const pk_rows *q, int32_t 
  * and its score is
  *   cap tanh(scale q.k / cap) - slope |p - j|
  * A prefix is seen by queries before its end too.  start: of the query's token, the first position of its document; negative ones are 0.
+ * PK_ERR_UNSUPPORTED also for slopes with a scale between 0 and 2^-60.
  */
 typedef struct {
     float cap;             /* > 0, finite; 0: scores are not capped                      */

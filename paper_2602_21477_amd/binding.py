@@ -718,7 +718,8 @@ class KVCache:
 
 
 class KVPool:
-    """The pages of a cache: who has them, and which are free (no arithmetic here).  Tables are int32 tensors [sequence, page] of the caller's, changed in place."""
+    """The pages of a cache: who has them, and which are free (no arithmetic here).  Tables are int32 tensors [sequence, page] of the caller's, changed in place.  Calls
+    go to the current stream of the cache's device, which has to be the current device."""
 
     def __init__(self, cache):
         self.handle = None

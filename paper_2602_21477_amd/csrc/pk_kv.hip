@@ -549,6 +549,7 @@ using namespace pk;
 
 namespace {
 
+constexpr float kLeastBiasedScale = 0x1p-60f;
 constexpr int kMaxHeads = 1024; // key/value heads of a cache, and query heads of one of them
 
 size_t up256(size_t v) { return (v + 255) / 256 * 256; }
@@ -631,8 +632,10 @@ int attend(pk_kv *kv, const pk_kv_batch *batch, const pk_rows *q, int32_t n_q_he
     a.blocks = blocks;
     a.n_blocks = n_blocks;
     if (scores && (scores->cap > 0.f || scores->slopes || scores->starts || scores->prefix)) {
+        // (a bias is made one of the products that the scale multiplies)
+        if (scores->slopes && scale != 0.f && std::fabs(scale) < kLeastBiasedScale) return PK_ERR_UNSUPPORTED;
         a.scored = 1;
-        a.cap = scores->cap;
+        a.cap = scores->cap > 0.f ? std::min(std::max(scores->cap, 1e-30f), 1e37f) : 0.f; // (nothing, and no cap at all, in 32 bits)
         a.slopes = scores->slopes;
         a.starts = scores->starts;
         a.prefix = scores->prefix;

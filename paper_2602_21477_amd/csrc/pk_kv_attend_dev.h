@@ -153,8 +153,8 @@ struct KvScoring {
     {
         capped = a.cap > 0.f, biased = a.slopes != nullptr;
         cap = a.cap * kLog2e;
-        z = qscale / cap;
-        twice = z * (2.f * kLog2e);
+        z = fminf(qscale / cap, 1e38f); // (0 of it is 0)
+        twice = fminf(z * (2.f * kLog2e), 3e38f);
         slope = biased ? a.slopes[query_head] * kLog2e : 0.f;
         if (capped) qscale = 1.f;
         else slope /= qscale;
@@ -1360,8 +1360,8 @@ hipError_t run(KvAttend a, hipStream_t s)
     // Most rows of queries of a sequence and head that are taken 16 at a time (above: 256 at a time).  Measured in us, 8 heads of 128 channels, 16
     // (256) at a time: bf16, 16 sequences of 64 rows over 8192 keys 182 (168), of 128 rows 309 (171), one of 64 rows over 32768 keys 54 (63), of
     // 128 rows 94 (65).  Codes of 8 bits cost the kernel for many more work for each tile, and half the reads here: int8, 16 sequences of 64 rows
-    // 115 (209), of 128 rows 214 (214), of 256 rows 382 (236); one of 128 rows over 32768 keys 65 (78), of 256 rows 112 (85); 4 bits, 16 sequences of 64 rows
-    // 81 (81), of 128 rows 147 (183), of 256 rows 201 (195), one of 128 rows over 32768 keys 45 (62).  (Other channels
+    // 115 (209), of 128 rows 214 (214), of 256 rows 382 (236); one of 128 rows over 32768 keys 65 (78), of 256 rows 112 (85); 4 bits, 16 sequences of 128 rows
+    // 147 (183), one of 128 rows over 32768 keys 45 (62).  (Other channels
     // and heads go by the same numbers, unmeasured; so do the numbers of parts.)
     a.few_rows = SPARSE ? INT32_MAX : kv_coded<S> ? kKvFewRows : 64;
     a.part_row = DP;

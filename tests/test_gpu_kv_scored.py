@@ -156,6 +156,16 @@ def test_scales_and_caps_of_any_size(gpu_device, storage, dtype, scale):
 
 
 @pytest.mark.parametrize("storage,dtype", [("bf16", "bf16"), ("i8", "bf16"), ("f4", "f16")])
+def test_caps_and_scales_at_the_ends_of_32_bits(gpu_device, storage, dtype):
+    for news in ([2, 1], [90, 1]):
+        s = Setup(storage, dtype, 1, 2, 64, 32, news, [130, 40], seed=62, spread=0.3)
+        s.q[1] = 0  # (scores of 0)
+        for scale, kind in ((0.125, dict(cap=3e38)), (0.125, dict(cap=1e-40)), (0.125, dict(cap=1e-30, slopes=0.1)), (1e-40, dict(cap=2.0)), (2.0 ** -60, dict(slopes=0.1)), (1e-40, dict(docs=9))):
+            h = s.how(**kind)
+            s.check(*s.run(scale, h), scale, h)
+
+
+@pytest.mark.parametrize("storage,dtype", [("bf16", "bf16"), ("i8", "bf16"), ("f4", "f16")])
 def test_without_some_pages(gpu_device, storage, dtype):
     s = Setup(storage, dtype, 2, 3, 64, 16, [5, 1, 20, 33], [70, 17, 20, 90], seed=55, missing=[(0, 0), (0, 2), (1, 0), (1, 1), (2, 0), (3, 5), (3, 4), (3, 3)])
     for kind in (dict(cap=9.0), dict(prefix=[40, 17, 20, 1]), dict(docs=33, slopes=0.1)):
@@ -254,6 +264,9 @@ def test_refusals(gpu_device):
                 dict(starts=torch.zeros(2, device="cuda")), dict(prefix=torch.zeros(2, dtype=torch.int32, device="cuda"))):
         with pytest.raises(ValueError):
             s.cache.attend(q, s.batch, 0.1, **bad)
+    with pytest.raises(B.PancakeError) as e:
+        s.cache.attend(q, s.batch, 1e-30, slopes=good)
+    assert e.value.status == B.PK_ERR_UNSUPPORTED
     for bad in (dict(window=-1), dict(scale=math.nan)):
         with pytest.raises(B.PancakeError) as e:
             s.cache.attend(q, s.batch, **{"scale": 0.1, "cap": 2.0, **bad})
