@@ -388,9 +388,10 @@ __global__ __launch_bounds__(kThreads) void kv_read_kernel(KvDev c, KvBatch b, c
             *reinterpret_cast<u32x4 *>(to) = unpack_run(w[0], w[1]);
             *reinterpret_cast<u32x4 *>(to + v_image<1, DP>(0, 16)) = unpack_run(w[2], w[3]);
         }
-    } else
-    for (int i = g.p0 / N * DP + tid; i < (g.p1 + N - 1) / N * DP; i += kThreads)
-        *reinterpret_cast<u32x4 *>(vimg + v_image<ES, DP>(i / DP * N, i % DP)) = *reinterpret_cast<const u32x4 *>(vp + (size_t)i * 16);
+    } else {
+        for (int i = g.p0 / N * DP + tid; i < (g.p1 + N - 1) / N * DP; i += kThreads)
+            *reinterpret_cast<u32x4 *>(vimg + v_image<ES, DP>(i / DP * N, i % DP)) = *reinterpret_cast<const u32x4 *>(vp + (size_t)i * 16);
+    }
     __syncthreads();
     const int sub = tid & (kRowLanes - 1), at = sub * E;
     if (at >= c.D) return;
