@@ -1186,14 +1186,18 @@ __global__ __launch_bounds__(NW * 64) void kv_tile_kernel(KvAttend a)
         }
         float above = m; // what a score has to exceed to be a new maximum
         if (far || held != 15u || (!(SCORED && base + kKvTile <= prefix) && __any(base + kKvTile - 1 > pos || base < from))) {
-            const int last = min(pos, sq.len - 1) - base, since = from - base;
+            // the tile's 64 keys as bits, of which a lane has the even or the odd bytes; two instructions a score
+            const int last = min(pos, sq.len - 1) - base, since = max(from - base, 0), upto = min(last, kKvTile - 1);
+            unsigned long long seen = upto >= since ? (~0ull >> (63 - upto)) & (~0ull << since) : 0ull;
+            if (SCORED && prefix > base) seen |= ~0ull >> (64 - min(prefix - base, kKvTile));
+            const unsigned long long runs = (held & 1 ? 0xffffull : 0ull) | (held & 2 ? 0xffffull << 16 : 0ull) | (held & 4 ? 0xffffull << 32 : 0ull) | (held & 8 ? 0xffffull << 48 : 0ull);
+            seen &= runs;
+            const uint32_t gone = ~__builtin_amdgcn_perm((uint32_t)(seen >> 32), (uint32_t)seen, hf ? 0x07050301u : 0x06040200u);
 #pragma unroll
-            for (int u = 0; u < 4; ++u)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const int key = u * 16 + hf * 8 + j;
-                    s[u >> 1][8 * (u & 1) + j] = ((key <= last && key >= since) || (SCORED && key < prefix - base)) && (held >> u & 1) ? s[u >> 1][8 * (u & 1) + j] : -INFINITY;
-                }
+            for (int i = 0; i < 32; ++i) {
+                const uint32_t none = (uint32_t)__builtin_amdgcn_sbfe((int)gone, i, 1);
+                s[i >> 4][i & 15] = __uint_as_float((none & 0xff800000u) | (~none & __float_as_uint(s[i >> 4][i & 15])));
+            }
             if (far) {
                 above = INFINITY;
                 float m1 = m;

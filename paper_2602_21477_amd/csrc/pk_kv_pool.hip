@@ -365,20 +365,25 @@ __device__ __forceinline__ uint32_t in_use(const KvPool &p, uint32_t word)
     return ~p.bits[word] & there;
 }
 
-// Pages in use before each word's, by one workgroup: 32768 words, a million pages, a step.
+// Pages in use before each word's, by one workgroup, 131072 pages a step: 13000 pages 4.7 us (32 words a thread, fewer steps for many pages: 10.3).
 __global__ __launch_bounds__(kGrantThreads) void kv_rank_kernel(KvPool from, KvPool to, int32_t *missing)
 {
     __shared__ int sums[kGrantThreads / 64];
-    constexpr int EACH = 32;
+    constexpr int EACH = 4;
     int upto = 0;
     for (uint32_t w0 = 0; w0 < from.n_words; w0 += kGrantThreads * EACH) {
         const uint32_t first = w0 + threadIdx.x * EACH;
-        int n = 0;
-        for (uint32_t w = first; w < min(first + EACH, from.n_words); ++w) n += __popc(in_use(from, w));
-        int total, at = upto + scan(n, sums, total);
-        for (uint32_t w = first; w < min(first + EACH, from.n_words); ++w) {
-            from.rank[w] = at;
-            at += __popc(in_use(from, w));
+        int n[EACH], all = 0;
+#pragma unroll
+        for (int k = 0; k < EACH; ++k) {
+            n[k] = first + k < from.n_words ? __popc(in_use(from, first + k)) : 0;
+            all += n[k];
+        }
+        int total, at = upto + scan(all, sums, total);
+#pragma unroll
+        for (int k = 0; k < EACH; ++k) {
+            if (first + k < from.n_words) from.rank[first + k] = at;
+            at += n[k];
         }
         upto += total;
     }
