@@ -109,6 +109,9 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 struct __attribute__((packed, aligned(2))) AnyEight16 {
     u32x4 v;
 };
+struct __attribute__((packed, aligned(2))) AnyFour16 {
+    u32x2 v;
+};
 struct __attribute__((packed, aligned(4))) AnyFour32 {
     f32x4 v;
 };
@@ -129,6 +132,30 @@ __device__ __forceinline__ void load_eight(float (&x)[8], const char *row, int a
         const u32x4 w = reinterpret_cast<const AnyEight16 *>(row + (size_t)at * 2)->v;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
+            if constexpr (T == PK_BF16) {
+                x[2 * i] = __uint_as_float(w[i] << 16);
+                x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+            } else {
+                const half2v h = __builtin_bit_cast(half2v, (uint32_t)w[i]);
+                x[2 * i] = (float)h[0];
+                x[2 * i + 1] = (float)h[1];
+            }
+        }
+    }
+}
+
+// Four of them.
+template <int T>
+__device__ __forceinline__ void load_four(float (&x)[4], const char *row, int at)
+{
+    if constexpr (T == PK_F32) {
+        const f32x4 a = reinterpret_cast<const AnyFour32 *>(row + (size_t)at * 4)->v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = a[i];
+    } else {
+        const u32x2 w = reinterpret_cast<const AnyFour16 *>(row + (size_t)at * 2)->v;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
             if constexpr (T == PK_BF16) {
                 x[2 * i] = __uint_as_float(w[i] << 16);
                 x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);

@@ -42,13 +42,9 @@ __device__ __forceinline__ void load_row(float (&x)[E], const char *row, int at,
         }
     } else {
         static_assert(E == 4, "");
-        float y[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = 0.f;
-        const int half = at & 4;
-        if (at < D) load_eight<T>(y, row, at - half);
-#pragma unroll
-        for (int i = 0; i < E; ++i) x[i] = half ? y[i + 4] : y[i];
+        for (int i = 0; i < E; ++i) x[i] = 0.f;
+        if (at < D) load_four<T>(x, row, at);
     }
 }
 
@@ -188,8 +184,8 @@ __device__ __forceinline__ float decode(const char *codes, int i)
 // read back.  They depend on the rows alone, not on the calls that brought them.  Every row is read once
 // and its codes written once, in the order of memory: without the page put together in LDS first, values went out a byte at a time (a
 // prompt of 65536 tokens with its reading back 245 us, with it 199).  Measured (medians): 65536 tokens of 8 heads of 128 from half precision to int8,
-// 403 MB in 117 us, 3.4 TB/s, the vector units (maxima, codes, bounds) two thirds busy; from bf16 to bf16, 537 MB in 128 us, 4.2 TB/s; of 64
-// channels 165 - 174 us, 1.2 - 1.5 TB/s.  One token of each of 64 sequences 7.1 us, of which most is the older rows of 512 pages read
+// 403 MB in 99 us, 4.1 TB/s, the vector units (maxima, codes, bounds) two thirds busy; to 4 bits, 341 MB in 100 us, 3.4 TB/s; from bf16 to bf16, 537 MB in
+// 122 us, 4.4 TB/s; of 64 channels 49 - 57 us (166 - 174 where two lanes each read the eight elements that they share).  One token of each of 64 sequences 7.1 us, of which most is the older rows of 512 pages read
 // back for their bounds, after two dependent loads.
 template <int S, int T, int DP>
 __global__ __launch_bounds__(kThreads) void kv_append_kernel(KvDev c, KvBatch b, KvRows kin, KvRows vin)
@@ -363,7 +359,7 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(KvDev c, KvBatch b,
 
 // One workgroup: one page of the batch's tokens, one head: the page into LDS as it lies in memory, out of it by rows, 16 lanes each.
 // Bound by memory: 131071 tokens of 8 heads of 128 from e4m3 to half precision, 805 MB in 168 us (median), 4.8 TB/s; 65536 from bf16 to bf16,
-// 537 MB in 121 us, 4.4 TB/s.
+// 537 MB in 118 us, 4.5 TB/s.
 template <int S, int T, int DP>
 __global__ __launch_bounds__(kThreads) void kv_read_kernel(KvDev c, KvBatch b, char *kout, char *vout)
 {

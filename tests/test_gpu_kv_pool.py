@@ -331,6 +331,40 @@ def test_a_step_of_branches_in_a_graph(gpu_device):
                 assert torch.equal(a[row * 99 + 99 - n:row * 99 + 99], c[row * 99 + 99 - n:row * 99 + 99]), (i, row)
 
 
+@pytest.mark.parametrize("generous", [False, True])
+def test_pools_of_many_pages(gpu_device, generous):
+    """300 000 pages, more than a step of either kernel looks at: the lowest free ones, wherever they lie, and ranks among all."""
+    n, P = 300_000, 16
+    cache = B.KVCache(n, 1, 8, storage=B.PK_I8, page_tokens=P)
+    pool = B.KVPool(cache)
+    full = torch.arange(290_000, dtype=torch.int32, device="cuda").view(290, 1000)
+    pool.adopt(full)
+    empty = torch.full((3, 40_000), -1, dtype=torch.int32, device="cuda")
+    b = B.KVBatch(empty, ints([0, 1, 1, 18]), ints([1, 0, 17]), 18, 18 if generous else 17, 40_000 * P if generous else 17)
+    assert pool.grant(b).item() == 0
+    assert empty[:, :2].tolist() == [[290_000, -1], [-1, -1], [290_001, 290_002]] and bool((empty[:, 2:] == -1).all())
+    rows = torch.arange(1, 290, 2, dtype=torch.int32, device="cuda")
+    pool.release(full, rows)
+    more = torch.full((1, 40_000), -1, dtype=torch.int32, device="cuda")
+    pages = 11_000  # of the first released rows: eleven and a bit, in 23 000 pages with holes between
+    b = B.KVBatch(more, ints([0, pages * P]), ints([pages * P]), pages * P, pages * P, pages * P)
+    assert pool.grant(b).item() == 0
+    free = torch.arange(290_000, device="cuda").view(290, 1000)[1::2].flatten()[:pages]
+    assert torch.equal(more[0, :pages].long(), free)
+    counts = pool.counts()
+    assert int(counts.sum()) == 145_000 + pages + 3 and int(counts.max()) == 1
+    rank = (counts > 0).long().cumsum(0) - 1
+    into = B.KVPool(B.KVCache(150_000, 1, 8, storage=B.PK_I8, page_tokens=P))
+    whole = torch.cat([full.flatten(), more[0, :pages], empty[0, :1], empty[2, :2]])[None].contiguous()
+    out, missing = pool.compact(into, whole)
+    want = torch.where(whole >= 0, rank[whole.clamp(min=0).long()], torch.full_like(rank[:1], -1)).int()
+    want[want >= 150_000] = -1
+    assert torch.equal(out, want) and missing.item() == 145_000 + pages + 3 - 150_000
+    assert bool((into.counts() == 1).all())
+    cache.close()
+    into.cache.close()
+
+
 def test_refusals(gpu_device):
     cache = B.KVCache(4, 1, 64, page_tokens=16)
     pool, tables = B.KVPool(cache), torch.full((2, 4), -1, dtype=torch.int32, device="cuda")
