@@ -13,16 +13,45 @@ constexpr int kThreads = 256;
 constexpr int kRowLanes = 16; // lanes that share a row: a quarter of a wave
 constexpr int kRowsAtOnce = kThreads / kRowLanes;
 
+// The larger and the smaller of two (without the rounds that fmaxf and fminf make for signalling NaNs: a quarter of an append's instructions).
+__device__ __forceinline__ float larger(float a, float b)
+{
+    float r;
+    asm("v_max_f32 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+    return r;
+}
+__device__ __forceinline__ float smaller(float a, float b)
+{
+    float r;
+    asm("v_min_f32 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+    return r;
+}
+__device__ __forceinline__ float larger_size(float a, float x) // of a, which is not negative, and the magnitude of x
+{
+    float r;
+    asm("v_max_f32 %0, %1, |%2|" : "=v"(r) : "v"(a), "v"(x));
+    return r;
+}
+
 // largest of 2, 4, 8 or 16 neighbouring lanes, in all of them, by lane moves (no LDS)
 template <int N>
 __device__ __forceinline__ float lanes_max(float x)
 {
-    auto with = [](float v, int moved) __attribute__((always_inline)) { return fmaxf(v, __int_as_float(moved)); };
+    auto with = [](float v, int moved) __attribute__((always_inline)) { return larger(v, __int_as_float(moved)); };
     x = with(x, __builtin_amdgcn_update_dpp(0, __float_as_int(x), 0xb1, 0xf, 0xf, true));                         // lanes 1 0 3 2
     if constexpr (N >= 4) x = with(x, __builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x4e, 0xf, 0xf, true));   // 2 3 0 1
     if constexpr (N >= 8) x = with(x, __builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x141, 0xf, 0xf, true));  // 7 6 .. 0
     if constexpr (N >= 16) x = with(x, __builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x140, 0xf, 0xf, true)); // 15 14 .. 0
     return x;
+}
+// F(x of lanes l, l ^ 16, l ^ 32 and l ^ 48)
+template <typename F>
+__device__ __forceinline__ float over_quarters(float x, F both)
+{
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = both(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    const auto q = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return both(__uint_as_float(q[0]), __uint_as_float(q[1]));
 }
 __device__ __forceinline__ float quarter_max(float x) { return lanes_max<kRowLanes>(x); }
 
@@ -120,7 +149,7 @@ __device__ __forceinline__ float encode(const float (&x)[E], char (&codes)[kv_pa
     if constexpr (S == PK_F4) {
         float most = 0.f;
 #pragma unroll
-        for (int i = 0; i < E; ++i) most = fmaxf(most, fabsf(x[i]));
+        for (int i = 0; i < E; ++i) most = larger_size(most, x[i]);
         const float group = lanes_max<32 / E>(most); // of 32 channels
         most = quarter_max(most);
         const float up = code_factor(most, kv_largest<S>);
@@ -150,7 +179,7 @@ __device__ __forceinline__ float encode(const float (&x)[E], char (&codes)[kv_pa
     } else if constexpr (kv_coded<S>) {
         float most = 0.f;
 #pragma unroll
-        for (int i = 0; i < E; ++i) most = fmaxf(most, fabsf(x[i]));
+        for (int i = 0; i < E; ++i) most = larger_size(most, x[i]);
         most = quarter_max(most);
         const float up = code_factor(most, kv_largest<S>);
 #pragma unroll
@@ -224,8 +253,8 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(KvDev c, KvBatch b,
                 z = decode<S, false>(codes, i);
             }
             if constexpr (kv_coded<S>) z *= scale;
-            hi[i] = fmaxf(hi[i], z);
-            lo[i] = fminf(lo[i], z);
+            hi[i] = larger(hi[i], z);
+            lo[i] = smaller(lo[i], z);
         }
     };
     // rows that were there, several asked for at once
@@ -277,10 +306,8 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(KvDev c, KvBatch b,
     }
 #pragma unroll
     for (int i = 0; i < E; ++i) {
-        hi[i] = fmaxf(hi[i], __shfl_xor(hi[i], 16));
-        lo[i] = fminf(lo[i], __shfl_xor(lo[i], 16));
-        hi[i] = fmaxf(hi[i], __shfl_xor(hi[i], 32));
-        lo[i] = fminf(lo[i], __shfl_xor(lo[i], 32));
+        hi[i] = over_quarters(hi[i], larger);
+        lo[i] = over_quarters(lo[i], smaller);
         if ((tid & 63) < kRowLanes) {
             red[tid >> 6][0][at + i] = hi[i];
             red[tid >> 6][1][at + i] = lo[i];
@@ -293,10 +320,10 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(KvDev c, KvBatch b,
         for (int i = 0; i < E; ++i) {
 #pragma unroll
             for (int w = 1; w < 4; ++w) {
-                hi[i] = fmaxf(hi[i], red[w][0][at + i]);
-                lo[i] = fminf(lo[i], red[w][1][at + i]);
+                hi[i] = larger(hi[i], red[w][0][at + i]);
+                lo[i] = smaller(lo[i], red[w][1][at + i]);
             }
-            most = fmaxf(most, fmaxf(fabsf(hi[i]), fabsf(lo[i])));
+            most = larger_size(larger_size(most, hi[i]), lo[i]);
         }
         most = quarter_max(most);
         const float up = code_factor(most, 127.f);

@@ -1301,14 +1301,19 @@ __global__ __launch_bounds__(NW * 64) void kv_tile_kernel(KvAttend a)
     }
     const size_t oh = (size_t)tok * c.H * G + h * G + member;
     const float inv = l > 0.f ? back / l : 0.f;
+    // a lane and the one 32 beyond hold four channels each of two runs of eight: exchanged, each writes a run
 #pragma unroll
     for (int d = 0; d < DT; ++d)
 #pragma unroll
-        for (int b = 0; b < 4; ++b) {
-            const int dd = d * 32 + b * 8 + hf * 4;
-            if (dd < c.D)
-                *reinterpret_cast<u32x2 *>(a.out + (oh * c.D + dd) * 2) =
-                    u32x2{pack16<T>(o[d][4 * b] * inv, o[d][4 * b + 1] * inv), pack16<T>(o[d][4 * b + 2] * inv, o[d][4 * b + 3] * inv)};
+        for (int b = 0; b < 4; b += 2) {
+            uint32_t w[2][2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) w[i][e] = pack16<T>(o[d][4 * (b + i) + 2 * e] * inv, o[d][4 * (b + i) + 2 * e + 1] * inv);
+            const auto x = __builtin_amdgcn_permlane32_swap(w[0][0], w[1][0], false, false), y = __builtin_amdgcn_permlane32_swap(w[0][1], w[1][1], false, false);
+            const int dd = d * 32 + (b + hf) * 8;
+            if (dd < c.D) *reinterpret_cast<u32x4 *>(a.out + (oh * c.D + dd) * 2) = u32x4{x[0], y[0], x[1], y[1]};
         }
     if (hf == 0 && a.lse) a.lse[oh] = l > 0.f ? (m * qscale + score_offset(a) + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
 }

@@ -21,7 +21,7 @@ struct KvPool {
     int32_t *list;          // [n_pages] free pages that a call hands out
     uint32_t *bits;         // [n_words] free pages, 32 a word (beyond n_pages: 0)
     int32_t *rank;          // [n_words] of a call: pages in use before a word's
-    int32_t *base, *copy_to, *copy_from; // [PK_KV_MAX_SEQS] of a call: pages that the sequences before need; the page copied for a sequence, or -1
+    int32_t *base, *copy_to, *copy_from; // [PK_KV_MAX_SEQS] of a call: entries of the sequences before; the page copied for a sequence, or -1
 };
 
 // The regions of an arena, bytes of a page each.
@@ -150,154 +150,193 @@ __device__ __forceinline__ int scan(int v, int *sums, int &total)
     return before + upto - v;
 }
 
-// Pages for a batch's new tokens, by one workgroup; a sequence has W lanes, a lane an entry of its table at a time.
+// All of the workgroup's writes and atomics are done, for all of its waves: the barrier does not wait for them, each wave waits for its own.  (All are of one
+// CU, whose cache they share: no fence, which would write back an L2.)
+__device__ __forceinline__ void all_done()
+{
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+}
+
+// Entries of a sequence's table that a call's tokens go into.
+struct KvEntries {
+    int begin, first, count; // the first new position; the first entry, and how many
+};
+__device__ __forceinline__ KvEntries kv_entries(const KvBatch &b, int s, int P, int logP)
+{
+    const KvSeq q = kv_seq(b, s, P);
+    const int begin = max(q.len - q.m, 0), first = begin >> logP;
+    return KvEntries{begin, first, q.m > 0 && q.len > 0 ? ((q.len - 1) >> logP) - first + 1 : 0};
+}
+
+// The lowest free pages, `need` of them, into list[0 ..), and out of the free ones; how many there are (more than needed may be counted).  1024 words a step, each thread
+// one, so that the pages of neighbouring words are listed by as many threads; four steps' words are asked for at once.
+struct KvFree {
+    uint32_t word[4];
+    __device__ __forceinline__ void ask(const KvPool &p, uint32_t w0)
+    {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t w = w0 + k * kGrantThreads + threadIdx.x;
+            word[k] = w < p.n_words ? p.bits[w] : 0;
+        }
+    }
+};
+__device__ __forceinline__ int take_free(const KvPool &p, KvFree &f, int need, int32_t *list, int *sums) // (f: asked for from word 0 on)
+{
+    int have = 0;
+    for (uint32_t w0 = 0;;) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (have >= need) return have;
+            uint32_t w = f.word[k];
+            const uint32_t mine = w0 + k * kGrantThreads + threadIdx.x;
+            int total, at = have + scan(__popc(w), sums, total);
+            while (w && at < need) {
+                list[at++] = (int32_t)(mine * 32 + __ffs(w) - 1);
+                w &= w - 1;
+            }
+            if (w != f.word[k]) p.bits[mine] = w;
+            have += total;
+        }
+        w0 += kGrantThreads * 4;
+        if (w0 >= p.n_words) return have;
+        f.ask(p, w0);
+    }
+}
+
+// Pages for a batch's new tokens, by one workgroup, 1024 entries at a time, in the order of sequences and positions:
 //   1  entries that hold a page of several owners are counted, and the last sequence with each is noted
-//   2  what an entry needs is decided and written in its place (-1: a page; -2 - page: a page instead of that one), needs are summed over the sequences
+//   2  what an entry needs is decided and written in its place (-1: a page; -2 - page: a page instead of that one)
 //   3  the lowest free pages, as many as are needed
 //   4  entries get theirs by rank; counts, and the list of pages to be copied, which the next launch does
-// Everything fits the caches: the time is that of four chains of dependent loads, for every 1024 / W sequences (and W entries).
-__global__ __launch_bounds__(kGrantThreads) void kv_grant_kernel(KvPool p, KvBatch b, int P, int logP, int W, int32_t *missing)
+// Everything fits the caches: the time is that of the chains of dependent loads, to which an entry's sequence, found among those before it, adds.
+// Measured (with the launch behind it): a prompt of 4096 tokens among 255 decoding sequences 15.1 us, 64 prompts of 8192 69, one of 131072 41.  By sequences, some lanes
+// each, with free pages listed by who has their words and fences between the phases: 78, 139, 100.
+__global__ __launch_bounds__(kGrantThreads) void kv_grant_kernel(KvPool p, KvBatch b, int P, int logP, int32_t *missing)
 {
     __shared__ int sums[kGrantThreads / 64];
     __shared__ int lost; // pages that are not there and would have to hold older tokens
-    const int tid = threadIdx.x, groups = kGrantThreads / W, in = tid & (W - 1), group = tid / W;
-    const int shift = (tid & 63) & ~(W - 1);
-    const unsigned long long mine = (W == 64 ? ~0ull : (1ull << W) - 1) << shift, below = mine & ((1ull << (tid & 63)) - 1);
-    int32_t *tables = const_cast<int32_t *>(b.tables);
+    const int tid = threadIdx.x;
     if (tid == 0) lost = 0;
-    __syncthreads();
+    int entries = 0;
+    for (int s0 = 0; s0 < b.n_seqs; s0 += kGrantThreads) {
+        const int s = s0 + tid, n = s < b.n_seqs ? kv_entries(b, s, P, logP).count : 0;
+        int total;
+        const int before = scan(n, sums, total);
+        if (s < b.n_seqs) {
+            p.base[s] = entries + before;
+            p.copy_to[s] = -1;
+        }
+        entries += total;
+    }
+    all_done();
 
-    // entries lp0 .. lp1 of a sequence are those that the call's tokens go into; `begin`: the first new position
-    struct Part {
-        int32_t *row;
-        int begin, lp0, lp1;
+    struct Entry {
+        int s;
+        int32_t *at;
+        bool older; // its page has tokens from before the call
     };
-    auto part = [&](int s) __attribute__((always_inline)) {
-        Part r{nullptr, 0, 0, -1};
-        if (s >= b.n_seqs) return r;
-        const KvSeq q = kv_seq(b, s, P);
-        r.row = tables + (size_t)s * b.table_stride;
-        r.begin = max(q.len - q.m, 0);
-        if (q.m > 0 && q.len > 0) r.lp0 = r.begin >> logP, r.lp1 = (q.len - 1) >> logP;
-        return r;
+    auto entry_of = [&](int e) __attribute__((always_inline)) {
+        int lo = 0, hi = b.n_seqs - 1; // the last sequence whose entries do not begin beyond e: one that has some
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (p.base[mid] <= e) lo = mid;
+            else hi = mid - 1;
+        }
+        const KvEntries k = kv_entries(b, lo, P, logP);
+        const int j = k.first + (e - p.base[lo]);
+        return Entry{lo, const_cast<int32_t *>(b.tables) + (size_t)lo * b.table_stride + j, k.begin > (int64_t)j << logP};
     };
 
-    for (int s = group; s < b.n_seqs; s += groups) {
-        const Part r = part(s);
-        for (int j = r.lp0 + in; j <= r.lp1; j += W) {
-            const uint32_t page = (uint32_t)r.row[j];
-            if (page < p.n_pages && p.refs[page] > 1) {
-                atomicAdd(&p.users[page], 1);
-                atomicMax(&p.last[page], s + 1);
-            }
+    for (int e = tid; e < entries; e += kGrantThreads) {
+        const Entry x = entry_of(e);
+        const uint32_t page = (uint32_t)*x.at;
+        if (page < p.n_pages && p.refs[page] > 1) {
+            atomicAdd(&p.users[page], 1);
+            atomicMax(&p.last[page], x.s + 1);
         }
     }
-    __threadfence();
-    __syncthreads();
+    all_done();
 
     int need = 0;
-    for (int s0 = 0; s0 < b.n_seqs; s0 += groups) {
-        const int s = s0 + group;
-        const Part r = part(s);
-        int n = 0;
-        for (int j = r.lp0 + in; j - in <= r.lp1; j += W) { // (all lanes of a group in step)
-            bool wants = false;
-            if (j <= r.lp1) {
-                const uint32_t page = (uint32_t)r.row[j];
-                const bool there = page < p.n_pages;
-                if (there) {
-                    // (written by other waves: read where their atomics wrote)
-                    const int refs = p.refs[page], users = __hip_atomic_load(&p.users[page], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT),
-                              last = __hip_atomic_load(&p.last[page], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                    wants = refs > 1 && (users < refs || last != s + 1);
-                    if (wants) r.row[j] = -2 - (int32_t)page;
-                } else {
-                    wants = r.begin <= j << logP;
-                    if (!wants) atomicAdd(&lost, 1);
-                    r.row[j] = -1;
-                }
+    for (int e0 = 0; e0 < entries; e0 += kGrantThreads) {
+        bool wants = false;
+        if (e0 + tid < entries) {
+            const Entry x = entry_of(e0 + tid);
+            const uint32_t page = (uint32_t)*x.at;
+            if (page < p.n_pages) {
+                // (written by other waves: read where their atomics wrote)
+                const int refs = p.refs[page], users = __hip_atomic_load(&p.users[page], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT),
+                          last = __hip_atomic_load(&p.last[page], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                wants = refs > 1 && (users < refs || last != x.s + 1);
+                if (wants) *x.at = -2 - (int32_t)page;
+            } else {
+                wants = !x.older;
+                if (!wants) atomicAdd(&lost, 1);
+                *x.at = -1;
             }
-            n += __popcll(__ballot(wants) & mine);
         }
         int total;
-        const int before = scan(in == 0 ? n : 0, sums, total);
-        if (in == 0 && s < b.n_seqs) p.base[s] = need + before;
+        scan(wants ? 1 : 0, sums, total);
         need += total;
     }
 
-    int have = 0;
-    for (uint32_t w0 = 0; w0 < p.n_words && have < need; w0 += kGrantThreads * 4) {
-        uint32_t word[4];
-        int n = 0;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            word[k] = w0 + tid * 4 + k < p.n_words ? p.bits[w0 + tid * 4 + k] : 0;
-            n += __popc(word[k]);
-        }
-        int total, at = have + scan(n, sums, total);
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-            for (uint32_t w = word[k]; w && at < need; w &= w - 1) p.list[at++] = (int32_t)((w0 + tid * 4 + k) * 32 + __ffs(w) - 1);
-        have += total;
-    }
-    __threadfence();
-    __syncthreads();
+    KvFree free;
+    free.ask(p, 0);
+    const int have = take_free(p, free, need, p.list, sums);
+    all_done();
 
-    for (int s = group; s < b.n_seqs; s += groups) {
-        const Part r = part(s);
-        int at = p.base[s];
-        if (in == 0) p.copy_to[s] = -1;
-        for (int j = r.lp0 + in; j - in <= r.lp1; j += W) {
-            const bool inside = j <= r.lp1;
-            const int32_t entry = inside ? r.row[j] : 0;
-            const bool older = r.begin > j << logP; // the page has tokens from before the call
-            const bool wants = inside && (entry < -1 || (entry == -1 && !older));
-            const unsigned long long all = __ballot(wants) & mine;
-            const int rank = at + __popcll(all & below);
-            at += __popcll(all);
-            if (!inside) continue;
-            const int32_t old = entry < -1 ? -2 - entry : entry;
-            if (old >= 0) p.users[old] = p.last[old] = 0;
-            if (!wants) continue;
-            const int32_t page = rank < have ? p.list[rank] : -1;
-            r.row[j] = page;
-            if (entry < -1) atomicSub(&p.refs[old], 1); // (it keeps one owner at least)
-            if (page < 0) continue;
-            p.refs[page] = 1;
-            atomicAnd(&p.bits[page >> 5], ~(1u << (page & 31)));
-            if (entry < -1 && older) {
-                p.copy_from[s] = old;
-                p.copy_to[s] = page;
-            }
+    int given = 0;
+    for (int e0 = 0; e0 < entries; e0 += kGrantThreads) {
+        const bool inside = e0 + tid < entries;
+        Entry x{};
+        int32_t entry = 0;
+        if (inside) {
+            x = entry_of(e0 + tid);
+            entry = *x.at; // (as this thread left it)
+        }
+        const bool wants = inside && (entry < -1 || (entry == -1 && !x.older));
+        int total;
+        const int rank = given + scan(wants ? 1 : 0, sums, total);
+        given += total;
+        if (!inside) continue;
+        const int32_t old = entry < -1 ? -2 - entry : entry;
+        if (old >= 0) p.users[old] = p.last[old] = 0;
+        if (!wants) continue;
+        const int32_t page = rank < have ? p.list[rank] : -1;
+        *x.at = page;
+        if (entry < -1) atomicSub(&p.refs[old], 1); // (it keeps one owner at least)
+        if (page < 0) continue;
+        p.refs[page] = 1;
+        if (entry < -1 && x.older) { // (a sequence's first entry alone)
+            p.copy_from[x.s] = old;
+            p.copy_to[x.s] = page;
         }
     }
     if (tid == 0 && missing) *missing = max(need - have, 0) + lost;
 }
 
 // The same where every entry has a thread of its own (a decoding step): entries, owners and what is decided stay in registers, the first free pages
-// (of 131072) are asked for at the start, and their list lies in LDS.  Measured: 256 branches, all of a shared page, 9.7 us (as above 18.0); four of one sequence 5.7 (13.4).
+// (of 131072) are asked for at the start, and their list lies in LDS.  Measured: 256 branches, four of each shared page, 7.1 us; four of one sequence 4 - 5.
 __global__ __launch_bounds__(kGrantThreads) void kv_grant_once_kernel(KvPool p, KvBatch b, int P, int logP, int W, int32_t *missing)
 {
     __shared__ int sums[kGrantThreads / 64];
     __shared__ int32_t list[kGrantThreads];
     __shared__ int lost;
     const int tid = threadIdx.x, in = tid & (W - 1), s = tid / W;
-    uint32_t word[4];
-    auto words = [&](uint32_t w0) __attribute__((always_inline)) {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) word[k] = w0 + tid * 4 + k < p.n_words ? p.bits[w0 + tid * 4 + k] : 0;
-    };
-    words(0);
+    KvFree free;
+    free.ask(p, 0);
     if (tid == 0) lost = 0;
     int32_t *entry = nullptr;
     uint32_t page = 0;
     bool inside = false, older = false;
     int refs = 0;
     if (s < b.n_seqs) {
-        const KvSeq q = kv_seq(b, s, P);
-        const int begin = max(q.len - q.m, 0), j = (begin >> logP) + in;
-        inside = q.m > 0 && q.len > 0 && j <= (q.len - 1) >> logP;
-        older = begin > (int64_t)j << logP; // the page has tokens from before the call
+        const KvEntries k = kv_entries(b, s, P, logP);
+        const int j = k.first + in;
+        inside = in < k.count;
+        older = k.begin > (int64_t)j << logP; // the page has tokens from before the call
         if (inside) {
             entry = const_cast<int32_t *>(b.tables) + (size_t)s * b.table_stride + j;
             page = (uint32_t)*entry;
@@ -312,8 +351,7 @@ __global__ __launch_bounds__(kGrantThreads) void kv_grant_once_kernel(KvPool p, 
     }
     const bool there = inside && page < p.n_pages, shared = there && refs > 1;
     bool wants = inside && !there && !older;
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); // (the barrier does not wait for atomics: each wave waits for its own)
-    __syncthreads();
+    all_done();
     if (inside && !there && older) atomicAdd(&lost, 1);
     if (shared) {
         // (where the other waves' atomics wrote, not in this CU's cache)
@@ -324,29 +362,13 @@ __global__ __launch_bounds__(kGrantThreads) void kv_grant_once_kernel(KvPool p, 
     const int rank = scan(wants ? 1 : 0, sums, need);
     if (shared) p.users[page] = p.last[page] = 0; // (all have read them: the scan is past)
 
-    int have = 0;
-    for (uint32_t w0 = 0;;) {
-        int n = 0;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) n += __popc(word[k]);
-        int total, at = have + scan(n, sums, total);
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-            for (uint32_t w = word[k]; w && at < need; w &= w - 1) list[at++] = (int32_t)((w0 + tid * 4 + k) * 32 + __ffs(w) - 1);
-        have += total;
-        w0 += kGrantThreads * 4;
-        if (have >= need || w0 >= p.n_words) break;
-        words(w0);
-    }
+    const int have = take_free(p, free, need, list, sums);
     __syncthreads();
     if (wants || (inside && !there)) {
         const int32_t mine = wants && rank < have ? list[rank] : -1;
         *entry = mine;
         if (shared) atomicSub(&p.refs[page], 1); // (it keeps one owner at least)
-        if (mine >= 0) {
-            p.refs[mine] = 1;
-            atomicAnd(&p.bits[mine >> 5], ~(1u << (mine & 31)));
-        }
+        if (mine >= 0) p.refs[mine] = 1;
         if (shared && older && mine >= 0) p.copy_from[s] = (int32_t)page;
         if (in == 0) p.copy_to[s] = shared && older ? mine : -1; // (older tokens lie in a sequence's first entry alone)
     } else if (in == 0 && s < b.n_seqs) p.copy_to[s] = -1;
@@ -593,7 +615,7 @@ int pk_kv_pool_grant(pk_kv_pool *pool, const pk_kv_batch *batch, int32_t *missin
     int W = 1;
     while (W < 64 && W < entries) W *= 2;
     if (entries <= W && (int64_t)b.n_seqs * W <= kGrantThreads) kv_grant_once_kernel<<<1, kGrantThreads, 0, s>>>(pool->dev, b, pool->kv.dev.P, pool->kv.dev.logP, W, missing);
-    else kv_grant_kernel<<<1, kGrantThreads, 0, s>>>(pool->dev, b, pool->kv.dev.P, pool->kv.dev.logP, W, missing);
+    else kv_grant_kernel<<<1, kGrantThreads, 0, s>>>(pool->dev, b, pool->kv.dev.P, pool->kv.dev.logP, missing);
     if (!none) {
         const KvMove m = move_between(pool->kv, pool->kv);
         kv_granted_copy_kernel<<<dim3(b.n_seqs, pieces_of(m, b.n_seqs, pool->kv.num_cu)), kThreads, 0, s>>>(pool->dev, m);
