@@ -432,9 +432,9 @@ int pk_index_free(pk_index *index);
  *   PK_F16, PK_BF16  rounded once to nearest even
  *   PK_I8            scale = max|x| * (1/127), codes rint(x * (127 / max|x|)); a row of zeros has scale 0
  *   PK_F8            scale = max|x| * (1/448), codes x * (448 / max|x|) rounded to nearest even e4m3
- *   PK_F4            scale = max|x| * (1/6), codes x * (6 / max|x|) rounded to nearest even e2m1 (0, 1/2, 1, 3/2, 2, 3, 4, 6); of a key
- *                    each 32 channels are first multiplied by 2^e and their codes stand for 2^-e of themselves: e the whole number by which
- *                    the exponent of their largest magnitude, its fraction with it, is below that of the row's, 15 at most
+ *   PK_F4            scale = max|x| * (1/6), codes x * (6 / max|x|) rounded to nearest even e2m1 (0, 1/2, 1, 3/2, 2, 3, 4, 6); each 32 channels
+ *                    of a key are first multiplied by 2^e, and their codes stand for 2^-e of themselves: e the largest whole number up to 15 for which 2^e
+ *                    times their largest magnitude is no more than max|x| (of rows below 2^-111: by the numbers' exponent fields)
  * all in 32 bits, so that a row's stored value depends on the row alone.  The bounds of a page (and head) are for every channel the
  * largest and the smallest stored value of the keys in it, as int8 codes hi = ceil(max * 127 / a - 2^-10),
  * lo = floor(min * 127 / a + 2^-10) with a = the largest magnitude among them, and the scale a * (1/127).
@@ -602,7 +602,7 @@ int pk_kv_pool_adopt(pk_kv_pool *pool, const pk_kv_tables *tables, void *stream)
  *   no page there          the lowest free one, in the order of sequences and positions
  *   a page of others too   the same instead of it; what it holds is copied where tokens from before the call are in it.  If all that
  *                          have the page write into it in this call, the last of them keeps it.
- * Where none is left the entry becomes -1 (and what is appended there is left out); a page that is not there and would have to hold tokens from before the
+ * Where none is left the entry becomes -1 (a page of others that it held is given up, and what is appended there is left out); a page that is not there and would have to hold tokens from before the
  * call stays away too.
  *   missing  DEVICE [1] int32 or NULL: the number of such entries
  */
@@ -613,7 +613,7 @@ int pk_kv_pool_grant(pk_kv_pool *pool, const pk_kv_batch *batch, int32_t *missin
 int pk_kv_pool_fork(pk_kv_pool *pool, const pk_kv_tables *tables, const int32_t *lens, const int32_t *from, const int32_t *to, int32_t n, void *stream);
 
 /* Row rows[i] keeps the pages of its first keep[i] tokens (keep NULL: none); the other entries become -1, and pages that nobody has any more
- * are free.  rows, keep DEVICE [n].  Rows that the tables have not are left out. */
+ * are free.  rows, keep DEVICE [n]; a row that is listed twice keeps what the lesser leaves.  Rows that the tables have not are left out. */
 int pk_kv_pool_release(pk_kv_pool *pool, const pk_kv_tables *tables, const int32_t *rows, const int32_t *keep, int32_t n, void *stream);
 
 /*

@@ -728,7 +728,8 @@ class KVPool:
         with torch.cuda.device(cache.arena.device):
             self.handle = pk_kv_pool_create(cache.handle, self.memory)
 
-    def _here(self, **tensors):
+    def _check(self, **tensors):
+        """The cache is open, and everything on its device."""
         if self.cache.handle is None:
             raise ValueError("the pool's cache is closed")
         for what, t in tensors.items():
@@ -737,50 +738,50 @@ class KVPool:
 
     def clear(self):
         """All pages are free."""
-        self._here()
+        self._check()
         pk_kv_pool_clear(self.handle, self.device)
 
     def adopt(self, tables):
         """Counts the pages of tables that were filled without the pool."""
-        self._here(tables=tables)
+        self._check(tables=tables)
         pk_kv_pool_adopt(self.handle, tables)
 
     def grant(self, batch):
         """Pages of their own for the batch's new tokens, shared ones copied first; batch.tables is changed.  Returns the number of entries that got none, an int32 tensor [1]."""
-        self._here()
+        self._check()
         if batch.device != self.device:
             raise ValueError(f"the batch is on device {batch.device}, the pool on {self.memory.device}")
-        missing = torch.empty(1, dtype=torch.int32, device=self.memory.device)
+        missing = batch.lens.new_empty(1)
         pk_kv_pool_grant(self.handle, batch.c, missing, self.device)
         return missing
 
     def fork(self, tables, lens, sources, targets):
         """Rows `targets` of the tables get the pages of rows `sources` (of lens tokens, by row of the tables)."""
-        self._here(tables=tables, lens=lens, sources=sources, targets=targets)
+        self._check(tables=tables, lens=lens, sources=sources, targets=targets)
         if lens.shape != (tables.shape[0],) or sources.dim() != 1 or sources.shape != targets.shape:
             raise ValueError("a fork has lens for every row of the tables, and as many sources as targets")
         pk_kv_pool_fork(self.handle, tables, lens, sources, targets)
 
     def release(self, tables, rows, keep=None):
         """Rows of the tables keep the pages of their first `keep` tokens (none where it is left out) and give up the others."""
-        self._here(tables=tables, rows=rows, keep=keep)
+        self._check(tables=tables, rows=rows, keep=keep)
         if rows.dim() != 1 or (keep is not None and keep.shape != rows.shape):
             raise ValueError("a release has a list of rows, and as many numbers of tokens to keep")
         pk_kv_pool_release(self.handle, tables, rows, keep)
 
     def compact(self, into, tables):
         """Moves the pages in use into the cache of another pool, side by side.  Returns the tables' new entries, and the number of pages that had no room, an int32 tensor [1]."""
-        self._here(tables=tables)
-        into._here()
+        self._check(tables=tables)
+        into._check()
         if into.device != self.device:
             raise ValueError(f"the other pool is on {into.memory.device}, this one on {self.memory.device}")
-        out, missing = torch.empty(tables.shape, dtype=torch.int32, device=tables.device), torch.empty(1, dtype=torch.int32, device=tables.device)
+        out, missing = tables.new_empty(tables.shape), tables.new_empty(1)
         pk_kv_pool_compact(self.handle, into.handle, tables, out, missing)
         return out, missing
 
     def counts(self):
         """Owners of every page, int32 [page]: 0 for a free one."""
-        self._here()
+        self._check()
         counts = torch.empty(self.cache.cfg.n_pages, dtype=torch.int32, device=self.memory.device)
         pk_kv_pool_counts(self.handle, counts)
         return counts

@@ -318,7 +318,7 @@ __global__ __launch_bounds__(kGrantThreads) void kv_grant_kernel(KvPool p, KvBat
 }
 
 // The same where every entry has a thread of its own (a decoding step): entries, owners and what is decided stay in registers, the first free pages
-// (of 131072) are asked for at the start, and their list lies in LDS.  Measured: 256 branches, four of each shared page, 7.1 us; four of one sequence 4 - 5.
+// (of 131072) are asked for at the start, and their list lies in LDS.  Measured: 256 branches, four of each shared page, 7.1 us; four of one sequence 5.7 (13.4).
 __global__ __launch_bounds__(kGrantThreads) void kv_grant_once_kernel(KvPool p, KvBatch b, int P, int logP, int W, int32_t *missing)
 {
     __shared__ int sums[kGrantThreads / 64];
