@@ -4,6 +4,7 @@
 #pragma once
 
 #include <algorithm>
+#include <cmath>
 
 #include "pk_kv.h"
 
@@ -1348,11 +1349,15 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttend a)
 // Parts that the keys are cut into (`tiles` tiles of 64 at most): so many that there are `wgs` workgroups, each with `least` tiles at least;
 // more of them, up to `more_wgs`, where each has `much` tiles, as sequences' lengths differ.  Within the room for partial results.  A window does
 // not enter: parts that lie outside it end at once and are joined as parts without a key (one token, window 4096 of 131072: 25 us).
+// A row's parts are joined one after the other, eight on their way, 0.13 us each, so that few long sequences of few heads are better off with fewer parts than
+// there are places: of T tiles 40 or 1.2 sqrt(T).  One token, us, so (and without): one head over 131072 keys, 4 bits 26 (77), bf16 28 (86); over 10^6 59 (94), 118 (173); two
+// heads over 32768 18 (25), 22 (35); 8 heads over 131072 37 (36), 108 (109).
 void cut(KvAttend &a, int64_t items, int64_t tiles, int rows, int64_t wgs, int least, int64_t more_wgs, int much)
 {
     const int64_t room = a.part_floats / ((int64_t)rows * a.part_row) / std::max<int64_t>(items, 1);
     const int64_t want = std::max(std::min((wgs + items - 1) / items, tiles / least), std::min((more_wgs + items - 1) / items, tiles / much));
-    const int64_t n = std::max<int64_t>(std::min(want, room), 1);
+    const int64_t most = std::max<int64_t>(40, (int64_t)(1.2 * std::sqrt((double)tiles)));
+    const int64_t n = std::max<int64_t>(std::min({want, room, most}), 1);
     a.split_tiles = (int32_t)((tiles + n - 1) / n);
     a.n_split = (int32_t)((tiles + a.split_tiles - 1) / a.split_tiles);
 }
