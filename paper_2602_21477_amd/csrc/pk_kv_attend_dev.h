@@ -133,6 +133,16 @@ __device__ __forceinline__ float max3(float a, float b, float c)
     return r;
 }
 
+// The largest of a number's values in 16 neighbouring lanes.
+__device__ __forceinline__ float over_row_max(float v)
+{
+    auto with = [](float x, int moved) __attribute__((always_inline)) { return fmaxf(x, __int_as_float(moved)); };
+    v = with(v, __builtin_amdgcn_update_dpp(0, __float_as_int(v), 0xb1, 0xf, 0xf, true));  // lanes 1 0 3 2
+    v = with(v, __builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x4e, 0xf, 0xf, true));  // 2 3 0 1
+    v = with(v, __builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x141, 0xf, 0xf, true)); // 7 6 .. 0
+    return with(v, __builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x140, 0xf, 0xf, true)); // 15 14 .. 0
+}
+
 // A number that all lanes of a wave have.
 __device__ __forceinline__ int same(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
@@ -244,14 +254,16 @@ __device__ __forceinline__ void kv_join_parts(const KvAttend &a, size_t first, i
     m = -INFINITY, l = 0.f;
 #pragma unroll
     for (int d = 0; d < DP / 64; ++d) y[d] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < n; s += AT_ONCE) {
+    // the row's threads look at a sixteenth of the maxima each
+    for (int s = 0; s < n; s += AT_ONCE * 16) {
         float x[AT_ONCE];
 #pragma unroll
-        for (int k = 0; k < AT_ONCE; ++k) x[k] = a.part_ml[((first + min(s + k, n - 1)) * BR + r) * 2];
+        for (int k = 0; k < AT_ONCE; ++k) x[k] = a.part_ml[((first + min(s + k * 16 + sub, n - 1)) * BR + r) * 2];
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int k = 0; k < AT_ONCE; ++k) m = fmaxf(m, x[k]);
     }
+    m = over_row_max(m);
     const float base = m == -INFINITY ? 0.f : m;
     for (int s = 0; s < n; s += AT_ONCE) {
         f32x2 ml[AT_ONCE];
@@ -795,11 +807,7 @@ __device__ __forceinline__ void reads_ahead()
 // The largest of a number's values in a wave.
 __device__ __forceinline__ float over_wave_max(float v)
 {
-    auto with = [](float x, int moved) __attribute__((always_inline)) { return fmaxf(x, __int_as_float(moved)); };
-    v = with(v, __builtin_amdgcn_update_dpp(0, __float_as_int(v), 0xb1, 0xf, 0xf, true));  // lanes 1 0 3 2
-    v = with(v, __builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x4e, 0xf, 0xf, true));  // 2 3 0 1
-    v = with(v, __builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x141, 0xf, 0xf, true)); // 7 6 .. 0
-    v = with(v, __builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x140, 0xf, 0xf, true)); // 15 14 .. 0
+    v = over_row_max(v);
     const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     return over_halves_max(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
 }
