@@ -245,7 +245,8 @@ __device__ __forceinline__ void kv_write_row(const KvAttend &a, int h, int tok, 
 }
 
 // The parts of row r of a tile of BR rows joined, from part `first` on and in order: their largest maximum, and sums and 4 channels in 64 in its
-// units.  Several at a time are asked for before any is used: one after the other they cost a latency each (64 parts of 8 heads: the join 12 us, else 40).
+// units.  Several at a time are asked for before any is used: one after the other they cost a latency each (64 parts of 8 heads: the join 12 us where
+// every thread looked at all the maxima, one by one 40; now 54 parts 8).
 template <int DP, int BR>
 __device__ __forceinline__ void kv_join_parts(const KvAttend &a, size_t first, int r, int sub, float qscale, float &m, float &l, f32x4 (&y)[DP / 64])
 {
@@ -1328,7 +1329,7 @@ __global__ __launch_bounds__(NW * 64) void kv_tile_kernel(KvAttend a)
 }
 
 // The parts of a row joined, in order: 16 threads a row.  Parts have BR rows; a workgroup joins 16 of them.  BR 16: the parts of the kernel
-// for few rows, else of the one for many.  5 - 12 us, a launch and a chain of loads: 48 sequences of 8 heads in 13 parts 7 us.
+// for few rows, else of the one for many.  4 - 8 us, a launch and a chain of loads: 48 sequences of 8 heads in 13 parts 7 us.
 template <int T, int DP, int BR, bool SPARSE>
 __global__ __launch_bounds__(256) void kv_join_kernel(KvAttend a)
 {
@@ -1358,8 +1359,8 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttend a)
 // more of them, up to `more_wgs`, where each has `much` tiles, as sequences' lengths differ.  Within the room for partial results.  A window does
 // not enter: parts that lie outside it end at once and are joined as parts without a key (one token, window 4096 of 131072: 25 us).
 // A row's parts are joined one after the other, eight on their way, 0.13 us each, so that few long sequences of few heads are better off with fewer parts than
-// there are places: of T tiles 40 or 1.2 sqrt(T).  One token, us, so (and without): one head over 131072 keys, 4 bits 26 (77), bf16 28 (86); over 10^6 59 (94), 118 (173); two
-// heads over 32768 18 (25), 22 (35); 8 heads over 131072 37 (36), 108 (109).
+// there are places: of T tiles 40 or 1.2 sqrt(T).  One token, us, so (and without): one head over 131072 keys, 4 bits 24 (51), bf16 26 (60); over 10^6 52 (67), 107 (136); two
+// heads over 32768 17 (20), 22 (30); 8 heads over 65536 25 (24), 57 (51), over 131072 35 (34), 104 (105).
 void cut(KvAttend &a, int64_t items, int64_t tiles, int rows, int64_t wgs, int least, int64_t more_wgs, int much)
 {
     const int64_t room = a.part_floats / ((int64_t)rows * a.part_row) / std::max<int64_t>(items, 1);
