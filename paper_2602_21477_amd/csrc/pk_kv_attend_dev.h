@@ -1359,13 +1359,13 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttend a)
 // more of them, up to `more_wgs`, where each has `much` tiles, as sequences' lengths differ.  Within the room for partial results.  A window does
 // not enter: parts that lie outside it end at once and are joined as parts without a key (one token, window 4096 of 131072: 25 us).
 // A row's parts are joined one after the other, eight on their way, 0.13 us each, so that few long sequences of few heads are better off with fewer parts than
-// there are places: of T tiles 40 or 1.2 sqrt(T).  One token, us, so (and without): one head over 131072 keys, 4 bits 24 (51), bf16 26 (60); over 10^6 52 (67), 107 (136); two
-// heads over 32768 17 (20), 22 (30); 8 heads over 65536 25 (24), 57 (51), over 131072 35 (34), 104 (105).
+// there are places: of T tiles 48 or 1.4 sqrt(T).  One token, us, so (and without): one head over 131072 keys, 4 bits 23 (50), bf16 25 (59); over 32768 14.5 (19), 14.4 (19); two
+// heads over 131072 24 (33), 31 (48); 4 heads over 65536 21 (23), 31 (39), over 200000 34 (34), 97 (89); 8 heads over 32768 18 (18), 32 (33), over 131072 34 (33), 104 (104).
 void cut(KvAttend &a, int64_t items, int64_t tiles, int rows, int64_t wgs, int least, int64_t more_wgs, int much)
 {
     const int64_t room = a.part_floats / ((int64_t)rows * a.part_row) / std::max<int64_t>(items, 1);
     const int64_t want = std::max(std::min((wgs + items - 1) / items, tiles / least), std::min((more_wgs + items - 1) / items, tiles / much));
-    const int64_t most = std::max<int64_t>(40, (int64_t)(1.2 * std::sqrt((double)tiles)));
+    const int64_t most = std::max<int64_t>(48, (int64_t)(1.4 * std::sqrt((double)tiles)));
     const int64_t n = std::max<int64_t>(std::min({want, room, most}), 1);
     a.split_tiles = (int32_t)((tiles + n - 1) / n);
     a.n_split = (int32_t)((tiles + a.split_tiles - 1) / a.split_tiles);
