@@ -828,6 +828,10 @@ struct KvTiles {
     static __device__ __forceinline__ int v_tok(int p) { return FOUR ? p / RB * 16 : p / DP * (128 / kv_bits<S>); }
     static constexpr int PG = ONE ? 1 : KP;
     static_assert(PIECES % NT == 0 || PIECES < NT, "");
+    // Whether a tile's pages are asked for ahead of the pieces of the one before it (fetch), not among them, where the compiler else has them.  Measured, first (among),
+    // us: bf16, 8 heads of 4, 4096 tokens over 32768 1990 (2040), 256 tokens behind a window of 4096 138 (148), 256 channels, 2048 over 8192 706 (720); codes no less: e4m3, 64
+    // channels, 16 sequences 1604 (1593), int8, 256 channels 796 (782), 4 bits 1140 (1133); capped, 64 channels, 2048 over 16384 553 (533), 128, 4096 over 32768 2330 (2350).
+    static constexpr bool PAGES_FIRST = !CODED && !(SCORED && DP == 64);
     struct Lds {
         u32x4 k[2][kKvTile * CH];
         u32x4 v[2][DP * 8];
@@ -880,6 +884,8 @@ struct KvTiles {
         }
     }
 
+    // NEXT: and the pages of tile j + 1, first.
+    template <bool NEXT>
     __device__ __forceinline__ void fetch(int j)
     {
         const int kb = first_of(j), vb = first_of(j - 1), tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
@@ -888,6 +894,10 @@ struct KvTiles {
             // (taken here, not where they were asked for: that would be a wait for all that is on its way)
             asm volatile("" : "+v"(kpage[0]), "+v"(vpage[0]));
             const uint32_t kp = (uint32_t)same((int)kpage[0]), vp = (uint32_t)same((int)vpage[0]);
+            if constexpr (NEXT) {
+                lookup(j + 1);
+                __builtin_amdgcn_sched_barrier(0);
+            }
             const char *kr = k + (place(kp) * P + (kb & (P - 1))) * RB, *vr = v + (place(vp) * P + (vb & (P - 1))) * RB;
             in_next = kp < n_pages ? 15u : 0u;
             if constexpr (CODED) { // (first: loads come back in their order, and the scales are wanted before the rest)
@@ -910,29 +920,38 @@ struct KvTiles {
             v_there = vp < n_pages;
             v_in = v_there ? ~0u : 0u;
         } else {
+            uint32_t kp[KP], vp[KP];
             v_in = 0;
 #pragma unroll
-            for (int i = 0; i < KP; ++i) asm volatile("" : "+v"(kpage[i]), "+v"(vpage[i]));
+            for (int i = 0; i < KP; ++i) {
+                asm volatile("" : "+v"(kpage[i]), "+v"(vpage[i]));
+                kp[i] = kpage[i], vp[i] = vpage[i];
+            }
             asm volatile("" : "+v"(spage));
+            const uint32_t sp = spage;
+            if constexpr (NEXT) {
+                lookup(j + 1);
+                __builtin_amdgcn_sched_barrier(0);
+            }
 #pragma unroll
             for (int i = 0; i < KP; ++i) {
                 const int p = tid + i * NT;
                 if (mine) {
                     // (a run of 16 tokens lies in one page)
                     constexpr int RUN = RB; // pieces of a run
-                    const size_t krun = place(kpage[i]) * P + ((kb + p / RUN * 16) & (P - 1)), vrun = place(vpage[i]) * P + ((vb + p / RUN * 16) & (P - 1));
+                    const size_t krun = place(kp[i]) * P + ((kb + p / RUN * 16) & (P - 1)), vrun = place(vp[i]) * P + ((vb + p / RUN * 16) & (P - 1));
                     kw[i] = *reinterpret_cast<const u32x4 *>(k + krun * RB + (p % RUN) * 16);
                     vw[i] = *reinterpret_cast<const u32x4 *>(v + vrun * RB + (p % RUN) * 16);
                     if constexpr (FOUR) kpow[i] = ke[krun * (DP / 32) + (uint32_t)e_place<DP>(k_tok(p) & 15, k_piece(p))];
                 }
-                v_in |= (vpage[i] < n_pages ? 1u : 0u) << i;
+                v_in |= (vp[i] < n_pages ? 1u : 0u) << i;
             }
-            const bool ok = spage < n_pages;
+            const bool ok = sp < n_pages;
             const unsigned long long b = __ballot(ok);
             in_next = (uint32_t)((b & 1) | (b >> 15 & 2) | (b >> 30 & 4) | (b >> 45 & 8));
             v_there = __all(v_in == (1u << KP) - 1);
             if constexpr (CODED) {
-                const size_t at = place(spage) * P + ((kb + lane) & (P - 1));
+                const size_t at = place(sp) * P + ((kb + lane) & (P - 1));
                 if (wave == 0) ksw = ks[at];
                 if (wave == 1) vsw = ok && kb + lane < len ? vs[at] : 0.f;
             }
@@ -1262,13 +1281,13 @@ __global__ __launch_bounds__(NW * 64) void kv_tile_kernel(KvAttend a)
 
     if (t0 < t1) {
         in.lookup(t0);
-        in.fetch(t0);
+        in.template fetch<false>(t0);
         in.lookup(t0 + 1);
         in.weigh();
         in.mask(t0);
         in.store(t0, lds);
         uint32_t held = in.in_next;
-        in.fetch(t0 + 1);
+        in.template fetch<false>(t0 + 1);
         in.lookup(t0 + 2);
         in.weigh();
         meet();
@@ -1278,8 +1297,8 @@ __global__ __launch_bounds__(NW * 64) void kv_tile_kernel(KvAttend a)
             in.mask(t + 1);
             in.store(t + 1, lds);
             const uint32_t held_next = in.in_next;
-            in.fetch(t + 2);
-            in.lookup(t + 3);
+            in.template fetch<in.PAGES_FIRST>(t + 2);
+            if constexpr (!in.PAGES_FIRST) in.lookup(t + 3);
             pv_products(t);
             qk_products(t);
             reads_ahead<4, 4 * DT, TWICE ? 2 : 1, 2 * KS>();
