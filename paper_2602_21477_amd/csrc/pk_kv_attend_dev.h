@@ -1046,8 +1046,9 @@ struct KvTiles {
 // 4.45 million cycles, of which the matrix cores are busy for 44 % and the reads of K and V out of LDS by eight waves take about as many,
 // at 2.1 GHz: the power that the products draw holds the clock there (the same launch over zeros 1.76 ms, at 2.4 GHz).  A product of 8192 x 8192 x 8192 runs at 1.2 - 1.35 PFLOP/s on
 // such numbers, 1.8 on zeros.  First form, each read waited for: 2.71 ms.
-template <int S, int T, int DP, int NW, bool ONE, bool SCORED>
-__global__ __launch_bounds__(NW * 64) void kv_tile_kernel(KvAttend a)
+// ALONE: one workgroup a CU, whose waves then may have more than 128 registers (run()).
+template <int S, int T, int DP, int NW, bool ONE, bool SCORED, bool ALONE = false>
+__global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(NW / 4, ALONE ? NW / 4 : 8))) void kv_tile_kernel(KvAttend a)
 {
     constexpr int BR = NW * 32;
     using Sc = KvScaling<S, T>;
@@ -1439,7 +1440,12 @@ hipError_t run(KvAttend a, hipStream_t s)
             if (alike) a.few_rows = 0;
             cut(a, units * a.c.H, tiles, BR, a.num_cu, 8, (alike ? 1 : 4) * a.num_cu, 16);
             const dim3 grid((unsigned)(units * a.n_split * a.c.H));
-            if (a.c.P >= kKvTile) kv_tile_kernel<S, T, DP, NW, true, SCORED><<<grid, NW * 64, 0, s>>>(a);
+            // Of 64 channels at bf16 the compiler gets by with 127 registers, so that two workgroups fit a CU: 15 % less time where there are workgroups for that, 17 % more where
+            // there are not, as there the 140 that it takes when told of one workgroup give the better order.  8 heads of 4, us, as chosen (other): 2048 tokens over 16384, 256
+            // workgroups, 334 (390); 4096 tokens 594 (588); 2100, 3000 tokens 529 (577), 544 (578); 16384 over 16384 1254 (1385).
+            constexpr bool PAIRS = S == PK_BF16 && DP == 64 && !SCORED;
+            if (a.c.P >= kKvTile && PAIRS && (int64_t)grid.x <= a.num_cu) kv_tile_kernel<S, T, DP, NW, true, SCORED, PAIRS><<<grid, NW * 64, 0, s>>>(a);
+            else if (a.c.P >= kKvTile) kv_tile_kernel<S, T, DP, NW, true, SCORED><<<grid, NW * 64, 0, s>>>(a);
             else kv_tile_kernel<S, T, DP, NW, false, SCORED><<<grid, NW * 64, 0, s>>>(a);
             if (a.n_split > 1) kv_join_kernel<T, DP, BR, false><<<dim3((unsigned)(units * (BR / 16)), a.c.H), 256, 0, s>>>(a);
         }
