@@ -1377,19 +1377,24 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttend a)
 
 // Parts that the keys are cut into (`tiles` tiles of 64 at most): so many that there are `wgs` workgroups, each with `least` tiles at least;
 // more of them, up to `more_wgs`, where each has `much` tiles, as sequences' lengths differ.  Within the room for partial results.  A window does
-// not enter: parts that lie outside it end at once and are joined as parts without a key (one token, window 4096 of 131072: 25 us).
-// A row's parts are joined one after the other, eight on their way, 0.13 us each, so that few long sequences of few heads are better off with fewer parts than
-// there are places: of T tiles 48 or 1.4 sqrt(T).  One token, us, so (and without): one head over 131072 keys, 4 bits 23 (50), bf16 25 (59); over 32768 14.5 (19), 14.4 (19); two
-// heads over 131072 24 (33), 31 (48); 4 heads over 65536 21 (23), 31 (39), over 200000 34 (34), 97 (89); 8 heads over 32768 18 (18), 32 (33), over 131072 34 (33), 104 (104).
-void cut(KvAttend &a, int64_t items, int64_t tiles, int rows, int64_t wgs, int least, int64_t more_wgs, int much)
+// not enter: parts that lie outside it end at once and are joined as parts without a key (one token, window 4096 of 131072: 8 heads 24 us, one 21).
+// `most` of them at most.
+void cut(KvAttend &a, int64_t items, int64_t tiles, int rows, int64_t wgs, int least, int64_t more_wgs, int much, int64_t most)
 {
     const int64_t room = a.part_floats / ((int64_t)rows * a.part_row) / std::max<int64_t>(items, 1);
     const int64_t want = std::max(std::min((wgs + items - 1) / items, tiles / least), std::min((more_wgs + items - 1) / items, tiles / much));
-    const int64_t most = std::max<int64_t>(48, (int64_t)(1.4 * std::sqrt((double)tiles)));
     const int64_t n = std::max<int64_t>(std::min({want, room, most}), 1);
     a.split_tiles = (int32_t)((tiles + n - 1) / n);
     a.n_split = (int32_t)((tiles + a.split_tiles - 1) / a.split_tiles);
 }
+
+// Most parts of the kernel for few rows.  A row's parts are joined one after the other, eight on their way, 0.13 us each, so that few long sequences of few heads are better off
+// with fewer parts than there are places: of T tiles 48 or 1.4 sqrt(T).  Measured, bf16, 8 query heads a head, us, so (and without): one token, one head over 32768 keys 15 (20), 131072 26
+// (58), 10^6 108 (136); two heads 17 (25), 32 (50), 212 (231); four 23 (30), 54 (58), 367 (412), over 200000 99 (90); eight 33 (35), 105 (105), 715 (752); 1024 listed
+// blocks, one head 21 (36), eight 56 (55); 4096 37 (69), 200 (205).
+// The kernel for many rows, whose tiles take 2 us each and not 0.2, is better off with all the places (run(), 32 tokens, one head over 131072 keys 60, with this limit 86; 10^6 180, 228;
+// two heads over 131072 64, 87; int8 67, 105; 256 channels 95, 135).
+int64_t most_parts(int64_t tiles) { return std::max<int64_t>(48, (int64_t)(1.4 * std::sqrt((double)tiles))); }
 
 template <int S, int T, int DP, bool SPARSE, bool SCORED>
 hipError_t run(KvAttend a, hipStream_t s)
@@ -1412,7 +1417,7 @@ hipError_t run(KvAttend a, hipStream_t s)
     if (SPARSE || !alike || rows <= a.few_rows) {
         a.row_tiles = (int32_t)((std::min<int64_t>(rows, a.few_rows) + 15) / 16);
         const int64_t units = seqs * a.row_tiles, items = units * a.c.H;
-        cut(a, items, tiles, 16, 2 * a.num_cu, 4, 16 * a.num_cu, 32);
+        cut(a, items, tiles, 16, 2 * a.num_cu, 4, 16 * a.num_cu, 32, most_parts(tiles));
         // The last part's workgroup joins them where all run at once: one token of 1025 keys 9.9 us, 7.1 + 3.8 with a launch of its own.  Where
         // there are many its fences cost more than a launch: 48 sequences of up to 32768 keys 494 us, 235 + 7 with the launch.
         a.join_here = items * a.n_split <= a.num_cu && items <= kKvArrivals;
@@ -1438,7 +1443,7 @@ hipError_t run(KvAttend a, hipStream_t s)
             const int64_t all = a.b.n_tokens * (int64_t)a.G, longs = std::min<int64_t>(a.b.n_seqs, all / (a.few_rows + 1));
             const int64_t units = alike ? seqs * ((rows + BR - 1) / BR) : std::min(longs * ((rows + BR - 1) / BR), all / BR + longs);
             if (alike) a.few_rows = 0;
-            cut(a, units * a.c.H, tiles, BR, a.num_cu, 8, (alike ? 1 : 4) * a.num_cu, 16);
+            cut(a, units * a.c.H, tiles, BR, a.num_cu, 8, (alike ? 1 : 4) * a.num_cu, 16, INT32_MAX);
             const dim3 grid((unsigned)(units * a.n_split * a.c.H));
             // Of 64 channels at bf16 the compiler gets by with 127 registers, so that two workgroups fit a CU: 15 % less time where there are workgroups for that, 17 % more where
             // there are not, as there the 140 that it takes when told of one workgroup give the better order.  8 heads of 4, us, as chosen (other): 2048 tokens over 16384, 256

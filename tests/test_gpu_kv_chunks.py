@@ -76,3 +76,10 @@ def run(storage, dtype, H, G, D, P, news, lens, window=0, seed=0):
                          ids=str)
 def test_chunks_of_64_channels(gpu_device, storage, H, G, D, P, news, lens):
     run(storage, "f16" if storage == "f16" else "bf16", H, G, D, P, news, lens, seed=1)
+
+
+@pytest.mark.parametrize("storage,dtype", [("bf16", "bf16"), ("i8", "bf16"), ("f4", "f16")])
+@pytest.mark.parametrize("H,G,D,P,news,lens", [(1, 8, 64, 64, [32], [70001]), (2, 8, 128, 16, [33], [33000]), (1, 8, 256, 64, [32], [66000]), (1, 16, 64, 32, [40, 20], [50000, 35000])], ids=str)
+def test_chunks_of_few_heads_in_many_parts(gpu_device, storage, dtype, H, G, D, P, news, lens):
+    """A part for every eight tiles of 64 keys, 64 and more of them."""
+    run(storage, dtype, H, G, D, P, news, lens, seed=2)
