@@ -13,7 +13,13 @@ constexpr int kThreads = 256;
 constexpr int kRowLanes = 16; // lanes that share a row: a quarter of a wave
 constexpr int kRowsAtOnce = kThreads / kRowLanes;
 
-// The larger and the smaller of two (without the rounds that fmaxf and fminf make for signalling NaNs: a quarter of an append's instructions).
+// The larger and the smaller of two (without the rounds that fmaxf and fminf make for signalling NaNs: a quarter of an append's instructions).  In a wave that is in the IEEE
+// mode, as it begins, a signalling NaN would come out as a quiet one, which the next maximum drops along with all before it; out of it a NaN of either
+// kind gives the other number.
+__device__ __forceinline__ void ignore_nans()
+{
+    __builtin_amdgcn_s_setreg(1 | 9 << 6 | 0 << 11, 0); // register MODE, from bit 9 (IEEE), one bit
+}
 __device__ __forceinline__ float larger(float a, float b)
 {
     float r;
@@ -225,6 +231,7 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(KvDev c, KvBatch b,
     constexpr bool FOUR = S == PK_F4;
     extern __shared__ __align__(16) char image[];
     __shared__ float red[4][2][DP];
+    ignore_nans();
     const int tid = threadIdx.x;
     KvPage g;
     if (!kv_page_of(c, b, g) || g.page >= c.n_pages) return;
