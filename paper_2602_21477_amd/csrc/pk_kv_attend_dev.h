@@ -156,13 +156,15 @@ struct KvRun {
 // y = cap tanh(x / cap) - slope |distance|, as a number that is scaled later, as products are:
 //   not capped          the product itself; a mask then costs nothing, a bias, in the products' units, two instructions a score
 //   cap <= kPlainCap    tanh z = 1 - 2 / (1 + e^2z): -1 / (1 + e^2z), whose scale is twice the cap; the cap itself, the same for all keys, is left to
-//                       the logarithm of the sum.  Off by 2^-23 of the cap, which is as little as a score of a few units is by itself
+//                       the logarithm of the sum.  Off by 2^-22 of the cap (measured; 2^-21 if all its operations are as far off as they may be), whatever the score's size: as
+//                       much as a score of a few units is by itself
 //   above               powers of two: beyond half the cap the same formula (its error is small beside such a score), below a polynomial, each score by
 //                       itself, so that it does not depend on what others there are; a wave that has none beyond does without the first
 // Measured, 4096 tokens over 32768, bf16, 32 query heads, us: not capped 2050, capped as here 2470 (with y itself 2585; all scores by the polynomial 2846; by the power, or
 // it where a wave has a score beyond half the cap, 3283).
 constexpr float kPlainCap = 64.f;
-__device__ __forceinline__ float score_offset(const KvAttend &a) { return a.cap <= kPlainCap ? a.cap * kLog2e : 0.f; } // (0 where scores are not capped)
+// Added to a maximum for the logarithm of the sum, before it is scaled: -1 / (1 + e^2z) + 1 / 2 is exact near 0, the cap added afterwards would leave 2^-18 of its own.
+__device__ __forceinline__ float score_middle(const KvAttend &a) { return a.cap > 0.f && a.cap <= kPlainCap ? 0.5f : 0.f; }
 
 struct KvScoring {
     float z, cap; // products times z: 2 x / cap as a power of two (above kPlainCap: x / cap)
@@ -229,8 +231,9 @@ struct KvSpan {
 };
 
 // What a workgroup (or the last one of a split row tile) does with a row of its results: 16 threads a row, four channels each at a time.
+// m: their largest score, in units of qscale.
 template <int T, int DP, typename F>
-__device__ __forceinline__ void kv_write_row(const KvAttend &a, int h, int tok, int member, int sub, float m, float l, F value)
+__device__ __forceinline__ void kv_write_row(const KvAttend &a, int h, int tok, int member, int sub, float m, float qscale, float l, F value)
 {
     const size_t oh = (size_t)tok * a.c.H * a.G + h * a.G + member;
     const float inv = l > 0.f ? 1.f / l : 0.f;
@@ -241,7 +244,7 @@ __device__ __forceinline__ void kv_write_row(const KvAttend &a, int h, int tok, 
         const f32x4 y = value(dd) * inv;
         *reinterpret_cast<u32x2 *>(a.out + (oh * a.c.D + dd) * 2) = u32x2{pack16<T>(y[0], y[1]), pack16<T>(y[2], y[3])};
     }
-    if (sub == 0 && a.lse) a.lse[oh] = l > 0.f ? (m + score_offset(a) + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+    if (sub == 0 && a.lse) a.lse[oh] = l > 0.f ? ((m + score_middle(a)) * qscale + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
 }
 
 // The parts of row r of a tile of BR rows joined, from part `first` on and in order: their largest maximum, and sums and 4 channels in 64 in its
@@ -693,7 +696,7 @@ __global__ __launch_bounds__(256, DP * kv_bits<S> / 8 > 128 || (S == PK_F4 && DP
         return y;
     };
     if (a.n_split == 1) {
-        if (in_row) kv_write_row<T, DP>(a, h, otok, omember, sub, mm * jq, ll, joined);
+        if (in_row) kv_write_row<T, DP>(a, h, otok, omember, sub, mm, jq, ll, joined);
         return;
     }
     const size_t slot = (size_t)unit * c.H + h, first = slot * a.n_split;
@@ -721,7 +724,7 @@ __global__ __launch_bounds__(256, DP * kv_bits<S> / 8 > 128 || (S == PK_F4 && DP
     float jm, jl;
     f32x4 y[DP / 64];
     kv_join_parts<DP, 16>(a, first, r, sub, jq, jm, jl, y);
-    kv_write_row<T, DP>(a, h, otok, omember, sub, jm * jq, jl, [&](int dd) __attribute__((always_inline)) { return y[dd / 64]; });
+    kv_write_row<T, DP>(a, h, otok, omember, sub, jm, jq, jl, [&](int dd) __attribute__((always_inline)) { return y[dd / 64]; });
 }
 
 // ------------------------------------------------------------------ long chunks
@@ -1345,7 +1348,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(NW / 4,
             const int dd = d * 32 + (b + hf) * 8;
             if (dd < c.D) *reinterpret_cast<u32x4 *>(a.out + (oh * c.D + dd) * 2) = u32x4{x[0], y[0], x[1], y[1]};
         }
-    if (hf == 0 && a.lse) a.lse[oh] = l > 0.f ? (m * qscale + score_offset(a) + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+    if (hf == 0 && a.lse) a.lse[oh] = l > 0.f ? ((m + score_middle(a)) * qscale + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
 }
 
 // The parts of a row joined, in order: 16 threads a row.  Parts have BR rows; a workgroup joins 16 of them.  BR 16: the parts of the kernel
@@ -1372,7 +1375,7 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttend a)
     float m, l;
     f32x4 y[DP / 64];
     kv_join_parts<DP, BR>(a, at, r, sub, qscale, m, l, y);
-    kv_write_row<T, DP>(a, h, tok, row % a.G, sub, m * qscale, l, [&](int dd) __attribute__((always_inline)) { return y[dd / 64]; });
+    kv_write_row<T, DP>(a, h, tok, row % a.G, sub, m, qscale, l, [&](int dd) __attribute__((always_inline)) { return y[dd / 64]; });
 }
 
 // Parts that the keys are cut into (`tiles` tiles of 64 at most): so many that there are `wgs` workgroups, each with `least` tiles at least;

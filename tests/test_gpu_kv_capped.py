@@ -1,0 +1,70 @@
+"""Attention with caps, slopes and scales at the ends of what they may be, and lse of rows that see few keys with scores far below their cap.
+
+Tolerances are those of test_gpu_kv_scored, but for a score's error by its cap, which there is 2^-21 of the score or of the cap.  Caps up to 64 are -1 / (1 + 2^p) in units of twice the cap, whatever the score:
+p is off by 4 roundings, 2^-22 of itself, which moves 1 / (1 + 2^p) by 2^-22 |z| sech^2 z / 2 <= 2^-22 0.23; 2^p by 2^-23 of itself, which moves it by 2^-25; the sum is rounded by 2^-24 of itself and the
+reciprocal by 2^-23 of itself, but no more than 2^-24 as it is below 1: together below (0.23 + 0.125 + 0.25 + 0.25) 2^-22, twice the cap: 2^-21 0.86 of it.  A sum with 1/2, for lse, adds 2^-25 of twice the cap
+where it is not exact: 2^-21 of the cap in all.
+lse: also 2^-20 ln 2, of int8 under bfloat16 2^-17 ln 2.  Weights are 2^(x + top - m), top 15, 16 or 127: top - m, where m is a little below 0, is rounded to 2^-20 (16 to 32) or 2^-17 (128 to 256), the
+same factor for all weights of a sum, which cancels in a result and is left in the logarithm."""
+import math
+
+import pytest
+import torch
+
+from paper_2602_21477_amd import binding as B
+import test_gpu_kv as base
+import test_gpu_kv_scored as scored
+from test_gpu_kv import U
+
+pytestmark = pytest.mark.gpu
+
+
+class Setup(scored.Setup):
+    def check_all(self, out, lse, scale, how):
+        """All of test_gpu_kv_scored's, but for the cap's error."""
+        ks, vs = self.stored()
+        u_out, u_w = U[self.kind], 2 * U[torch.float16] if self.storage in ("i8", "f8") else U[self.kind]
+        out, lse, q, cap = out.cpu().double(), lse.cpu().double(), self.q.double(), float(how["cap"])
+        slopes = how["slopes"].double() if "slopes" in how else torch.zeros(self.H * self.G, dtype=torch.float64)
+        for row, i, pos in self.tokens():
+            key = torch.arange(self.lens[i])
+            mask = key <= pos
+            if "starts" in how:
+                mask &= key >= how["starts"][row]
+            if "prefix" in how:
+                mask |= key < how["prefix"][i]
+            for h in range(self.H):
+                k, v, far = ks[i][mask, h], vs[i][mask, h], (pos - key[mask]).abs().double()
+                rows = slice(h * self.G, (h + 1) * self.G)
+                where = f"row {row} sequence {i} position {pos} head {h}"
+                x = (q[row, rows] @ k.T) * scale
+                size = ((q[row, rows].abs() @ k.abs().T) * abs(scale)).amax(1, keepdim=True)
+                most = x.abs().amax(1, keepdim=True)
+                if cap:
+                    x = cap * torch.tanh(x / cap)
+                bias = slopes[rows, None] * far
+                x = x - bias
+                w = torch.softmax(x, 1)
+                near = x > x.amax(1, keepdim=True) - 60
+                by_cap = 2.0 ** -21 * cap if cap <= 64 else 2.0 ** -21 * (2 * most).clamp(max=cap)
+                off_score = (self.D + 8) * 2.0 ** -24 * size + by_cap + ((2.0 ** -22 * bias.abs() + 2.0 ** -23 * x.abs()) * near).amax(1, keepdim=True)
+                e = 2 * off_score + 2.0 ** -20
+                ref, a = w @ v, w @ v.abs()
+                cut = 2.0 ** -126 * v.abs().sum(0) + (2.0 ** -40 * v.shape[0] * v.abs().max() + 2.0 ** -24 if self.kind == torch.float16 else 2.0 ** -126)
+                bound = u_out * ref.abs() + (u_w + e) * (1 + u_out) * a + cut
+                off = (out[row, rows] - ref).abs()
+                assert torch.all(off <= bound), f"{where}: {float((off / bound).max())} of the bound"
+                full = torch.logsumexp(x, 1)
+                common = math.log(2) * (2.0 ** -17 if self.storage == "i8" and self.kind == torch.bfloat16 else 2.0 ** -20)
+                assert torch.all((lse[row, rows] - full).abs() <= e[:, 0] / 2 + 2.0 ** -20 * full.abs() + common), f"{where}: lse"
+
+
+@pytest.mark.parametrize("storage,dtype", scored.CODES)
+@pytest.mark.parametrize("cap", [1.0, 30.0, 50.0, 64.0, 65.0, 1000.0])
+@pytest.mark.parametrize("docs", [1, 3])
+def test_few_keys_with_scores_far_below_the_cap(gpu_device, storage, dtype, cap, docs):
+    for news in ([3, 2], [90, 1]):
+        s = Setup(storage, dtype, 2, 3, 64, 32, news, [130, 40], seed=81, spread=1.0)
+        s.q = (s.q.float() * 0.02).to(s.kind)
+        h = s.how(cap=cap, docs=docs)
+        s.check_all(*s.run(0.125, h), 0.125, h)
