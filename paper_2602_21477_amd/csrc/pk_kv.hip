@@ -666,7 +666,9 @@ int attend(pk_kv *kv, const pk_kv_batch *batch, const pk_rows *q, int32_t n_q_he
         // (a bias is made one of the products that the scale multiplies)
         if (scores->slopes && scale != 0.f && std::fabs(scale) < kLeastBiasedScale) return PK_ERR_UNSUPPORTED;
         a.scored = 1;
-        a.cap = scores->cap > 0.f ? std::min(std::max(scores->cap, 1e-30f), 1e37f) : 0.f; // (nothing, and no cap at all, in 32 bits)
+        // (nothing, and no cap at all, in 32 bits: a product over the cap, in the units of the scale, is a normal number)
+        const float most = std::min(std::fabs(scale), 1.f) * 0x1p126f;
+        a.cap = scores->cap > 0.f ? std::min({std::max(scores->cap, 1e-30f), scale != 0.f ? std::max(most, 128.f) : 1e37f, 1e37f}) : 0.f;
         a.slopes = scores->slopes;
         a.starts = scores->starts;
         a.prefix = scores->prefix;

@@ -68,3 +68,19 @@ def test_few_keys_with_scores_far_below_the_cap(gpu_device, storage, dtype, cap,
         s.q = (s.q.float() * 0.02).to(s.kind)
         h = s.how(cap=cap, docs=docs)
         s.check_all(*s.run(0.125, h), 0.125, h)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("cap", [65.0, 1e6, 1e30, 1e37, 3e38])
+@pytest.mark.parametrize("power", [12, 7])
+def test_wide_caps_of_small_scales(gpu_device, dtype, cap, power):
+    """Large products that a small scale brings to scores of a few units: a cap beyond 64 leaves them, whatever its size over the scale's."""
+    for storage in (dtype, "i8", "f8", "f4"):
+        for news in ([2, 1], [90, 1]):
+            s = Setup(storage, dtype, 1, 2, 64, 32, news, [130, 40], seed=82, spread=0.3)
+            large, scale = 2.0 ** power, 2.0 ** (-2 * power - 3)
+            s.q = s.q * large
+            s.k = [x * large for x in s.k]
+            s.write(news=s.lens, rows=(s.k, s.v))
+            h = s.how(cap=cap)
+            s.check_all(*s.run(scale, h), scale, h)
