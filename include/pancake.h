@@ -532,7 +532,7 @@ int pk_kv_attend(pk_kv *kv, const pk_kv_batch *batch, const pk_rows *q, int32_t 
  */
 typedef struct {
     float cap;             /* > 0, finite; 0: scores are not capped                      */
-    const float *slopes;   /* DEVICE [n_q_heads], finite, or NULL                        */
+    const float *slopes;   /* DEVICE [n_q_heads], finite (beyond 2^36: as that), or NULL */
     const int32_t *starts; /* DEVICE [n_tokens] or NULL                                  */
     const int32_t *prefix; /* DEVICE [n_seqs] tokens of a sequence or NULL               */
 } pk_kv_scores;

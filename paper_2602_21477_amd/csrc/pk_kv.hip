@@ -580,7 +580,7 @@ using namespace pk;
 
 namespace {
 
-constexpr float kLeastBiasedScale = 0x1p-60f;
+constexpr float kLeastBiasedScale = 0x1p-60f; // of products, or of capped scores: what a bias is made one of
 constexpr int kMaxHeads = 1024; // key/value heads of a cache, and query heads of one of them
 
 size_t up256(size_t v) { return (v + 255) / 256 * 256; }
@@ -668,7 +668,7 @@ int attend(pk_kv *kv, const pk_kv_batch *batch, const pk_rows *q, int32_t n_q_he
         a.scored = 1;
         // (nothing, and no cap at all, in 32 bits: a product over the cap, in the units of the scale, is a normal number)
         const float most = std::min(std::fabs(scale), 1.f) * 0x1p126f;
-        a.cap = scores->cap > 0.f ? std::min({std::max(scores->cap, 1e-30f), scale != 0.f ? std::max(most, 128.f) : 1e37f, 1e37f}) : 0.f;
+        a.cap = scores->cap > 0.f ? std::min({std::max(scores->cap, kLeastBiasedScale), scale != 0.f ? std::max(most, 128.f) : 1e37f, 1e37f}) : 0.f;
         a.slopes = scores->slopes;
         a.starts = scores->starts;
         a.prefix = scores->prefix;

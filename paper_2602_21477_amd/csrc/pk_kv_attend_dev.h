@@ -165,6 +165,7 @@ struct KvRun {
 constexpr float kPlainCap = 64.f;
 // Added to a maximum for the logarithm of the sum, before it is scaled: -1 / (1 + e^2z) + 1 / 2 is exact near 0, the cap added afterwards would leave 2^-18 of its own.
 __device__ __forceinline__ float score_middle(const KvAttend &a) { return a.cap > 0.f && a.cap <= kPlainCap ? 0.5f : 0.f; }
+constexpr float kMostSlope = 0x1p36f; // over the least unit of y, 2^-60, and times any distance, it is a number
 
 struct KvScoring {
     float z, cap; // products times z: 2 x / cap as a power of two (above kPlainCap: x / cap)
@@ -179,7 +180,7 @@ struct KvScoring {
         if (plain) z *= 2.f * kLog2e;
         z = fminf(z, 3e38f);
         if (capped) qscale = plain ? 2.f * cap : 1.f;
-        slope = biased ? a.slopes[query_head] * kLog2e / qscale : 0.f;
+        slope = biased ? __builtin_amdgcn_fmed3f(a.slopes[query_head], -kMostSlope, kMostSlope) * kLog2e / qscale : 0.f;
     }
     // z times a polynomial in z^2 that was fitted to tanh(z) / z up to 1/2 (off by 2^-26 of it), times the cap.
     __device__ __forceinline__ float near(float x) const

@@ -84,3 +84,39 @@ def test_wide_caps_of_small_scales(gpu_device, dtype, cap, power):
             s.write(news=s.lens, rows=(s.k, s.v))
             h = s.how(cap=cap)
             s.check_all(*s.run(scale, h), scale, h)
+
+
+@pytest.mark.parametrize("storage,dtype", [("bf16", "bf16"), ("i8", "bf16"), ("f4", "f16")])
+@pytest.mark.parametrize("cap", [0.0, 1e-38, 2.0, 1000.0])
+@pytest.mark.parametrize("slope", [1e9, 1e25, 3e38])
+def test_steep_slopes_leave_the_nearest_key(gpu_device, storage, dtype, cap, slope):
+    """All weight is the nearest key's (with the other sign the farthest one's), and no product with a distance is anything but a number."""
+    for news in ([2, 1], [90, 1]):
+        for sign in (1.0, -1.0):
+            s = Setup(storage, dtype, 1, 2, 64, 32, news, [130, 40], seed=83, spread=0.3)
+            n = sum(news)
+            _, vs = s.stored()
+            where = {"slopes": torch.full((2,), sign * slope), "cap": cap}
+            # everything; and a prefix alone, each query's nearest key then far away
+            for extra, nearest, farthest in (({}, lambda pos: pos, lambda pos: 0), ({"starts": torch.full((n,), 10 ** 6, dtype=torch.int32), "prefix": torch.tensor([9, 9], dtype=torch.int32)},
+                                                                                     lambda pos: min(pos, 8), lambda pos: 0 if pos >= 4 else 8)):
+                out, lse = s.run(0.125, {**where, **extra})
+                for row, i, pos in s.tokens():
+                    if "prefix" in extra and pos in (4,):
+                        continue  # (both ends as far)
+                    v = vs[i][nearest(pos) if sign > 0 else farthest(pos), 0]
+                    off = (out[row].cpu().double() - v).abs()
+                    # one weight, of 1: its rounding with a value's scale, and the result's
+                    assert bool((off <= 2 * 2 * U[s.kind] * v.abs() + 2.0 ** -24).all()), (row, pos, sign, float(off.max()))
+                    assert not bool(lse[row].isnan().any()), (row, pos)
+
+
+@pytest.mark.parametrize("storage,dtype", [("bf16", "bf16"), ("f8", "f16")])
+@pytest.mark.parametrize("cap", [1e-40, 1e-25, 2.0 ** -61])
+def test_caps_of_next_to_nothing(gpu_device, storage, dtype, cap):
+    """Every key that is seen weighs the same, or by its distance alone."""
+    for news in ([2, 1], [90, 1]):
+        s = Setup(storage, dtype, 1, 2, 64, 32, news, [130, 40], seed=84, spread=0.3)
+        for kind in (dict(cap=cap), dict(cap=cap, slopes=1.0), dict(cap=cap, slopes=-0.01)):
+            h = s.how(**kind)
+            s.check_all(*s.run(0.125, h), 0.125, h)
