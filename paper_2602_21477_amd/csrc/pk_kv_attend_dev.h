@@ -160,8 +160,8 @@ struct KvRun {
 //                       much as a score of a few units is by itself
 //   above               powers of two: beyond half the cap the same formula (its error is small beside such a score), below a polynomial, each score by
 //                       itself, so that it does not depend on what others there are; a wave that has none beyond does without the first
-// Measured, 4096 tokens over 32768, bf16, 32 query heads, us: not capped 2050, capped as here 2470 (with y itself 2585; all scores by the polynomial 2846; by the power, or
-// it where a wave has a score beyond half the cap, 3283).
+// Measured, 4096 tokens over 32768, bf16, 32 query heads, us: not capped 2000, a cap of 30 2300 - 2420, of 1000 (no score near half of it) 3700, slopes alone 2620.  When a cap of 30 took 2470: with
+// y itself 2585, all scores by the polynomial 2846, by the power, or it where a wave has a score beyond half the cap, 3283.
 constexpr float kPlainCap = 64.f;
 // Added to a maximum for the logarithm of the sum, before it is scaled: -1 / (1 + e^2z) + 1 / 2 is exact near 0, the cap added afterwards would leave 2^-18 of its own.
 __device__ __forceinline__ float score_middle(const KvAttend &a) { return a.cap > 0.f && a.cap <= kPlainCap ? 0.5f : 0.f; }
@@ -308,7 +308,7 @@ __device__ __forceinline__ void kv_join_parts(const KvAttend &a, size_t first, i
 // parts reads few of them.  ONE: a tile of keys lies in one page.
 // Measured (medians), 8 heads of 128, 4 query heads each: one token of each of 48 sequences of up to 32768 tokens, int8, 1.22 GB in 235 us,
 // 5.2 TB/s (without what is asked for ahead 446); one token of 1025, bf16, 9.2 us, a chain of lengths, pages, keys and the join.
-// Of 256 channels at 16 bits K and V do not fit the 512 registers of one wave a SIMD: 70 - 122 of them go to scratch, 268 - 376 bytes a lane (48
+// Of 256 channels at 16 bits K and V do not fit the 512 registers of one wave a SIMD: 69 - 128 of them go to scratch, 268 - 376 bytes a lane (48
 // sequences of 8192 bf16 tokens, a token each, 787 us, 4.1 TB/s; int8, with no scratch, 296 us, 5.5 TB/s; 4 bits 172 us, 250 where two waves of a SIMD have 256 registers each).
 // 4 bits: one token of each of 48 sequences of up to 65536 tokens, 128 channels, 1.11 GB in 228 us, 4.9 TB/s: three waves a SIMD with half the bytes of 8 bits on
 // their way, vector units 38 % busy.
@@ -1044,10 +1044,10 @@ struct KvTiles {
 // The running maximum is of the bare products (the queries carry the scale's sign); O is rescaled only when some query's maximum
 // has grown.  Once a wave has met a maximum beyond kNear, its scores are lessened by it before they are scaled, in the branch that else
 // masks them.  In every tile that cost a long chunk 2.2 % and mixed chunks 2.7 % (the maximum so far as the products' start value: 2.5 and 5 %,
-// as most tiles raise some query's); so 0.1 - 0.4 and 1 %.  The masks are bits: of comparisons for each key 16381 tokens in documents of 700 took 477 us, so 325.  Of 256 channels, which leave no register, in every tile all the same: 2048 tokens
+// as most tiles raise some query's); so 0.1 - 0.4 and 1 %.  The masks are bits: of comparisons for each key 16381 tokens in documents of 700 took 477 us, so 325 (304 now).  Of 256 channels, which leave no register, in every tile all the same: 2048 tokens
 // over 8192, bf16, 702 us, in the branch 749, not at all 690.  ONE: a tile of keys lies in one page.
-// Measured, bf16, 32 query heads of 128 channels: 4096 tokens over 32768 2.04 ms (median; from card to card and run to run 1.99 - 2.19), 1.0 PFLOP/s.
-// 4.45 million cycles, of which the matrix cores are busy for 44 % and the reads of K and V out of LDS by eight waves take about as many,
+// Measured, bf16, 32 query heads of 128 channels: 4096 tokens over 32768 2.00 ms (median; from card to card and run to run 1.97 - 2.10), 1.0 PFLOP/s.
+// 4.25 million cycles, of which the matrix cores are busy for 46 % and the reads of K and V out of LDS by eight waves take about as many,
 // at 2.1 GHz: the power that the products draw holds the clock there (the same launch over zeros 1.76 ms, at 2.4 GHz).  A product of 8192 x 8192 x 8192 runs at 1.2 - 1.35 PFLOP/s on
 // such numbers, 1.8 on zeros.  First form, each read waited for: 2.71 ms.
 // ALONE: one workgroup a CU, whose waves then may have more than 128 registers (run()).
@@ -1440,7 +1440,7 @@ hipError_t run(KvAttend a, hipStream_t s)
     if constexpr (!SPARSE) {
         if (rows > a.few_rows) {
             // (a wave holds 32 x DP sums and the queries: of 256 channels these take all 512 registers, one wave a SIMD, and more over pages of
-            // fewer than 64 tokens: 36 go to scratch at 16 bits, 52 with scores of other kinds; 2048 tokens over 8192 705 - 760 us at bf16, 930 at int8.  Of 64 channels 4 waves a workgroup were slower: 16 ragged sequences 171 us, 143
+            // fewer than 64 tokens: 38 go to scratch at 16 bits, 53 with scores of other kinds; 2048 tokens over 8192 700 - 720 us at 16 bits, 1030 - 1040 over such pages, 907 at int8 under bf16.  Of 64 channels 4 waves a workgroup were slower: 16 ragged sequences 171 us, 143
             // with 8)
             constexpr int NW = DP == 256 ? 4 : 8, BR = NW * 32;
             // row tiles of the sequences that have more rows than the others' kernel takes: at most
