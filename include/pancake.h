@@ -527,7 +527,9 @@ int pk_kv_attend(pk_kv *kv, const pk_kv_batch *batch, const pk_rows *q, int32_t 
  *   j < prefix, or start <= j <= p (window > 0: and j > p - window),  j in the sequence,
  * and its score is
  *   cap tanh(scale q.k / cap) - slope |p - j|
- * (off by 2^-21 of a cap up to 64, by 2^-21 of itself under a wider one, beside the product's rounding).  A prefix is seen by queries before its end too.  start: of the query's token, the first position of its document; negative ones are 0.
+ * A prefix is seen by queries before its end too.  start: of the query's token, the first position of its document; negative ones are 0.
+ * Beside the product's rounding a score is off by no more than 2^-21 of its cap (caps up to 64) or of itself (wider ones), and a bias by 2^-22 of itself.  Caps below
+ * 2^-60 count as that, and wide ones as no more than 2^126 times the scale.
  * PK_ERR_UNSUPPORTED also for slopes with a scale between 0 and 2^-60.
  */
 typedef struct {
